@@ -59,7 +59,8 @@ typedef enum {
   PE_OP_PREFILL_PRUNE = 1,
   PE_OP_EVICT_BLOCKS = 2,
   PE_OP_PAGED_DECODE = 3,
-  PE_OP_APPEND_PAGED_DECODE = 4
+  PE_OP_APPEND_PAGED_DECODE = 4,
+  PE_OP_TREE_DECODE = 5
 } pe_op;
 
 /* Cache layout (Sec. 2.4 leaves the granularity open).
@@ -95,8 +96,8 @@ typedef struct pe_cache_desc {
 } pe_cache_desc;
 
 /* Bytes of device workspace `op` needs for `desc`.  `total_tokens` is the packed prompt length
- * (sum of L) for PE_OP_PREFILL_PRUNE and ignored otherwise.  Returns 0 for ops that need none and
- * for an invalid desc.  For the attention ops the size follows pe_decode_splits(desc). */
+ * (sum of L) for PE_OP_PREFILL_PRUNE, the number of drafts for PE_OP_TREE_DECODE, and ignored otherwise.  Returns 0 for ops
+ * that need none and for an invalid desc.  For the attention ops (4) the size follows pe_decode_splits(desc). */
 size_t pe_workspace_bytes(int op, const pe_cache_desc* desc, int64_t total_tokens);
 
 /* Static string for a pe_status value. */
@@ -334,6 +335,49 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
                                   const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* freed_phys,
                                   const int32_t* spare, int32_t* spare_used, int32_t n_spare, float softmax_scale,
                                   void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * (5) Attention of a tree of drafted tokens over the cache -- Eq. 1 for up to PE_MAX_DRAFTS queries per sequence at once, as
+ *     a verification of speculative decoding asks for (the paper has one query a step; nothing in the cache changes).
+ *     Draft i of sequence s attends to the seq_lens[s] cached tokens and to those drafts j < draft_lens[s] of the same sequence
+ *     whose bit j is set in tree_mask[s][i] (bit 0 the lowest; its own bit is not implied, later bits are not looked at, and a
+ *     mask need not describe a tree: a chain's word is (2 << i) - 1):
+ *     out[s][i][h][:] = sum_a softmax_a(softmax_scale * <q[s][i][h], k_a>) v_a over those tokens a, with the keys and values of
+ *     row (s, h / (Hq/Hk)) of the cache and of head h / (Hq/Hk) of the drafts.  A query that attends to nothing gives zeros.
+ *     fp32 accumulation, output rounded to desc->dtype.
+ *     q, out: [S][num_drafts][Hq][D].  k_draft, v_draft: [S][num_drafts][Hk][D], read only, not part of the cache.
+ *     draft_lens: [S] int32, or NULL where every sequence has num_drafts (values are taken as if clamped to 0..num_drafts);
+ *     rows of `out` behind a sequence's last draft are left as they were.  tree_mask: [S][num_drafts] 64-bit words.
+ *     q, the drafts in use and the tokens attended to are finite; what lies behind a row's end or behind a sequence's last
+ *     draft may be anything.  A draft in use is finite even where no mask names it.
+ *     `out` may be q itself and must not otherwise overlap what is read.  desc->decode_splits is the number of splits of a row here too (0: the
+ *     library's choice); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
+ *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29.
+ *     workspace: pe_workspace_bytes(PE_OP_TREE_DECODE, desc, num_drafts) (split partials).
+ *     shared: block_table [S][max_blocks].
+ */
+#define PE_MAX_DRAFTS 64
+int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q, const void* k_draft, const void* v_draft,
+                   const int32_t* draft_lens, const uint64_t* tree_mask, const void* k_pool, const void* v_pool,
+                   const int32_t* block_table, const int32_t* seq_lens, float softmax_scale, void* out, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/*
+ * What follows a verification: the accepted drafts join the cache, in the order of path[s][0 .. path_lens[s]).  Each call
+ * appends drafts path[s][path_done[s] ...] of every sequence, up to the end of its newest page or of its path, whichever comes
+ * first, so that a caller can score and evict (3) when a page has filled and call again for the rest: with slot =
+ * seq_lens[s] % B, min(path_lens[s] - path_done[s], B - slot) tokens go to the newest page (slot 0: a new page is linked in
+ * first, as in pe_append_kv), and seq_lens[s] and path_done[s] grow by their number.  A sequence with nothing left is untouched.
+ * A draft may be named more than once.  The path ends in front of an entry outside 0..num_drafts-1.
+ * k_draft, v_draft: as in (5), not overlapping the pools.  path: [S][max_path] int32.  path_lens, path_done: [S] int32 (path_done
+ * is 0 for a new path; values of path_lens above max_path count as max_path).  spare, spare_used, freed_phys as in
+ * pe_append_kv; a sequence with seq_lens[s] >= max_blocks*B is left untouched.  At most 65536 KV heads.
+ * shared: as in pe_append_kv.
+ */
+int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_draft, const void* v_draft, const int32_t* path,
+                   int32_t max_path, const int32_t* path_lens, int32_t* path_done, void* k_pool, void* v_pool,
+                   int32_t* block_table, int32_t* seq_lens, int32_t* freed_phys, const int32_t* spare, int32_t* spare_used,
+                   int32_t n_spare, void* stream);
 
 #ifdef __cplusplus
 }

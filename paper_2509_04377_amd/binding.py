@@ -22,12 +22,15 @@ PE_ERR_INVALID_ARG, PE_ERR_UNSUPPORTED, PE_ERR_WORKSPACE, PE_ERR_HIP = -1, -2, -
 PE_F32, PE_BF16 = 0, 1
 PE_OP_SCORE_BLOCKS, PE_OP_PREFILL_PRUNE, PE_OP_EVICT_BLOCKS, PE_OP_PAGED_DECODE = 0, 1, 2, 3
 PE_OP_APPEND_PAGED_DECODE = 4
+PE_OP_TREE_DECODE = 5
+PE_MAX_DRAFTS = 64
 PE_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
 EXPORTS = ["pe_workspace_bytes", "pe_status_string", "pe_version", "pe_decode_splits",
            "pe_score_blocks", "pe_prefill_prune", "pe_evict_blocks", "pe_paged_decode", "pe_append_kv",
            "pe_append_paged_decode", "pe_score_recent_blocks", "pe_evict_blocks_cached", "pe_evict_blocks_ex", "pe_score_evict",
-           "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers"]
+           "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers",
+           "pe_tree_decode", "pe_append_path"]
 
 
 class pe_cache_desc(ctypes.Structure):
@@ -134,6 +137,10 @@ def lib():
         L.pe_score_recent_blocks.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp]
         L.pe_evict_blocks_cached.restype = ctypes.c_int
         L.pe_evict_blocks_cached.argtypes = [dp, vp, vp, vp, i32, vp, vp, vp]
+        L.pe_tree_decode.restype = ctypes.c_int
+        L.pe_tree_decode.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+        L.pe_append_path.restype = ctypes.c_int
+        L.pe_append_path.argtypes = [dp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached"):
@@ -383,3 +390,26 @@ def pe_append_paged_decode_layers(desc, num_layers, new_k, new_v, q, k_pool, v_p
                                                  _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]),
                                                  float(softmax_scale), _addr(out, "out"), wp, wn, _stream())
     check(status, "pe_append_paged_decode_layers")
+
+
+def pe_tree_decode(desc, num_drafts, q, k_draft, v_draft, draft_lens, tree_mask, k_pool, v_pool, block_table, seq_lens,
+                   softmax_scale, out, workspace=None):
+    """tree_mask: int64 (bit j of a word is draft j; bit 63 the sign)."""
+    wp, wn = _ws(workspace)
+    check(lib().pe_tree_decode(ctypes.byref(desc), int(num_drafts), _addr(q, "q"), _addr(k_draft, "k_draft"),
+                               _addr(v_draft, "v_draft"), _addr_opt(draft_lens, "draft_lens", torch.int32),
+                               _addr(tree_mask, "tree_mask", torch.int64), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                               _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                               float(softmax_scale), _addr(out, "out"), wp, wn, _stream()), "pe_tree_decode")
+
+
+def pe_append_path(desc, k_draft, v_draft, path, path_lens, path_done, k_pool, v_pool, block_table, seq_lens, freed_phys, spare,
+                   spare_used):
+    check(lib().pe_append_path(ctypes.byref(desc), int(k_draft.shape[1]), _addr(k_draft, "k_draft"), _addr(v_draft, "v_draft"),
+                               _addr(path, "path", torch.int32), int(path.shape[-1]),
+                               _addr(path_lens, "path_lens", torch.int32), _addr(path_done, "path_done", torch.int32),
+                               _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                               _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                               _addr(freed_phys, "freed_phys", torch.int32), _addr(spare, "spare", torch.int32),
+                               _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]), _stream()),
+          "pe_append_path")
