@@ -60,7 +60,8 @@ typedef enum {
   PE_OP_EVICT_BLOCKS = 2,
   PE_OP_PAGED_DECODE = 3,
   PE_OP_APPEND_PAGED_DECODE = 4,
-  PE_OP_TREE_DECODE = 5
+  PE_OP_TREE_DECODE = 5,
+  PE_OP_SELECT_PAGES = 6
 } pe_op;
 
 /* Cache layout (Sec. 2.4 leaves the granularity open).
@@ -378,6 +379,34 @@ int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_
                    int32_t max_path, const int32_t* path_lens, int32_t* path_done, void* k_pool, void* v_pool,
                    int32_t* block_table, int32_t* seq_lens, int32_t* freed_phys, const int32_t* spare, int32_t* spare_used,
                    int32_t n_spare, void* stream);
+
+/*
+ * (6) Attention over selected pages: of a cache that is not pruned (or hardly), each query reads the pages whose keys can give
+ *     the largest products with it.  Three calls: pe_page_bounds when pages fill, and in a decode step pe_select_pages, whose
+ *     outputs are a table and lengths that pe_paged_decode (with a desc of max_blocks = num_pages) or pe_tree_decode read.
+ *
+ * pe_page_bounds: the elementwise smallest and largest key of full pages, in desc->dtype (values of keys: nothing is rounded),
+ * kept by physical page, so that they stay right when tables are compacted and only pages that fill have to be bounded again.
+ *     bounds[page][0][d] = min_i K[i][d], bounds[page][1][d] = max_i K[i][d] over the page's B tokens
+ * for the pages block_table[s][hk][j], max(0, n - recent) <= j < n = seq_lens[s] / B, of every row; recent = 0: for every full
+ * page.  Others are left as they were.  bounds: [num_phys_blocks][2][D], 16-byte aligned; shared: [num_phys_blocks][2][Hk][D].
+ *
+ * pe_select_pages: of a row with n = ceil(seq_lens[s] / B) pages, the newest one (full or not) and the min(num_pages, n) - 1
+ * others with the highest scores (ties: lowest index), in their order.  The score of page j is
+ *     sum over the query heads h of the row, sum_d max(q[s][h][d] lo[d], q[s][h][d] hi[d])
+ * -- for each head no less than its product with any key of the page -- accumulated in fp64 and rounded once to fp32.
+ * Only the bounds of full pages other than the newest are read, and those only of rows with more than num_pages pages.
+ *     q: [S][Hq][D].  block_table_out: [S][Hk][num_pages], the physical pages, -1 padded.  seq_lens_out: [S], the tokens in
+ * them (the same for all heads).  page_idx_out: NULL, or [S][Hk][num_pages], their logical indices in block_table, ascending, -1
+ * padded.  The outputs must not overlap block_table or seq_lens.
+ *     workspace: pe_workspace_bytes(PE_OP_SELECT_PAGES, desc, 0) (the scores).
+ *     shared: one selection per sequence, over the query heads of all KV heads; block_table_out, page_idx_out [S][num_pages].
+ */
+int pe_page_bounds(const pe_cache_desc* desc, const void* k_pool, const int32_t* block_table, const int32_t* seq_lens,
+                   int32_t recent, void* bounds_inout, void* stream);
+int pe_select_pages(const pe_cache_desc* desc, const void* q, const void* bounds, const int32_t* block_table,
+                    const int32_t* seq_lens, int32_t num_pages, int32_t* block_table_out, int32_t* seq_lens_out,
+                    int32_t* page_idx_out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,44 @@
+// Launch interfaces of the calls that bound pages' keys and select pages by a query.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "pe_check.h"
+
+namespace pe {
+
+struct BoundsArgs {
+  const void* k_pool;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  void* bounds;
+  int recent;  // 0: every full page; n: the n most recently filled ones of each row
+  int num_seqs, num_kv_heads, head_dim, block_size, max_blocks;
+  bool is_bf16, shared;
+};
+hipError_t launch_page_bounds(const BoundsArgs& a, hipStream_t stream);
+
+struct SelectArgs {
+  const void* q;
+  const void* bounds;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* idx_out;  // may be null
+  float* scores;     // workspace: [rows][max_blocks]
+  int pages;         // selected ones of a row, at most
+  int num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, max_blocks;
+  bool is_bf16, shared;
+};
+hipError_t launch_select_pages(const SelectArgs& a, hipStream_t stream);
+
+// One score for every table entry.
+inline size_t select_workspace_bytes(const pe_cache_desc* d) {
+  const int64_t rows = d->layout == PE_LAYOUT_SHARED ? d->num_seqs : (int64_t)d->num_seqs * d->num_kv_heads;
+  return (size_t)rows * d->max_blocks * sizeof(float);
+}
+
+}  // namespace pe
