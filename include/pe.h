@@ -61,7 +61,8 @@ typedef enum {
   PE_OP_PAGED_DECODE = 3,
   PE_OP_APPEND_PAGED_DECODE = 4,
   PE_OP_TREE_DECODE = 5,
-  PE_OP_SELECT_PAGES = 6
+  PE_OP_SELECT_PAGES = 6,
+  PE_OP_DECODE_WEIGHTS = 7
 } pe_op;
 
 /* Cache layout (Sec. 2.4 leaves the granularity open).
@@ -353,7 +354,7 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
  *     draft may be anything.  A draft in use is finite even where no mask names it.
  *     `out` may be q itself and must not otherwise overlap what is read.  desc->decode_splits is the number of splits of a row here too (0: the
  *     library's choice); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
- *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29.
+ *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29, at most 65536 KV heads.
  *     workspace: pe_workspace_bytes(PE_OP_TREE_DECODE, desc, num_drafts) (split partials).
  *     shared: block_table [S][max_blocks].
  */
@@ -407,6 +408,29 @@ int pe_page_bounds(const pe_cache_desc* desc, const void* k_pool, const int32_t*
 int pe_select_pages(const pe_cache_desc* desc, const void* q, const void* bounds, const int32_t* block_table,
                     const int32_t* seq_lens, int32_t num_pages, int32_t* block_table_out, int32_t* seq_lens_out,
                     int32_t* page_idx_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * (7) Paged decode attention that also keeps the weight each page got -- for an eviction by accumulated attention (the kind of
+ *     importance that the paper's attention-free score is the alternative to: Sec. 3), with the eviction calls of (3).
+ *     `out` as pe_paged_decode.  For every row and every page j < n = ceil(seq_lens[s] / B):
+ *        weights_out[s][hk][j] = decay * before + sum over the row's query heads h, sum over the page's tokens t of
+ *                                softmax_t(softmax_scale * <q[s][h], K_t>),
+ *     before = weights_in[s][hk][j] where that is finite, else 0 (a page's first step); entries j >= n become +INF.  fp32.
+ *     Kept from step to step, the array can be the scores of pe_evict_blocks_cached, or of pe_evict_blocks_ex with
+ *     cached_scores: these move its entries with the table and leave +INF where a page is gone, so that the next page there
+ *     begins with nothing.  (A page that has just filled has had little time to be attended to: pe_evict_blocks_ex can protect
+ *     the last ones.)
+ *     decay: 0..1; 1 adds up, less forgets.  weights_in: NULL (nothing before), or [S][Hk][max_blocks] fp32, which may be
+ *     weights_out itself; no other overlap with it, with q or with out.  out may be q itself.
+ *     workspace: pe_workspace_bytes(PE_OP_DECODE_WEIGHTS, desc, 0).  desc->decode_splits is the number of splits of a row (0: the
+ *     library's choice; more are used where a split would have over 61440 / (Hq/Hk) tokens of the table; tables for which 256 of
+ *     those are too few are PE_ERR_UNSUPPORTED), the other decode_* fields are not looked at.  At most 65536 KV heads.
+ *     shared: block_table [S][max_blocks]; the weights keep their shape (one row a head; evictions take the head mean).
+ */
+int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void* k_pool, const void* v_pool,
+                            const int32_t* block_table, const int32_t* seq_lens, float softmax_scale, float decay,
+                            const float* weights_in, float* weights_out, void* out, void* workspace, size_t workspace_bytes,
+                            void* stream);
 
 #ifdef __cplusplus
 }

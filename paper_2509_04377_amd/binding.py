@@ -22,7 +22,7 @@ PE_ERR_INVALID_ARG, PE_ERR_UNSUPPORTED, PE_ERR_WORKSPACE, PE_ERR_HIP = -1, -2, -
 PE_F32, PE_BF16 = 0, 1
 PE_OP_SCORE_BLOCKS, PE_OP_PREFILL_PRUNE, PE_OP_EVICT_BLOCKS, PE_OP_PAGED_DECODE = 0, 1, 2, 3
 PE_OP_APPEND_PAGED_DECODE = 4
-PE_OP_TREE_DECODE, PE_OP_SELECT_PAGES = 5, 6
+PE_OP_TREE_DECODE, PE_OP_SELECT_PAGES, PE_OP_DECODE_WEIGHTS = 5, 6, 7
 PE_MAX_DRAFTS = 64
 PE_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -30,7 +30,8 @@ EXPORTS = ["pe_workspace_bytes", "pe_status_string", "pe_version", "pe_decode_sp
            "pe_score_blocks", "pe_prefill_prune", "pe_evict_blocks", "pe_paged_decode", "pe_append_kv",
            "pe_append_paged_decode", "pe_score_recent_blocks", "pe_evict_blocks_cached", "pe_evict_blocks_ex", "pe_score_evict",
            "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers",
-           "pe_tree_decode", "pe_append_path", "pe_page_bounds", "pe_select_pages"]
+           "pe_tree_decode", "pe_append_path", "pe_page_bounds", "pe_select_pages",
+           "pe_paged_decode_weights"]
 
 
 class pe_cache_desc(ctypes.Structure):
@@ -145,6 +146,8 @@ def lib():
         L.pe_page_bounds.argtypes = [dp, vp, vp, vp, i32, vp, vp]
         L.pe_select_pages.restype = ctypes.c_int
         L.pe_select_pages.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.pe_paged_decode_weights.restype = ctypes.c_int
+        L.pe_paged_decode_weights.argtypes = [dp, vp, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp, vp, sz, vp]
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached"):
@@ -432,3 +435,13 @@ def pe_select_pages(desc, q, bounds, block_table, seq_lens, num_pages, block_tab
                                 int(num_pages), _addr(block_table_out, "block_table_out", torch.int32),
                                 _addr(seq_lens_out, "seq_lens_out", torch.int32),
                                 _addr_opt(page_idx_out, "page_idx_out", torch.int32), wp, wn, _stream()), "pe_select_pages")
+
+
+def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, softmax_scale, decay, weights_in, weights_out, out,
+                            workspace=None):
+    wp, wn = _ws(workspace)
+    check(lib().pe_paged_decode_weights(ctypes.byref(desc), _addr(q, "q"), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                        _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                        float(softmax_scale), float(decay), _addr_opt(weights_in, "weights_in", torch.float32),
+                                        _addr(weights_out, "weights_out", torch.float32), _addr(out, "out"), wp, wn, _stream()),
+          "pe_paged_decode_weights")

@@ -5,7 +5,7 @@
 // read and written by that workgroup alone, so both are updated in place.  Phase 1 links a new page into each row when the newest
 // one is full; phase 2 copies token rows, 16 bytes a lane.
 #include "pe_device.h"
-#include "pe_tree.h"
+#include "pe_rows.h"
 
 namespace pe {
 namespace {

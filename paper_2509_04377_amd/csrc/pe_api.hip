@@ -9,7 +9,7 @@
 #include "pe_check.h"
 #include "pe_launch.h"
 #include "pe_select.h"
-#include "pe_tree.h"
+#include "pe_rows.h"
 
 // Split partials of pe_paged_decode_static: one copy per GPU, held until the process ends.  In host code this
 // name is only a handle for hipGetSymbolAddress; kernels are given the address that call returns.
@@ -253,6 +253,8 @@ size_t pe_workspace_bytes(int op, const pe_cache_desc* desc, int64_t total_token
                                        desc->layout == PE_LAYOUT_SHARED);
     case PE_OP_TREE_DECODE:
       return pe::tree_workspace_bytes(desc, total_tokens);
+    case PE_OP_DECODE_WEIGHTS:
+      return pe::weights_workspace_bytes(desc);
     case PE_OP_SELECT_PAGES:
       return pe::select_workspace_bytes(desc);
     default:
