@@ -76,9 +76,10 @@ def _load_host():
     if os.path.exists(HOST_PATH):
         try:
             from . import _pe_host
-            if _pe_host.bind_descriptor(pe_cache_desc) == _layout(pe_cache_desc):
+            if (_pe_host.bind_descriptor(pe_cache_desc) == _layout(pe_cache_desc) and
+                    _pe_host.bind_evict_opts(pe_evict_opts) == _layout(pe_evict_opts)):
                 return _pe_host
-            why = "has another pe_cache_desc"
+            why = "has another pe_cache_desc or pe_evict_opts"
         except (ImportError, AttributeError) as e:
             why = "does not load: %s" % e
     warnings.warn("_pe_host.so %s (%s): arguments are checked in Python, some 3 us more a call; build as for libpe.so" % (why, HOST_PATH),
@@ -150,7 +151,8 @@ def lib():
         L.pe_paged_decode_weights.argtypes = [dp, vp, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp, vp, sz, vp]
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
-                     "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached"):
+                     "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
+                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages"):
             setattr(L, "addr_" + name, ctypes.cast(getattr(L, "pe_" + name), vp).value)
         _lib = L
     return _lib
@@ -326,13 +328,15 @@ def pe_evict_blocks_cached(desc, scores_inout, block_table, seq_lens, budget_tok
 
 
 def pe_evict_blocks_ex(desc, opts, scores, block_table, seq_lens, budget_tokens, evicted_logical_out, freed_phys_out):
-    check(lib().pe_evict_blocks_ex(ctypes.byref(desc), ctypes.byref(opts),
-                                    _addr_opt(scores, "scores", torch.float32),
-                                    _addr(block_table, "block_table", torch.int32),
-                                    _addr(seq_lens, "seq_lens", torch.int32), int(budget_tokens),
-                                    _addr(evicted_logical_out, "evicted_logical_out", torch.int32),
-                                    _addr(freed_phys_out, "freed_phys_out", torch.int32), _stream()),
-           "pe_evict_blocks_ex")
+    L = lib()
+    status = _host.evict_blocks_ex(L.addr_evict_blocks_ex, desc, opts, scores, block_table, seq_lens, budget_tokens,
+                                   evicted_logical_out, freed_phys_out)
+    if status is None:
+        status = L.pe_evict_blocks_ex(ctypes.byref(desc), ctypes.byref(opts), _addr_opt(scores, "scores", torch.float32),
+                                      _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                      int(budget_tokens), _addr(evicted_logical_out, "evicted_logical_out", torch.int32),
+                                      _addr(freed_phys_out, "freed_phys_out", torch.int32), _stream())
+    check(status, "pe_evict_blocks_ex")
 
 
 def pe_paged_decode(desc, q, k_pool, v_pool, block_table, seq_lens, softmax_scale, out, workspace=None):
@@ -402,46 +406,68 @@ def pe_append_paged_decode_layers(desc, num_layers, new_k, new_v, q, k_pool, v_p
 def pe_tree_decode(desc, num_drafts, q, k_draft, v_draft, draft_lens, tree_mask, k_pool, v_pool, block_table, seq_lens,
                    softmax_scale, out, workspace=None):
     """tree_mask: int64 (bit j of a word is draft j; bit 63 the sign)."""
-    wp, wn = _ws(workspace)
-    check(lib().pe_tree_decode(ctypes.byref(desc), int(num_drafts), _addr(q, "q"), _addr(k_draft, "k_draft"),
-                               _addr(v_draft, "v_draft"), _addr_opt(draft_lens, "draft_lens", torch.int32),
-                               _addr(tree_mask, "tree_mask", torch.int64), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                               _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                               float(softmax_scale), _addr(out, "out"), wp, wn, _stream()), "pe_tree_decode")
+    L = lib()
+    status = _host.tree_decode(L.addr_tree_decode, desc, num_drafts, q, k_draft, v_draft, draft_lens, tree_mask, k_pool, v_pool,
+                               block_table, seq_lens, softmax_scale, out, workspace)
+    if status is None:
+        wp, wn = _ws(workspace)
+        status = L.pe_tree_decode(ctypes.byref(desc), int(num_drafts), _addr(q, "q"), _addr(k_draft, "k_draft"),
+                                  _addr(v_draft, "v_draft"), _addr_opt(draft_lens, "draft_lens", torch.int32),
+                                  _addr(tree_mask, "tree_mask", torch.int64), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                  _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                  float(softmax_scale), _addr(out, "out"), wp, wn, _stream())
+    check(status, "pe_tree_decode")
 
 
 def pe_append_path(desc, k_draft, v_draft, path, path_lens, path_done, k_pool, v_pool, block_table, seq_lens, freed_phys, spare,
                    spare_used):
-    check(lib().pe_append_path(ctypes.byref(desc), int(k_draft.shape[1]), _addr(k_draft, "k_draft"), _addr(v_draft, "v_draft"),
-                               _addr(path, "path", torch.int32), int(path.shape[-1]),
-                               _addr(path_lens, "path_lens", torch.int32), _addr(path_done, "path_done", torch.int32),
-                               _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                               _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                               _addr(freed_phys, "freed_phys", torch.int32), _addr(spare, "spare", torch.int32),
-                               _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]), _stream()),
-          "pe_append_path")
+    L = lib()
+    status = _host.append_path(L.addr_append_path, desc, k_draft, k_draft, v_draft, path, path, path_lens, path_done, k_pool, v_pool,
+                               block_table, seq_lens, freed_phys, spare, spare_used, spare)
+    if status is None:
+        status = L.pe_append_path(ctypes.byref(desc), int(k_draft.shape[1]), _addr(k_draft, "k_draft"), _addr(v_draft, "v_draft"),
+                                  _addr(path, "path", torch.int32), int(path.shape[-1]),
+                                  _addr(path_lens, "path_lens", torch.int32), _addr(path_done, "path_done", torch.int32),
+                                  _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                  _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                  _addr(freed_phys, "freed_phys", torch.int32), _addr(spare, "spare", torch.int32),
+                                  _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]), _stream())
+    check(status, "pe_append_path")
 
 
 def pe_page_bounds(desc, k_pool, block_table, seq_lens, recent, bounds_inout):
-    check(lib().pe_page_bounds(ctypes.byref(desc), _addr(k_pool, "k_pool"), _addr(block_table, "block_table", torch.int32),
-                               _addr(seq_lens, "seq_lens", torch.int32), int(recent), _addr(bounds_inout, "bounds_inout"), _stream()),
-          "pe_page_bounds")
+    L = lib()
+    status = _host.page_bounds(L.addr_page_bounds, desc, k_pool, block_table, seq_lens, recent, bounds_inout)
+    if status is None:
+        status = L.pe_page_bounds(ctypes.byref(desc), _addr(k_pool, "k_pool"), _addr(block_table, "block_table", torch.int32),
+                                  _addr(seq_lens, "seq_lens", torch.int32), int(recent), _addr(bounds_inout, "bounds_inout"),
+                                  _stream())
+    check(status, "pe_page_bounds")
 
 
 def pe_select_pages(desc, q, bounds, block_table, seq_lens, num_pages, block_table_out, seq_lens_out, page_idx_out, workspace):
-    wp, wn = _ws(workspace)
-    check(lib().pe_select_pages(ctypes.byref(desc), _addr(q, "q"), _addr(bounds, "bounds"),
-                                _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                                int(num_pages), _addr(block_table_out, "block_table_out", torch.int32),
-                                _addr(seq_lens_out, "seq_lens_out", torch.int32),
-                                _addr_opt(page_idx_out, "page_idx_out", torch.int32), wp, wn, _stream()), "pe_select_pages")
+    L = lib()
+    status = _host.select_pages(L.addr_select_pages, desc, q, bounds, block_table, seq_lens, num_pages, block_table_out, seq_lens_out,
+                                page_idx_out, workspace)
+    if status is None:
+        wp, wn = _ws(workspace)
+        status = L.pe_select_pages(ctypes.byref(desc), _addr(q, "q"), _addr(bounds, "bounds"),
+                                   _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                   int(num_pages), _addr(block_table_out, "block_table_out", torch.int32),
+                                   _addr(seq_lens_out, "seq_lens_out", torch.int32),
+                                   _addr_opt(page_idx_out, "page_idx_out", torch.int32), wp, wn, _stream())
+    check(status, "pe_select_pages")
 
 
 def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, softmax_scale, decay, weights_in, weights_out, out,
                             workspace=None):
-    wp, wn = _ws(workspace)
-    check(lib().pe_paged_decode_weights(ctypes.byref(desc), _addr(q, "q"), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                                        _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                                        float(softmax_scale), float(decay), _addr_opt(weights_in, "weights_in", torch.float32),
-                                        _addr(weights_out, "weights_out", torch.float32), _addr(out, "out"), wp, wn, _stream()),
-          "pe_paged_decode_weights")
+    L = lib()
+    status = _host.paged_decode_weights(L.addr_paged_decode_weights, desc, q, k_pool, v_pool, block_table, seq_lens, softmax_scale, decay,
+                                        weights_in, weights_out, out, workspace)
+    if status is None:
+        wp, wn = _ws(workspace)
+        status = L.pe_paged_decode_weights(ctypes.byref(desc), _addr(q, "q"), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                           _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                           float(softmax_scale), float(decay), _addr_opt(weights_in, "weights_in", torch.float32),
+                                           _addr(weights_out, "weights_out", torch.float32), _addr(out, "out"), wp, wn, _stream())
+    check(status, "pe_paged_decode_weights")

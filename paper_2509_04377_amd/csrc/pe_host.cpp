@@ -50,6 +50,24 @@ struct IntsOrNone {
   std::tuple<Address> c;
   bool get(PyObject* o) { return o == Py_None || address_of(o, true, at::kInt, &std::get<0>(c)); }
 };
+struct FloatsOrNone {
+  std::tuple<Address> c;
+  bool get(PyObject* o) { return o == Py_None || address_of(o, true, at::kFloat, &std::get<0>(c)); }
+};
+struct Words {  // 64-bit integers
+  std::tuple<Address> c;
+  bool get(PyObject* o) { return address_of(o, true, at::kLong, &std::get<0>(c)); }
+};
+struct SecondDim {  // the size of a tensor's second dimension
+  std::tuple<int32_t> c;
+  bool get(PyObject* o) {
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.dim() < 2) return false;
+    std::get<0>(c) = (int32_t)t.size(1);
+    return true;
+  }
+};
 struct LastDim {  // the size of a tensor's last dimension
   std::tuple<int32_t> c;
   bool get(PyObject* o) {
@@ -96,24 +114,31 @@ struct Workspace {
   }
 };
 
-// binding.py's ctypes structure (see bind_descriptor); nullptr: not named yet.
-PyTypeObject* descriptor_type = nullptr;
+// binding.py's ctypes structures (see bind_descriptor); nullptr: not named yet.
+PyTypeObject *descriptor_type = nullptr, *evict_opts_type = nullptr;
 
-// The descriptor: an object of that type and of no other, read through the buffer protocol.
+// A structure: an object of that type and of no other, read through the buffer protocol.
+template <typename T>
+bool structure(PyObject* o, PyTypeObject* type, T* to) {
+  if (type == nullptr || Py_TYPE(o) != type) return false;
+  Py_buffer b;
+  if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+    PyErr_Clear();
+    return false;
+  }
+  const bool fits = b.len == (Py_ssize_t)sizeof(T);
+  if (fits) memcpy(to, b.buf, sizeof(T));
+  PyBuffer_Release(&b);
+  return fits;
+}
 struct Desc {
   pe_cache_desc d;
-  bool get(PyObject* o) {
-    if (descriptor_type == nullptr || Py_TYPE(o) != descriptor_type) return false;
-    Py_buffer b;
-    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
-      PyErr_Clear();
-      return false;
-    }
-    const bool fits = b.len == (Py_ssize_t)sizeof(d);
-    if (fits) memcpy(&d, b.buf, sizeof(d));
-    PyBuffer_Release(&b);
-    return fits;
-  }
+  bool get(PyObject* o) { return structure(o, descriptor_type, &d); }
+};
+struct EvictOpts {
+  pe_evict_opts opts;
+  std::tuple<const pe_evict_opts*> c{&opts};
+  bool get(PyObject* o) { return structure(o, evict_opts_type, &opts); }
 };
 
 template <typename... Args, size_t... I>
@@ -176,8 +201,26 @@ PyObject* bind_descriptor(PyObject*, PyObject* type) {
   return layout;
 }
 
+// The same for the eviction's options.
+PyObject* bind_evict_opts(PyObject*, PyObject* type) {
+  if (!PyType_Check(type)) {
+    PyErr_SetString(PyExc_TypeError, "the type of the options");
+    return nullptr;
+  }
+#define PE_FIELD(f) #f, (Py_ssize_t)offsetof(pe_evict_opts, f), (Py_ssize_t)sizeof(pe_evict_opts::f)
+  PyObject* layout = Py_BuildValue("(n(snn)(snn)(snn)(snn)(snn))", (Py_ssize_t)sizeof(pe_evict_opts), PE_FIELD(policy), PE_FIELD(protect_first),
+                                   PE_FIELD(protect_last), PE_FIELD(share_heads), PE_FIELD(cached_scores));
+#undef PE_FIELD
+  if (layout == nullptr) return nullptr;
+  Py_INCREF(type);
+  Py_XDECREF((PyObject*)evict_opts_type);
+  evict_opts_type = reinterpret_cast<PyTypeObject*>(type);
+  return layout;
+}
+
 PyMethodDef methods[] = {
     {"bind_descriptor", bind_descriptor, METH_O, nullptr},
+    {"bind_evict_opts", bind_evict_opts, METH_O, nullptr},
     // q, k_pool, v_pool, block_table, seq_lens, softmax_scale, out, workspace
     method<call<decltype(&pe_paged_decode), Tensor, Tensor, Tensor, Ints, Ints, Float, Tensor, Workspace>>("paged_decode"),
     // new_k, new_v, q, k_pool, v_pool, block_table, seq_lens, seq_lens_out, freed_phys, spare, spare_used, spare, softmax_scale,
@@ -199,6 +242,22 @@ PyMethodDef methods[] = {
     // scores, block_table, seq_lens, budget_tokens, evicted_logical_out, freed_phys_out
     method<call<decltype(&pe_evict_blocks), Floats, Ints, Ints, Number<int32_t>, Ints, Ints>>("evict_blocks"),
     method<call<decltype(&pe_evict_blocks_cached), Floats, Ints, Ints, Number<int32_t>, Ints, Ints>>("evict_blocks_cached"),
+    // opts, scores, block_table, seq_lens, budget_tokens, evicted_logical_out, freed_phys_out
+    method<call<decltype(&pe_evict_blocks_ex), EvictOpts, FloatsOrNone, Ints, Ints, Number<int32_t>, Ints, Ints>>("evict_blocks_ex"),
+    // num_drafts, q, k_draft, v_draft, draft_lens, tree_mask, k_pool, v_pool, block_table, seq_lens, softmax_scale, out, workspace
+    method<call<decltype(&pe_tree_decode), Number<int32_t>, Tensor, Tensor, Tensor, IntsOrNone, Words, Tensor, Tensor, Ints, Ints, Float,
+                Tensor, Workspace>>("tree_decode"),
+    // k_draft, k_draft, v_draft, path, path, path_lens, path_done, k_pool, v_pool, block_table, seq_lens, freed_phys, spare,
+    // spare_used, spare
+    method<call<decltype(&pe_append_path), SecondDim, Tensor, Tensor, Ints, LastDim, Ints, Ints, Tensor, Tensor, Ints, Ints, Ints, Ints, Ints,
+                LastDim>>("append_path"),
+    // q, k_pool, v_pool, block_table, seq_lens, softmax_scale, decay, weights_in, weights_out, out, workspace
+    method<call<decltype(&pe_paged_decode_weights), Tensor, Tensor, Tensor, Ints, Ints, Float, Float, FloatsOrNone, Floats, Tensor,
+                Workspace>>("paged_decode_weights"),
+    // k_pool, block_table, seq_lens, recent, bounds_inout
+    method<call<decltype(&pe_page_bounds), Tensor, Ints, Ints, Number<int32_t>, Tensor>>("page_bounds"),
+    // q, bounds, block_table, seq_lens, num_pages, block_table_out, seq_lens_out, page_idx_out, workspace
+    method<call<decltype(&pe_select_pages), Tensor, Tensor, Ints, Ints, Number<int32_t>, Ints, Ints, IntsOrNone, Workspace>>("select_pages"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pe_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
