@@ -17,295 +17,439 @@ namespace {
 constexpr int kWaves = 4;
 
 // ---- bounds --------------------------------------------------------------------------------------------------------------
-// One wave a page and head.  A lane's 16 bytes of every TPL-th token, the smallest and largest over its tokens, then over the lanes
-// that hold the same elements.
+// A lane has 16 bytes of every token of one page (head-shared: of one head too), so nothing is exchanged between lanes, and the lanes of
+// a wave read whole token rows.  Sixteen loads are in flight.
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) { return (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xffff0000u); }
+
 template <typename T>
-__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
-  return (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xffff0000u);
-}
-
-template <int FROM, int N>
-__device__ __forceinline__ void bounds_over_lanes(float (&lo)[N], float (&hi)[N]) {
-  if constexpr (FROM < kWave) {
+__global__ __launch_bounds__(kWaves * kWave) void page_bounds_kernel(const uint4* k_pool, const int32_t* block_table, const int32_t* seq_lens,
+                                                                     uint4* bounds, int chunks, int rows_per_seq, int log2_block, int max_blocks,
+                                                                     int per_row, int groups, int recent, int64_t first_row) {
+  constexpr int EPL = Elem<T>::kPerVec;
+  const uint32_t in = blockIdx.x / (uint32_t)groups;
+  const int64_t row = first_row + in;  // of the table
+  const uint32_t unit = (blockIdx.x - in * (uint32_t)groups) * (kWaves * kWave) + threadIdx.x;  // (page, chunk of its token rows)
+  int j = (int)(unit / (uint32_t)chunks);
+  const int c = (int)(unit - (uint32_t)j * (uint32_t)chunks);
+  const int len = seq_lens[(uint32_t)row / (uint32_t)rows_per_seq];
+  int full = len > 0 ? len >> log2_block : 0;
+  full = full < max_blocks ? full : max_blocks;
+  if (j >= per_row) return;
+  if (recent) j += full - per_row;
+  if (j < 0 || j >= full) return;
+  const int page = block_table[row * max_blocks + j];
+  if (page < 0) return;
+  const uint4* from = k_pool + (((int64_t)page << log2_block) * chunks + c);
+  float lo[EPL], hi[EPL];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      lo[e] = fminf(lo[e], lane_xor_f32<FROM>(lo[e]));
-      hi[e] = fmaxf(hi[e], lane_xor_f32<FROM>(hi[e]));
-    }
-    bounds_over_lanes<FROM * 2>(lo, hi);
+  for (int e = 0; e < EPL; ++e) {
+    lo[e] = __builtin_inff();
+    hi[e] = -__builtin_inff();
   }
-}
-
-template <typename T, int D>
-__global__ __launch_bounds__(kWaves * kWave) void page_bounds_kernel(const void* k_pool, const int32_t* block_table, const int32_t* seq_lens,
-                                                                     void* bounds, int recent, int num_kv_heads, int log2_block, int max_blocks,
-                                                                     int shared, int64_t items, int per_row) {
-  using Geo = RowGeom<T, D>;
-  constexpr int EPL = Geo::kPerVec, LPR = Geo::kLanesPerRow, TPL = Geo::kTokensPerLoad;
-  const int lane = lane_id(), u = lane % LPR, grp = lane / LPR;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-  for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
-    const int64_t row = item / per_row;  // (sequence, KV head)
-    int j = (int)(item - row * per_row);
-    const int s = (int)(row / num_kv_heads), hk = (int)(row - (int64_t)s * num_kv_heads);
-    const int len = seq_lens[s];
-    int full = len > 0 ? len >> log2_block : 0;
-    full = full < max_blocks ? full : max_blocks;
-    if (recent > 0) j += full - per_row;
-    if (j < 0 || j >= full) continue;
-    const int page = block_table[(shared ? s : row) * max_blocks + j];
-    if (page < 0) continue;
-    const int heads = shared ? num_kv_heads : 1;
-    const int64_t first = ((int64_t)page << log2_block) * heads * LPR + (shared ? hk * LPR : 0);
-    float lo[EPL], hi[EPL];
+  for (int t = 0; t < 1 << log2_block; t += 16) {
+    uint4 k[16];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-      lo[e] = __builtin_inff();
-      hi[e] = -__builtin_inff();
-    }
-    for (int t = 0; t < 1 << log2_block; t += 16) {
-      uint4 k[16 / TPL];
+    for (int i = 0; i < 16; ++i) k[i] = load_vec_stream(from, (int64_t)(t + i) * chunks);
 #pragma unroll
-      for (int i = 0; i < 16 / TPL; ++i) k[i] = load_vec_stream(k_pool, first + (int64_t)(t + i * TPL + grp) * heads * LPR + u);
+    for (int i = 0; i < 16; ++i)
 #pragma unroll
-      for (int i = 0; i < 16 / TPL; ++i)
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-          const float x = vec_elem<T>(k[i], e);
-          lo[e] = fminf(lo[e], x);
-          hi[e] = fmaxf(hi[e], x);
-        }
-    }
-    bounds_over_lanes<LPR>(lo, hi);
-    if (grp < 2) {
-      const float(&v)[EPL] = grp == 0 ? lo : hi;
-      uint4 w;
-      if constexpr (sizeof(T) == 4)
-        w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-      else
-        w = make_uint4(pack_pair<T>(v[0], v[1]), pack_pair<T>(v[2], v[3]), pack_pair<T>(v[4], v[5]), pack_pair<T>(v[6], v[7]));
-      static_cast<uint4*>(bounds)[((int64_t)page * 2 + grp) * heads * LPR + (shared ? hk * LPR : 0) + u] = w;
-    }
+      for (int e = 0; e < EPL; ++e) {
+        const float x = vec_elem<T>(k[i], e);
+        lo[e] = fminf(lo[e], x);
+        hi[e] = fmaxf(hi[e], x);
+      }
+  }
+  uint4* to = bounds + ((int64_t)page * 2 * chunks + c);
+  if constexpr (sizeof(T) == 4) {
+    to[0] = make_uint4(__float_as_uint(lo[0]), __float_as_uint(lo[1]), __float_as_uint(lo[2]), __float_as_uint(lo[3]));
+    to[chunks] = make_uint4(__float_as_uint(hi[0]), __float_as_uint(hi[1]), __float_as_uint(hi[2]), __float_as_uint(hi[3]));
+  } else {
+    to[0] = make_uint4(pack_pair(lo[0], lo[1]), pack_pair(lo[2], lo[3]), pack_pair(lo[4], lo[5]), pack_pair(lo[6], lo[7]));
+    to[chunks] = make_uint4(pack_pair(hi[0], hi[1]), pack_pair(hi[2], hi[3]), pack_pair(hi[4], hi[5]), pack_pair(hi[6], hi[7]));
   }
 }
 
 // ---- scores --------------------------------------------------------------------------------------------------------------
-// A wave scores 16 * 64 / LPB pages: the 2 D bounds of a page and head are LPB lanes' 16 bytes, lo in the lower half of them and hi in
-// the upper.  Sixteen loads are in flight; their sums meet in a reduce-scatter.  Head-shared rows add their heads up before it.
+// A wave scores 16 * 64 / LPB pages at a time: the 2 D bounds of a page and head are LPB lanes' 16 bytes, lo in the lower half of them and hi
+// in the upper.  Sixteen loads are in flight; their sums meet in a reduce-scatter.
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const void* q, const void* bounds, const int32_t* block_table,
-                                                                     const int32_t* seq_lens, float* scores, int num_kv_heads, int group,
-                                                                     int log2_block, int max_blocks, int shared, int pages, int parts,
-                                                                     int64_t first_row) {
-  constexpr int EPL = Elem<T>::kPerVec, LPB = 2 * D / EPL, PPL = kWave / LPB, NL = 16, kPages = NL * PPL;
-  const int lane = lane_id(), u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-  const int64_t row = first_row + blockIdx.x / (uint32_t)parts;  // of the table
-  const int part = (int)(blockIdx.x % (uint32_t)parts);
-  const int s = (int)(shared ? row : row / num_kv_heads);
-  int len = seq_lens[s];
-  const int all = len > 0 ? (int)(((int64_t)len + (1 << log2_block) - 1) >> log2_block) : 0;
-  const int n = (all < max_blocks ? all : max_blocks) - 1;  // candidates: all but the newest page
-  const int base = (part * kWaves + wave) * kPages;
-  if (n < pages || base >= n) return;  // (with n + 1 <= pages every page is taken)
-  const int32_t* bt = block_table + row * max_blocks;
-  const int heads = shared ? num_kv_heads : 1, head0 = shared ? 0 : (int)(row - (int64_t)s * num_kv_heads);
-  int64_t at[NL];
+struct Scorer {
+  static constexpr int EPL = Elem<T>::kPerVec, LPB = 2 * D / EPL, PPL = kWave / LPB, NL = 16, kPages = NL * PPL;
+
+  // The page (behind `base`) whose score the lane is left with, if it is left with one.
+  static __device__ __forceinline__ int page_of(int lane) { return bit_reverse<4>(lane & 15) * PPL + lane / LPB; }
+  static __device__ __forceinline__ bool has_page(int lane) { return lane % LPB < NL; }
+
+  // Scores of pages base .. base + kPages - 1 (of n), over the heads head, head + step, ... of the row's `heads` (first of them: q_head).
+  static __device__ __forceinline__ double score(const uint4* q, const uint4* bounds, const int32_t* bt, int64_t q_head, int group, int heads,
+                                                 int head, int step, int base, int n, int lane) {
+    const int u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
+    int64_t at[NL];
 #pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int j = base + i * PPL + lane / LPB;
-    const int page = bt[j < n ? j : n - 1];
-    at[i] = ((int64_t)(page < 0 ? 0 : page) * 2 + up) * heads * (LPB / 2) + v;
-  }
-  double sum[NL];
-#pragma unroll
-  for (int i = 0; i < NL; ++i) sum[i] = 0.0;
-  for (int h = 0; h < heads; ++h) {
-    uint4 b[NL];
-#pragma unroll
-    for (int i = 0; i < NL; ++i) b[i] = load_vec(bounds, at[i] + h * (LPB / 2));
-    double w[EPL];
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) w[e] = 0.0;
-    const uint4* from = static_cast<const uint4*>(q) + ((int64_t)s * num_kv_heads + head0 + h) * group * (LPB / 2) + v;
-    for (int x = 0; x < group; ++x) {
-      const uint4 qv = from[x * (LPB / 2)];
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        const float f = vec_elem<T>(qv, e);
-        w[e] += (double)(up ? fmaxf(f, 0.f) : fminf(f, 0.f));
-      }
+    for (int i = 0; i < NL; ++i) {
+      const int j = base + i * PPL + lane / LPB;
+      const int page = bt[j < n ? j : n - 1];
+      at[i] = ((int64_t)(page < 0 ? 0 : page) * 2 + up) * heads * (LPB / 2) + v;
     }
+    double sum[NL];
 #pragma unroll
-    for (int i = 0; i < NL; ++i)
+    for (int i = 0; i < NL; ++i) sum[i] = 0.0;
+    for (int h = head; h < heads; h += step) {
+      uint4 b[NL];
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) sum[i] = fma((double)vec_elem<T>(b[i], e), w[e], sum[i]);
+      for (int i = 0; i < NL; ++i) b[i] = load_vec(bounds, at[i] + h * (LPB / 2));
+      double w[EPL];
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) w[e] = 0.0;
+      const uint4* from = q + (q_head + h) * group * (LPB / 2) + v;
+      for (int x = 0; x < group; ++x) {
+        const uint4 qv = from[x * (LPB / 2)];
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) {
+          const float f = vec_elem<T>(qv, e);
+          w[e] += (double)(up ? fmaxf(f, 0.f) : fminf(f, 0.f));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) sum[i] = fma((double)vec_elem<T>(b[i], e), w[e], sum[i]);
+    }
+    return all_reduce_f64<NL, LPB>(reduce_scatter_f64<NL>(sum, lane));
   }
-  double total = reduce_scatter_f64<NL>(sum, lane);  // of load bit_reverse(lane & 15)
-  total = all_reduce_f64<NL, LPB>(total);
-  const int j = base + bit_reverse<4>(lane & 15) * PPL + lane / LPB;
-  if (u < NL && j < n) scores[row * max_blocks + j] = (float)total;
+};
+
+struct Row {  // of the table
+  int64_t row;
+  int s, len, all;  // its sequence, tokens, pages
+};
+__device__ __forceinline__ Row row_at(int64_t row, const int32_t* seq_lens, int rows_per_seq, int log2_block, int max_blocks) {
+  Row r;
+  r.row = row;
+  r.s = (int)((uint32_t)row / (uint32_t)rows_per_seq);
+  const int64_t most = (int64_t)max_blocks << log2_block;
+  const int len = seq_lens[r.s];
+  r.len = len < 0 ? 0 : len < most ? len : (int)most;
+  r.all = (int)(((int64_t)r.len + (1 << log2_block) - 1) >> log2_block);
+  return r;
+}
+
+// Scores of a row's pages but the newest, for a launch behind this one.  A workgroup has its four waves' pages, or with several heads a
+// decision those of one wave, of which each wave takes every fourth head.
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4* q, const uint4* bounds, const int32_t* block_table,
+                                                                     const int32_t* seq_lens, float* scores, int rows_per_seq, int heads, int group,
+                                                                     int log2_block, int max_blocks, int pages, int parts, int64_t first_row) {
+  using SC = Scorer<T, D>;
+  __shared__ double of_heads[kWaves][kWave];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const uint32_t in = blockIdx.x / (uint32_t)parts;
+  const int part = (int)(blockIdx.x - in * (uint32_t)parts);
+  const Row r = row_at(first_row + in, seq_lens, rows_per_seq, log2_block, max_blocks);
+  const int n = r.all - 1;  // candidates
+  const int base = (heads > 1 ? part : part * kWaves + wave) * SC::kPages;
+  if (n < pages || base >= n) return;  // (with n + 1 <= pages every page is taken; several heads: the same in all waves)
+  const int32_t* bt = block_table + r.row * max_blocks;
+  const int j = base + SC::page_of(lane);
+  float* to = scores + r.row * max_blocks + j;
+  const bool mine = SC::has_page(lane) && j < n;
+  if (heads == 1) {
+    const double total = SC::score(q, bounds, bt, r.row, group, 1, 0, 1, base, n, lane);
+    if (mine) *to = (float)total;
+    return;
+  }
+  of_heads[wave][lane] = SC::score(q, bounds, bt, r.row * heads, group, heads, wave, kWaves, base, n, lane);
+  __syncthreads();
+  if (wave != 0 || !mine) return;
+  double total = of_heads[0][lane];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) total += of_heads[w][lane];
+  *to = (float)total;
 }
 
 // ---- selection -----------------------------------------------------------------------------------------------------------
-// One workgroup a row.  Scores as whole numbers in the same order; the smallest one that is taken is found two bits at a time, by
-// counting those that reach each of three thresholds; what reaches it is taken, of equal ones the first.
-constexpr int kThreads = 1024, kSelectWaves = kThreads / kWave, kHeld = 8;
+// One workgroup a row.  Scores as whole numbers in the same order; the smallest one that is taken lies in one of 1024 equal parts of their
+// range, and there in one of 1024 parts of that, and so on: a count of each part in LDS, then the part in which the sum from above
+// reaches what is needed.  (Scores of about the same size differ in their low bits alone: parts of their range hold about as many each,
+// digits of the numbers would not.)  A wave holds consecutive pages, so that one exchange tells where its first one goes.
+constexpr int kParts = 1024, kHeld = 8;
 
 __device__ __forceinline__ uint32_t order_of(float f) {
   const uint32_t b = __float_as_uint(f + 0.f);  // (-0 is 0)
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-
-__global__ __launch_bounds__(kThreads) void select_pages_kernel(const float* scores, const int32_t* block_table, const int32_t* seq_lens,
-                                                                int32_t* table_out, int32_t* lens_out, int32_t* idx_out, int num_kv_heads,
-                                                                int log2_block, int max_blocks, int shared, int pages, int64_t first_row) {
-  __shared__ uint32_t counts[16][4];
-  __shared__ uint32_t above[2][kSelectWaves], equal[2][kSelectWaves];
-  const int64_t row = first_row + blockIdx.x;
-  const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int s = (int)(shared ? row : row / num_kv_heads);
-  const int64_t most = (int64_t)max_blocks << log2_block;
-  int len = seq_lens[s];
-  len = len < 0 ? 0 : len < most ? len : (int)most;
-  const int all = (int)(((int64_t)len + (1 << log2_block) - 1) >> log2_block);
-  const int taken = all < pages ? all : pages;
-  const int32_t* bt = block_table + row * max_blocks;
-  int32_t* to = table_out + row * pages;
-  int32_t* idx = idx_out != nullptr ? idx_out + row * pages : nullptr;
-  for (int i = taken + tid; i < pages; i += kThreads) {
-    to[i] = -1;
-    if (idx != nullptr) idx[i] = -1;
-  }
-  if (tid == 0 && (shared || row == (int64_t)s * num_kv_heads)) lens_out[s] = len - ((all - taken) << log2_block);
-  if (all <= pages) {
-    for (int i = tid; i < all; i += kThreads) {
-      to[i] = bt[i];
-      if (idx != nullptr) idx[i] = i;
-    }
-    return;
-  }
-  const int n = all - 1, need = pages - 1;  // need < n
-  if (tid == 0) {
-    to[need] = bt[n];
-    if (idx != nullptr) idx[need] = n;
-  }
-  if (need == 0) return;
-  const float* sc = scores + row * max_blocks;
-  const int rounds = (n + kThreads - 1) / kThreads;
-  uint32_t held[kHeld];
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + tid < n ? order_of(sc[i * kThreads + tid]) : 0u;
-  if (tid < 64) counts[tid / 4][tid % 4] = 0u;
-  __syncthreads();
-  uint32_t least = 0u;
-  for (int bit = 30, at = 0; bit >= 0; bit -= 2, ++at) {
-    uint32_t c[3] = {0u, 0u, 0u};
-    const auto count = [&](uint32_t key) {
-#pragma unroll
-      for (int t = 0; t < 3; ++t) c[t] += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= least + ((uint32_t)(t + 1) << bit)));
-    };
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (i < rounds) count(held[i]);
-    for (int i = kHeld; i < rounds; ++i) {
-      const int j = i * kThreads + tid;
-      count(j < n ? order_of(sc[j]) : 0u);
-    }
-    if (lane < 3) atomicAdd(&counts[at][lane], lane == 0 ? c[0] : lane == 1 ? c[1] : c[2]);
-    __syncthreads();
-    uint32_t step = 0u;
-#pragma unroll
-    for (int t = 0; t < 3; ++t)
-      if (counts[at][t] >= (uint32_t)need) step = (uint32_t)(t + 1) << bit;
-    least += step;
-  }
-  // what lies above is counted again, to know how many of the equal ones go
-  __shared__ uint32_t over;
-  if (tid == 0) over = 0u;
-  __syncthreads();
-  uint32_t c = 0u;
-  for (int i = 0; i < rounds; ++i) {
-    const int j = i * kThreads + tid;
-    c += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(j < n && order_of(sc[j]) > least));
-  }
-  if (lane == 0) atomicAdd(&over, c);
-  __syncthreads();
-  const int ties = need - (int)over;  // the first of the equal ones
-  int at_above = 0, at_equal = 0;
-  const uint64_t below = (1ull << lane) - 1;
-  for (int i = 0; i < rounds; ++i) {
-    const int j = i * kThreads + tid;
-    const uint32_t key = j < n ? order_of(sc[j]) : 0u;
-    const uint64_t gt = __builtin_amdgcn_ballot_w64(j < n && key > least), eq = __builtin_amdgcn_ballot_w64(j < n && key == least);
-    if (lane == 0) {
-      above[i & 1][wave] = (uint32_t)__builtin_popcountll(gt);
-      equal[i & 1][wave] = (uint32_t)__builtin_popcountll(eq);
-    }
-    __syncthreads();
-    int my_above = at_above, my_equal = at_equal;
-    for (int w = 0; w < kSelectWaves; ++w) {
-      const int a = (int)above[i & 1][w], e = (int)equal[i & 1][w];
-      if (w < wave) {
-        my_above += a;
-        my_equal += e;
-      }
-      at_above += a;
-      at_equal += e;
-    }
-    my_above += (int)__builtin_popcountll(gt & below);
-    my_equal += (int)__builtin_popcountll(eq & below);
-    const bool is_gt = (gt >> lane & 1u) != 0, is_eq = (eq >> lane & 1u) != 0 && my_equal < ties;
-    if (is_gt || is_eq) {
-      const int pos = my_above + (my_equal < ties ? my_equal : ties);
-      to[pos] = bt[j];
-      if (idx != nullptr) idx[pos] = j;
-    }
+template <int M = 1>
+__device__ __forceinline__ void least_and_most(uint32_t& lo, uint32_t& hi) {
+  if constexpr (M < kWave) {
+    const uint32_t a = (uint32_t)lane_xor_i32<M>((int)lo), b = (uint32_t)lane_xor_i32<M>((int)hi);
+    lo = a < lo ? a : lo;
+    hi = b > hi ? b : hi;
+    least_and_most<M * 2>(lo, hi);
   }
 }
 
-template <typename T, int D>
+template <int WAVES>
+struct SelectState {
+  alignas(16) uint32_t count[2][kParts];
+  uint32_t lo[WAVES], hi[WAVES];
+  int above[WAVES], equal[WAVES];
+};
+
+// Of n scores the `need` < n highest (of equal ones the first), in their order: table entries and indices.
+template <int WAVES>
+__device__ __forceinline__ void select_row(const float* sc, int n, int need, const int32_t* bt, int32_t* to, int32_t* idx, SelectState<WAVES>& sm) {
+  const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int each = (n + WAVES * kWave - 1) / (WAVES * kWave), first = wave * each * kWave + lane;  // of `each` times 64
+  uint32_t held[kHeld];
+  int32_t page[kHeld];
+  uint32_t lo = ~0u, hi = 0u;
+  const auto at = [&](int i) { return first + i * kWave; };
+  const auto key = [&](int i) { return at(i) < n ? order_of(sc[at(i)]) : 0u; };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const bool in = i < each && at(i) < n;
+    page[i] = in ? bt[at(i)] : -1;
+    held[i] = in ? order_of(sc[at(i)]) : 0u;
+    lo = in && held[i] < lo ? held[i] : lo;
+    hi = in && held[i] > hi ? held[i] : hi;
+  }
+  for (int i = kHeld; i < each; ++i)
+    if (at(i) < n) {
+      const uint32_t k = key(i);
+      lo = k < lo ? k : lo;
+      hi = k > hi ? k : hi;
+    }
+  least_and_most(lo, hi);
+  if (lane == 0) {
+    sm.lo[wave] = lo;
+    sm.hi[wave] = hi;
+  }
+  for (int i = tid; i < 2 * kParts; i += WAVES * kWave) sm.count[0][i] = 0u;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    lo = sm.lo[w] < lo ? sm.lo[w] : lo;
+    hi = sm.hi[w] > hi ? sm.hi[w] : hi;
+  }
+  // Keys above `least` go, and `ties` of those that are equal to it.
+  uint32_t least = lo;
+  int ties = need;
+  for (int turn = 0; hi != lo; ++turn) {
+    uint32_t* count = sm.count[turn & 1];
+    const uint32_t range = hi - lo;
+    const int bits = 32 - __builtin_clz(range), shift = bits > 10 ? bits - 10 : 0;
+    const auto add = [&](uint32_t k) {
+      if (k - lo <= range) atomicAdd(&count[(k - lo) >> shift], 1u);
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (i < each && at(i) < n) add(held[i]);
+    for (int i = kHeld; i < each; ++i)
+      if (at(i) < n) add(key(i));
+    __syncthreads();
+    // lane l has the parts from 1023 - 16 l down; every wave finds the same one
+    uint32_t part[16], sum = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 c = *reinterpret_cast<const uint4*>(&count[kParts - 16 * (lane + 1) + 4 * i]);
+      part[4 * i] = c.x, part[4 * i + 1] = c.y, part[4 * i + 2] = c.z, part[4 * i + 3] = c.w;
+      sum += (c.x + c.y) + (c.z + c.w);
+    }
+    const uint32_t upto = wave_prefix_sum_u32(sum);
+    const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto >= (uint32_t)ties));  // (all of the range are `ties` at least)
+    uint32_t over = upto - sum, found = 0u, inside = 0u;
+    bool open = true;
+#pragma unroll
+    for (int i = 15; i >= 0; --i) {
+      const bool here = open && over + part[i] >= (uint32_t)ties;
+      if (here) {
+        found = (uint32_t)(kParts - 16 * (lane + 1) + i);
+        inside = part[i];
+        open = false;
+      }
+      if (open) over += part[i];
+    }
+    found = (uint32_t)__builtin_amdgcn_readlane((int)found, owner);
+    inside = (uint32_t)__builtin_amdgcn_readlane((int)inside, owner);
+    ties -= __builtin_amdgcn_readlane((int)over, owner);
+    lo += found << shift;
+    least = lo;
+    if (inside == (uint32_t)ties) {  // all of it go: it is no lowest part (need < n), so there is a number below
+      least = lo - 1u;
+      ties = 0;
+      break;
+    }
+    if (shift == 0) break;
+    hi = lo + ((1u << shift) - 1u);
+    for (int i = tid; i < kParts; i += WAVES * kWave) sm.count[(turn & 1) ^ 1][i] = 0u;
+    __syncthreads();
+  }
+  int above = 0, equal = 0;
+  const auto both = [&](int i, uint32_t k) {
+    above += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(at(i) < n && k > least));
+    equal += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(at(i) < n && k == least));
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (i < each) both(i, held[i]);
+  for (int i = kHeld; i < each; ++i) both(i, key(i));
+  if (lane == 0) {
+    sm.above[wave] = above;
+    sm.equal[wave] = equal;
+  }
+  __syncthreads();
+  above = equal = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w)
+    if (w < wave) {
+      above += sm.above[w];
+      equal += sm.equal[w];
+    }
+  const uint64_t below = (1ull << lane) - 1;
+  const auto put = [&](int i, uint32_t k, int32_t entry) {
+    const uint64_t gt = __builtin_amdgcn_ballot_w64(at(i) < n && k > least), eq = __builtin_amdgcn_ballot_w64(at(i) < n && k == least);
+    const int before = equal + (int)__builtin_popcountll(eq & below);
+    if ((gt >> lane & 1u) != 0 || ((eq >> lane & 1u) != 0 && before < ties)) {
+      const int pos = above + (int)__builtin_popcountll(gt & below) + (before < ties ? before : ties);
+      to[pos] = entry;
+      if (idx != nullptr) idx[pos] = at(i);
+    }
+    above += (int)__builtin_popcountll(gt);
+    equal += (int)__builtin_popcountll(eq);
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (i < each) put(i, held[i], page[i]);
+  for (int i = kHeld; i < each; ++i) put(i, key(i), at(i) < n ? bt[at(i)] : -1);
+}
+
+// What of a row's outputs does not depend on scores; true if that is everything.
+template <int WAVES>
+__device__ __forceinline__ bool frame_row(const Row& r, const int32_t* bt, int32_t* to, int32_t* idx, int32_t* lens_out, bool first_head,
+                                          int log2_block, int pages) {
+  const int tid = (int)threadIdx.x, taken = r.all < pages ? r.all : pages;
+  for (int i = taken + tid; i < pages; i += WAVES * kWave) {
+    to[i] = -1;
+    if (idx != nullptr) idx[i] = -1;
+  }
+  if (tid == 0 && first_head) lens_out[r.s] = r.len - ((r.all - taken) << log2_block);
+  if (r.all <= pages) {
+    for (int i = tid; i < r.all; i += WAVES * kWave) {
+      to[i] = bt[i];
+      if (idx != nullptr) idx[i] = i;
+    }
+    return true;
+  }
+  if (tid == 0) {  // the newest
+    to[pages - 1] = bt[r.all - 1];
+    if (idx != nullptr) idx[pages - 1] = r.all - 1;
+  }
+  return pages == 1;
+}
+
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void select_pages_kernel(const float* scores, const int32_t* block_table, const int32_t* seq_lens,
+                                                                     int32_t* table_out, int32_t* lens_out, int32_t* idx_out, int rows_per_seq,
+                                                                     int log2_block, int max_blocks, int pages, int64_t first_row) {
+  __shared__ SelectState<WAVES> sm;
+  const Row r = row_at(first_row + blockIdx.x, seq_lens, rows_per_seq, log2_block, max_blocks);
+  const int32_t* bt = block_table + r.row * max_blocks;
+  int32_t *to = table_out + r.row * pages, *idx = idx_out != nullptr ? idx_out + r.row * pages : nullptr;
+  if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
+  select_row<WAVES>(scores + r.row * max_blocks, r.all - 1, pages - 1, bt, to, idx, sm);
+}
+
+// Scores and selection in one launch, for rows that one workgroup reads soon enough.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4* q, const uint4* bounds, const int32_t* block_table,
+                                                                     const int32_t* seq_lens, int32_t* table_out, int32_t* lens_out,
+                                                                     int32_t* idx_out, int rows_per_seq, int heads, int group, int log2_block,
+                                                                     int max_blocks, int pages, int64_t first_row) {
+  using SC = Scorer<T, D>;
+  __shared__ SelectState<WAVES> sm;
+  extern __shared__ float sc[];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const Row r = row_at(first_row + blockIdx.x, seq_lens, rows_per_seq, log2_block, max_blocks);
+  const int32_t* bt = block_table + r.row * max_blocks;
+  int32_t *to = table_out + r.row * pages, *idx = idx_out != nullptr ? idx_out + r.row * pages : nullptr;
+  if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
+  const int n = r.all - 1;
+  for (int base = wave * SC::kPages; base < n; base += WAVES * SC::kPages) {
+    const double total = SC::score(q, bounds, bt, r.row * heads, group, heads, 0, 1, base, n, lane);
+    const int j = base + SC::page_of(lane);
+    if (SC::has_page(lane) && j < n) sc[j] = (float)total;
+  }
+  __syncthreads();
+  select_row<WAVES>(sc, n, pages - 1, bt, to, idx, sm);
+}
+
+template <typename T>
 hipError_t launch_bounds_as(const BoundsArgs& a, hipStream_t stream) {
   int log2_block = 0;
   while ((1 << log2_block) < a.block_size) ++log2_block;
+  const int rows_per_seq = a.shared ? 1 : a.num_kv_heads;
+  const int chunks = a.head_dim * (int)sizeof(T) / 16 * (a.shared ? a.num_kv_heads : 1);
   const int per_row = a.recent > 0 && a.recent < a.max_blocks ? a.recent : a.max_blocks;
-  const int64_t items = (int64_t)a.num_seqs * a.num_kv_heads * per_row;
-  const int64_t groups = (items + kWaves - 1) / kWaves;
-  hipLaunchKernelGGL((page_bounds_kernel<T, D>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(kWaves * kWave), 0, stream, a.k_pool,
-                     a.block_table, a.seq_lens, a.bounds, a.recent > 0 ? per_row : 0, a.num_kv_heads, log2_block, a.max_blocks, a.shared ? 1 : 0,
-                     items, per_row);
+  const int64_t units = (int64_t)per_row * chunks, rows = (int64_t)a.num_seqs * rows_per_seq;
+  const int64_t groups = (units + kWaves * kWave - 1) / (kWaves * kWave);
+  const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / groups;  // rows of a launch (of fewer than 2^32 threads)
+  if (some < 1) return hipErrorInvalidValue;
+  for (int64_t row = 0; row < rows; row += some) {
+    const int64_t now = rows - row < some ? rows - row : some;
+    hipLaunchKernelGGL((page_bounds_kernel<T>), dim3((unsigned)(now * groups)), dim3(kWaves * kWave), 0, stream, (const uint4*)a.k_pool,
+                       a.block_table, a.seq_lens, (uint4*)a.bounds, chunks, rows_per_seq, log2_block, a.max_blocks, per_row, (int)groups,
+                       a.recent > 0 ? 1 : 0, row);
+  }
   return hipGetLastError();
+}
+
+template <int WAVES>
+void launch_select_of(const SelectArgs& a, int rows_per_seq, int log2_block, int64_t rows, hipStream_t stream) {
+  constexpr int64_t kRows = 1 << 21;  // of a launch (of fewer than 2^32 threads)
+  for (int64_t row = 0; row < rows; row += kRows)
+    hipLaunchKernelGGL((select_pages_kernel<WAVES>), dim3((unsigned)(rows - row < kRows ? rows - row : kRows)), dim3(WAVES * kWave), 0, stream,
+                       a.scores, a.block_table, a.seq_lens, a.table_out, a.lens_out, a.idx_out, rows_per_seq, log2_block, a.max_blocks, a.pages,
+                       row);
 }
 
 template <typename T, int D>
 hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
-  constexpr int kPages = kWaves * 16 * kWave / (2 * D / Elem<T>::kPerVec);  // of a workgroup
   int log2_block = 0;
   while ((1 << log2_block) < a.block_size) ++log2_block;
-  const int64_t rows = a.shared ? a.num_seqs : (int64_t)a.num_seqs * a.num_kv_heads;
-  const int group = a.num_q_heads / a.num_kv_heads, parts = (a.max_blocks + kPages - 1) / kPages;
+  const int rows_per_seq = a.shared ? 1 : a.num_kv_heads, heads = a.shared ? a.num_kv_heads : 1;
+  const int64_t rows = (int64_t)a.num_seqs * rows_per_seq;
+  const int group = a.num_q_heads / a.num_kv_heads;
+  constexpr int64_t kRows = 1 << 21;
+  if ((int64_t)a.max_blocks * heads * 2 * D * (int64_t)sizeof(T) <= select_one_launch_bytes()) {
+    for (int64_t row = 0; row < rows; row += kRows)
+      hipLaunchKernelGGL((score_select_kernel<T, D, 8>), dim3((unsigned)(rows - row < kRows ? rows - row : kRows)), dim3(8 * kWave),
+                         (size_t)a.max_blocks * sizeof(float), stream, (const uint4*)a.q, (const uint4*)a.bounds, a.block_table, a.seq_lens,
+                         a.table_out, a.lens_out, a.idx_out, rows_per_seq, heads, group, log2_block, a.max_blocks, a.pages, row);
+    return hipGetLastError();
+  }
+  constexpr int kPages = Scorer<T, D>::kPages;
+  const int64_t each = heads > 1 ? kPages : kPages * kWaves, parts = (a.max_blocks + each - 1) / each;
   if (a.max_blocks > a.pages && a.pages > 1) {
-    const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / parts;  // rows of a launch (of fewer than 2^32 threads)
+    const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / parts;
     if (some < 1) return hipErrorInvalidValue;
     for (int64_t row = 0; row < rows; row += some) {
       const int64_t now = rows - row < some ? rows - row : some;
-      hipLaunchKernelGGL((score_pages_kernel<T, D>), dim3((unsigned)(now * parts)), dim3(kWaves * kWave), 0, stream, a.q, a.bounds, a.block_table,
-                         a.seq_lens, a.scores, a.num_kv_heads, group, log2_block, a.max_blocks, a.shared ? 1 : 0, a.pages, parts, row);
+      hipLaunchKernelGGL((score_pages_kernel<T, D>), dim3((unsigned)(now * parts)), dim3(kWaves * kWave), 0, stream, (const uint4*)a.q,
+                         (const uint4*)a.bounds, a.block_table, a.seq_lens, a.scores, rows_per_seq, heads, group, log2_block, a.max_blocks,
+                         a.pages, (int)parts, row);
     }
   }
-  constexpr int64_t kRows = 1 << 21;
-  for (int64_t row = 0; row < rows; row += kRows)
-    hipLaunchKernelGGL(select_pages_kernel, dim3((unsigned)(rows - row < kRows ? rows - row : kRows)), dim3(kThreads), 0, stream, a.scores,
-                       a.block_table, a.seq_lens, a.table_out, a.lens_out, a.idx_out, a.num_kv_heads, log2_block, a.max_blocks,
-                       a.shared ? 1 : 0, a.pages, row);
+  if (a.max_blocks <= 4 * kWave * kHeld)
+    launch_select_of<4>(a, rows_per_seq, log2_block, rows, stream);
+  else
+    launch_select_of<16>(a, rows_per_seq, log2_block, rows, stream);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_page_bounds(const BoundsArgs& a, hipStream_t stream) {
-  if (a.is_bf16) return a.head_dim == 64 ? launch_bounds_as<bf16_t, 64>(a, stream) : launch_bounds_as<bf16_t, 128>(a, stream);
-  return a.head_dim == 64 ? launch_bounds_as<float, 64>(a, stream) : launch_bounds_as<float, 128>(a, stream);
+  return a.is_bf16 ? launch_bounds_as<bf16_t>(a, stream) : launch_bounds_as<float>(a, stream);
 }
 
 hipError_t launch_select_pages(const SelectArgs& a, hipStream_t stream) {
