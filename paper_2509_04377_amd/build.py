@@ -10,7 +10,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpe.so")
 HOST_LIB = os.path.join(HERE, "_pe_host.so")
 SOURCES = ["pe_api.hip", "score_blocks.hip", "evict_blocks.hip", "paged_decode.hip", "paged_decode_bf16.hip",
-           "prefill_prune.hip", "pe_api_rows.hip", "paged_rows.hip", "append_path.hip", "pe_api_pages.hip",
+           "prefill_prune.hip", "pe_api_rows.hip", "paged_rows.hip", "tree_wide.hip", "append_path.hip", "pe_api_pages.hip",
            "select_pages.hip"]
 # Packed fp32 VALU ops are switched off for all device code.  The leading kernel arguments (up to 14 dwords) are preloaded
 # into scalar registers instead of being loaded by every wave.

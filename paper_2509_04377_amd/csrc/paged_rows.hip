@@ -13,8 +13,8 @@
 //   at chunk 4*j + g; the contraction runs over the chunks, and Q is loaded by the same map.  Lane l is left with the logits of
 //   tokens 4*g + r of query n, r < 4.
 //   PV (A = V transposed, B = P): out^T[d][n] = sum_t V[t][d] P[t][n].  The logits' registers are the B operand as they lie
-//   (contraction index: the tokens 4*g + r of the step's 16-token parts), and row m of A is d = m*E + e in product e, E = D/16:
-//   lane l loads elements n*E .. n*E + E - 1 of its tokens 4*g + r, whole token rows for 16 neighbouring lanes.
+//   (contraction index: the tokens 4*g + r of the step's 16-token parts), and row m of A is d = m*E + e in product e, E = D/16
+//   (fp32: d = 64*(e/4) + 4*m + e%4): lane l loads those of row n of its tokens 4*g + r, whole runs of a token for 16 lanes.
 //   bfloat16 products contract 32 tokens (two parts), fp32 ones four, one for each r.
 //
 // bfloat16: a probability goes into the product as two bfloat16 terms, p = hi + lo + less than 2^-16 p (hi the upper half of its
@@ -27,40 +27,13 @@
 // Page weights (WEIGHTS): the sum of a part's probabilities is kept in LDS with the reference it is relative to (a store to memory
 // there would turn every wait for a load into a full one), and when the row's sums are known a page's weight is that of its parts.
 // With several splits each writes its pages' sums, and the launch that merges the splits makes the weights.
-#include "pe_decode_common.h"
-#include "pe_rows.h"
+#include "pe_rows_device.h"
 
 namespace pe {
 namespace {
 
-constexpr float kNegInf = -__builtin_inff();
-constexpr float kGrow = 3.f;
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-
-// What a wave needs before its first load comes first (the leading arguments are in scalar registers when it starts).
-struct RowsParams {
-  const int32_t *seq_lens, *block_table;
-  const void *k_pool, *v_pool;
-  int num_kv_heads, max_blocks;  // max_blocks < 0: a table row is a sequence's
-  uint32_t inv_heads;
-  uint32_t shape;                // log2 of the page size, query heads per KV head, order of the workgroups, splits
-  int tiles, drafts;             // workgroups for the query rows of a row; queries of a sequence
-  const void* q;
-  float scale_log2e;
-  float decay;
-  const int32_t* draft_lens;     // or null: every sequence has all of them
-  const uint64_t* mask;
-  const void *k_draft, *v_draft;
-  void* out;
-  float* partials;
-  const float* weights_in;       // or null
-  float* weights_out;
-  float* page_sums;              // [rows][max_blocks][G], where there are several splits
-};
 
 // Row geometry: elements of a 16-byte K chunk, chunks a lane loads of a token, elements of V a lane loads of a token.
 template <typename T, int D>
@@ -73,18 +46,10 @@ struct Geo {
   static constexpr int kChunks = D / kElems / 4;  // K: chunks a lane loads
   static constexpr int E = D / 16;                // V: elements a lane loads of a token
   static constexpr int kVDwords = E * (int)sizeof(T) / 4;
+  // The element of V that a lane's element e is, for lane n (row n of the product): 16 bytes a lane (D = 64, bfloat16: 8), so that
+  // 16 neighbouring lanes read 256 consecutive bytes.
+  static __device__ __forceinline__ int element_of(int n, int e) { return kBf16 ? n * E + e : e / 4 * 64 + n * 4 + e % 4; }
 };
-
-__device__ __forceinline__ int drafts_of(const RowsParams& p, int s) {
-  if (p.draft_lens == nullptr) return p.drafts;
-  const int have = p.draft_lens[s];
-  return have < 0 ? 0 : have < p.drafts ? have : p.drafts;
-}
-__device__ __forceinline__ int length_of(const RowsParams& p, int s, int max_blocks, int log2_block) {
-  const int len = p.seq_lens[s];
-  const int64_t most = (int64_t)max_blocks << log2_block;  // (a longer row is a caller error: its table ends here)
-  return len < 0 ? 0 : len < most ? len : (int)most;
-}
 
 // The weight of a page, from what earlier calls left and what this one adds.
 __device__ __forceinline__ void put_weight(const RowsParams& p, int64_t at, float got) {
@@ -97,7 +62,7 @@ __device__ __forceinline__ void put_weight(const RowsParams& p, int64_t at, floa
 }
 
 template <typename T, int D, int NQ, bool WEIGHTS>
-__global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(const RowsParams p) {
+__global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParams p) {
   using GE = Geo<T, D>;
   constexpr int STEP = GE::kStep, PARTS = GE::kParts, CH = GE::kChunks, E = GE::E, VD = GE::kVDwords, PER = GE::kPerRound;
   constexpr int ROWS = 16 * NQ;
@@ -168,16 +133,16 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
       if (keys) {
         const uint32_t off = ((uint32_t)n < last ? (uint32_t)n : last) * stride + (uint32_t)g * 16u;
 #pragma unroll
-        for (int j = 0; j < CH; ++j) kb[part][j] = *reinterpret_cast<const uint4*>(base + off + j * 64);
+        for (int j = 0; j < CH; ++j) kb[part][j] = load_vec(base + off, j * 4);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t t = (uint32_t)(4 * g + r);
-          const uint32_t off = (t < last ? t : last) * stride + (uint32_t)n * (E * (uint32_t)sizeof(T));
+          const uint32_t off = (t < last ? t : last) * stride + (uint32_t)n * (VD >= 4 ? 16u : 8u);
           if constexpr (VD >= 4) {
 #pragma unroll
             for (int w = 0; w < VD; w += 4) {
-              const uint4 v = *reinterpret_cast<const uint4*>(base + off + w * 4);
+              const uint4 v = load_vec_stream(base + off, w * 4);
               vb[part][r][w] = v.x, vb[part][r][w + 1] = v.y, vb[part][r][w + 2] = v.z, vb[part][r][w + 3] = v.w;
             }
           } else {
@@ -194,10 +159,12 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
   uint4 q[NQ][CH];
   uint64_t sees[NQ];  // drafts that the lane's query row attends to
   load(0, ids, true);
+  // (In this order: what is waited for first in the loop, K, has V behind it there, and the queries must not lie in between.)
+  __builtin_amdgcn_sched_barrier(0);
   const uint64_t real = drafts >= 64 ? ~0ull : (1ull << drafts) - 1;
 #pragma unroll
   for (int a = 0; a < NQ; ++a) {
-    const int r = row0 + 16 * a + n;
+    const int r = row0 + 16 * a + n;  // (behind the last one: the first one again, and written nowhere)
     int draft = 0, h = r < rows ? r : 0;
     if constexpr (!WEIGHTS) {
       draft = h / group;
@@ -207,18 +174,11 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
                                                        (((int64_t)s * (WEIGHTS ? 1 : p.drafts) + draft) * num_q_heads + hk * group + h) * D);
 #pragma unroll
     for (int j = 0; j < CH; ++j) q[a][j] = from[4 * j + g];
-    sees[a] = WEIGHTS ? 0ull : p.mask[(int64_t)s * p.drafts + draft];
+    sees[a] = WEIGHTS ? 0ull : p.mask[(int64_t)s * p.drafts + draft] & real;
   }
+  __builtin_amdgcn_sched_barrier(0);
   load(0, ids, false);
-#pragma unroll
-  for (int a = 0; a < NQ; ++a)
-    if (row0 + 16 * a + n >= rows) {
-#pragma unroll
-      for (int j = 0; j < CH; ++j) q[a][j] = make_uint4(0u, 0u, 0u, 0u);
-      sees[a] = 0ull;
-    } else {
-      sees[a] &= real;
-    }
+  __builtin_amdgcn_sched_barrier(0);
 
   f32x4_t acc[NQ][E];
   float m_run[NQ], m_ref[NQ], l_run[NQ];
@@ -239,10 +199,14 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
 #pragma unroll
     for (int a = 0; a < NQ; ++a)
 #pragma unroll
-      for (int part = 0; part < PARTS; ++part) {
-        f32x4_t c = {0.f, 0.f, 0.f, 0.f};
+      for (int part = 0; part < PARTS; ++part) x[a][part] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
+    for (int j = 0; j < CH; ++j)  // (neighbouring products add to different sums)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+        for (int a = 0; a < NQ; ++a) {
+          f32x4_t& c = x[a][part];
           if constexpr (GE::kBf16) {
             c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kb[part][j]), __builtin_bit_cast(bf16x8_t, q[a][j]),
                                                         c, 0, 0, 0);
@@ -253,8 +217,10 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
             c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kb[part][j].w), __uint_as_float(q[a][j].w), c, 0, 0, 0);
           }
         }
-        x[a][part] = c * p.scale_log2e;
-      }
+#pragma unroll
+    for (int a = 0; a < NQ; ++a)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) x[a][part] *= p.scale_log2e;
     load(k + 1, ids_next, true);
     if (!pool || tok0 + STEP > end) {
 #pragma unroll
@@ -317,18 +283,23 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
         lo[a] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-        const uint4 t = make_uint4(__builtin_amdgcn_perm(vb[0][1][e >> 1], vb[0][0][e >> 1], sel),
-                                   __builtin_amdgcn_perm(vb[0][3][e >> 1], vb[0][2][e >> 1], sel),
-                                   __builtin_amdgcn_perm(vb[PARTS - 1][1][e >> 1], vb[PARTS - 1][0][e >> 1], sel),
-                                   __builtin_amdgcn_perm(vb[PARTS - 1][3][e >> 1], vb[PARTS - 1][2][e >> 1], sel));
-        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, t);
+      for (int e = 0; e < E; e += 2) {
+        bf16x8_t v[2];
 #pragma unroll
-        for (int a = 0; a < NQ; ++a) {
-          acc[a][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi[a], acc[a][e], 0, 0, 0);
-          acc[a][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo[a], acc[a][e], 0, 0, 0);
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t sel = i != 0 ? 0x07060302u : 0x05040100u;
+          v[i] = __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_amdgcn_perm(vb[0][1][e >> 1], vb[0][0][e >> 1], sel),
+                                                         __builtin_amdgcn_perm(vb[0][3][e >> 1], vb[0][2][e >> 1], sel),
+                                                         __builtin_amdgcn_perm(vb[PARTS - 1][1][e >> 1], vb[PARTS - 1][0][e >> 1], sel),
+                                                         __builtin_amdgcn_perm(vb[PARTS - 1][3][e >> 1], vb[PARTS - 1][2][e >> 1], sel)));
         }
+#pragma unroll
+        for (int term = 0; term < 2; ++term)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int a = 0; a < NQ; ++a)
+              acc[a][e + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[i], term == 0 ? hi[a] : lo[a], acc[a][e + i], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -348,12 +319,12 @@ __global__ __launch_bounds__(kThreads, NQ >= 4 ? 1 : 2) void paged_rows_kernel(c
   for (int a = 0; a < NQ; ++a) {
     const float l = rows_sum(l_run[a]);
     if (g == 0) sm_ml[wave][n] = make_float2(m_run[a], l);
-    // lane (g, n) has rows 4*g + r of C: elements (4*g + r) * E + e of query n
+    // lane (g, n) has rows m = 4*g + r of C: elements element_of(m, e) of query n
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
       for (int e = 0; e < E; e += 4)
-        *reinterpret_cast<float4*>(&sm_acc[wave][n][(4 * g + r) * E + e]) =
+        *reinterpret_cast<float4*>(&sm_acc[wave][n][GE::element_of(4 * g + r, e)]) =
             make_float4(acc[a][e][r], acc[a][e + 1][r], acc[a][e + 2][r], acc[a][e + 3][r]);
     }
     __syncthreads();
@@ -494,12 +465,9 @@ __global__ __launch_bounds__(kThreads) void weights_merge_kernel(const RowsParam
 
 template <typename T, int D, int NQ>
 hipError_t launch_tiles(const RowsArgs& a, RowsParams p, hipStream_t stream) {
-  p.tiles = (a.drafts * shape_group(p.shape) + 16 * NQ - 1) / (16 * NQ);
-  PlaceGrid grid;
-  if (!place_grid(a.num_seqs, a.num_kv_heads, a.splits * p.tiles, true, &grid)) return hipErrorInvalidValue;
-  p.shape |= (grid.xcd ? kShapeXcd : 0u) | (grid.linear ? kShapeLinear : 0u);
-  p.inv_heads = grid.inv_heads;
-  const dim3 blocks(grid.x, grid.y), threads(kThreads);
+  dim3 blocks;
+  const dim3 threads(kThreads);
+  if (!rows_grid(a, 16 * NQ, &p, &blocks)) return hipErrorInvalidValue;
   if constexpr (NQ == 1) {
     if (a.weights_out != nullptr) {
       hipLaunchKernelGGL((paged_rows_kernel<T, D, 1, true>), blocks, threads, a.part_bytes, stream, p);
@@ -509,22 +477,23 @@ hipError_t launch_tiles(const RowsArgs& a, RowsParams p, hipStream_t stream) {
     }
   }
   hipLaunchKernelGGL((paged_rows_kernel<T, D, NQ, false>), blocks, threads, 0, stream, p);
-  if (a.splits > 1) {
-    const int64_t merges = (int64_t)a.num_seqs * a.num_kv_heads * ((a.drafts * shape_group(p.shape) + kWaves - 1) / kWaves);
-    hipLaunchKernelGGL((rows_merge_kernel<T, D>), dim3((unsigned)merges), threads, 0, stream, p);
-  }
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_rows(const RowsArgs& a, const RowsParams& p, hipStream_t stream) {
-  switch (a.tile_rows) {
-    case 16: return launch_tiles<T, D, 1>(a, p, stream);
-    case 32: return launch_tiles<T, D, 2>(a, p, stream);
-    case 64:
-      if constexpr (sizeof(T) == 2) return launch_tiles<T, D, 4>(a, p, stream);
+  hipError_t rc = hipErrorInvalidValue;
+  if (a.tile_rows == 16) rc = launch_tiles<T, D, 1>(a, p, stream);
+  if (a.tile_rows == 32) rc = launch_tiles<T, D, 2>(a, p, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (a.tile_rows > 32) rc = launch_tree_wide(a, p, stream);
   }
-  return hipErrorInvalidValue;
+  if (rc == hipSuccess && a.splits > 1 && a.weights_out == nullptr) {
+    const int64_t merges = (int64_t)a.num_seqs * a.num_kv_heads * ((a.drafts * shape_group(p.shape) + kWaves - 1) / kWaves);
+    hipLaunchKernelGGL((rows_merge_kernel<T, D>), dim3((unsigned)merges), dim3(kThreads), 0, stream, p);
+    rc = hipGetLastError();
+  }
+  return rc;
 }
 
 }  // namespace

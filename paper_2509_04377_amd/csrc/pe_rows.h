@@ -60,7 +60,9 @@ struct PathArgs {
 hipError_t launch_append_path(const PathArgs& a, hipStream_t stream);
 
 // Query rows that a workgroup of the attention takes.
-inline int tree_tile_rows(bool is_bf16, int rows) { return rows <= 16 ? 16 : rows <= 32 || !is_bf16 ? 32 : 64; }
+inline int tree_tile_rows(bool is_bf16, int rows) {
+  return rows <= 16 ? 16 : rows <= 32 || !is_bf16 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
 
 inline int tree_splits(bool is_bf16, int64_t kv_rows, int rows, int64_t tokens, int compute_units) {
   const int tile = tree_tile_rows(is_bf16, rows);

@@ -1,0 +1,61 @@
+// What the kernels for several query rows share: their arguments and small steps.
+#pragma once
+
+#include "pe_decode_common.h"
+#include "pe_rows.h"
+
+namespace pe {
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kGrow = 3.f;  // how far above the largest logit (log2) a reference is set
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+
+// What a wave needs before its first load comes first (the leading arguments are in scalar registers when it starts).
+struct RowsParams {
+  const int32_t *seq_lens, *block_table;
+  const void *k_pool, *v_pool;
+  int num_kv_heads, max_blocks;  // max_blocks < 0: a table row is a sequence's
+  uint32_t inv_heads;
+  uint32_t shape;                // log2 of the page size, query heads per KV head, order of the workgroups, splits
+  int tiles, drafts;             // workgroups for the query rows of a row; queries of a sequence
+  const void* q;
+  float scale_log2e;
+  float decay;
+  const int32_t* draft_lens;     // or null: every sequence has all of them
+  const uint64_t* mask;
+  const void *k_draft, *v_draft;
+  void* out;
+  float* partials;
+  const float* weights_in;       // or null
+  float* weights_out;
+  float* page_sums;              // [rows][max_blocks][G], where there are several splits
+};
+
+__device__ __forceinline__ int drafts_of(const RowsParams& p, int s) {
+  if (p.draft_lens == nullptr) return p.drafts;
+  const int have = p.draft_lens[s];
+  return have < 0 ? 0 : have < p.drafts ? have : p.drafts;
+}
+__device__ __forceinline__ int length_of(const RowsParams& p, int s, int max_blocks, int log2_block) {
+  const int len = p.seq_lens[s];
+  const int64_t most = (int64_t)max_blocks << log2_block;  // (a longer row is a caller error: its table ends here)
+  return len < 0 ? 0 : len < most ? len : (int)most;
+}
+
+// The grid for `rows` query rows a workgroup, and what of the arguments goes with it.
+inline bool rows_grid(const RowsArgs& a, int rows, RowsParams* p, dim3* blocks) {
+  p->tiles = (a.drafts * shape_group(p->shape) + rows - 1) / rows;
+  PlaceGrid grid;
+  if (!place_grid(a.num_seqs, a.num_kv_heads, a.splits * p->tiles, true, &grid)) return false;
+  p->shape |= (grid.xcd ? kShapeXcd : 0u) | (grid.linear ? kShapeLinear : 0u);
+  p->inv_heads = grid.inv_heads;
+  *blocks = dim3(grid.x, grid.y);
+  return true;
+}
+
+// The attention of trees with many query rows, without the merge of the splits (tree_wide.hip).
+hipError_t launch_tree_wide(const RowsArgs& a, const RowsParams& p, hipStream_t stream);
+
+}  // namespace pe

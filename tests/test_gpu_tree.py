@@ -48,7 +48,7 @@ def _case(seed, lens, counts, T, Hk, G, D, B, dtype, shared, kind="tree", scale=
     return c, q, kd, vd, sees, words
 
 
-def _want(c, q, kd, vd, sees, counts, G):
+def _want(c, q, kd, vd, sees, counts, G, scale=None):
     S, T, Hq, D = q.shape
     want, bound = torch.zeros((S, T, Hq, D), dtype=torch.float64), torch.zeros((S, T, Hq, D), dtype=torch.float64)
     for s, n in enumerate(counts):
@@ -56,12 +56,12 @@ def _want(c, q, kd, vd, sees, counts, G):
             k = torch.cat((c.k[s][h // G], kd[s, :n, h // G].double()))
             v = torch.cat((c.v[s][h // G], vd[s, :n, h // G].double()))
             m = torch.cat((torch.ones((n, c.lens[s]), dtype=torch.bool), sees[s, :n, :n]), 1)
-            o, _, b = attend(q[s, :n, h].double(), k, v, m)
+            o, _, b = attend(q[s, :n, h].double(), k, v, m, scale)
             want[s, :n, h], bound[s, :n, h] = o, b
     return want, bound
 
 
-def _run(c, q, kd, vd, words, counts, T, splits=0, out=None, ws=None):
+def _run(c, q, kd, vd, words, counts, T, splits=0, out=None, ws=None, scale=None):
     desc = c.desc(pe, q.shape[2], decode_splits=splits)
     kp, vp, table, lens = c.to(DEV)
     if out is None:
@@ -71,7 +71,8 @@ def _run(c, q, kd, vd, words, counts, T, splits=0, out=None, ws=None):
         if ws is not None:
             ws.fill_(0xff)   # NaN wherever nothing is written
     dl = None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV)
-    pe.pe_tree_decode(desc, T, q.to(DEV), kd.to(DEV), vd.to(DEV), dl, words.to(DEV), kp, vp, table, lens, q.shape[3] ** -0.5, out, ws)
+    pe.pe_tree_decode(desc, T, q.to(DEV), kd.to(DEV), vd.to(DEV), dl, words.to(DEV), kp, vp, table, lens,
+                      q.shape[3] ** -0.5 if scale is None else scale, out, ws)
     return out
 
 
@@ -123,6 +124,19 @@ def test_large_logits(dt):
     want, bound = _want(c, q, kd, vd, sees, counts, G)
     for splits in (1, 4):
         _check(_run(c, q, kd, vd, words, counts, T, splits), want, bound, counts, DTYPES[dt])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 16, 60])
+@pytest.mark.parametrize("scale", [0.0, -0.25, 1.5])
+def test_any_finite_scale(dt, T, scale):
+    """Zero weighs all alike, a negative one prefers the smallest product."""
+    print("case scale", dt, T, scale, flush=True)
+    lens, counts, G = [130, 0, 17], [T, T, 2], 4
+    c, q, kd, vd, sees, words = _case(7, lens, counts, T, 1, G, 128, 16, DTYPES[dt], False, "any")
+    want, bound = _want(c, q, kd, vd, sees, counts, G, scale)
+    for splits in (1, 2):
+        _check(_run(c, q, kd, vd, words, counts, T, splits, scale=scale), want, bound, counts, DTYPES[dt])
 
 
 def test_one_draft_is_a_decode_step():
