@@ -2,8 +2,8 @@
 //
 // The products count here, not the traffic: 256 query rows ask for 256 operations a byte of the cache.  A workgroup owns 32 query rows a
 // wave and one split of the tokens (tiles of 64, the drafts are the last one); K and V of a tile go through LDS once for all its waves,
-// which read them as operands of the 32 x 32 x 16 products.  The next tile is on its way to registers while one is computed, and goes
-// into the other half of LDS behind it; one barrier a tile.
+// which read them as operands of the 32 x 32 x 16 products.  Two tiles are on their way to registers while one is computed out of one half
+// of LDS and the next is put into the other; one barrier a tile.
 //
 // With lane l = 32*h + n:
 //   QK (A = K, B = Q): C[m][n] = <k_m, q_n>.  Lane l reads 16 bytes of token n (as row m), chunk 2*j + h; a token's chunks lie in LDS in an
@@ -23,13 +23,19 @@ constexpr int kTile = 64;  // tokens
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
+template <int P>
+struct Parity {
+  static constexpr int value = P;
+};
+
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsParams p) {
   constexpr int NT = WAVES * kWave, ROWS = 32 * WAVES;
   constexpr int CPT = D / 8;                 // 16-byte chunks of a token
-  constexpr int NL = kTile * CPT / NT;       // chunks of K (and of V) that a thread brings
+  constexpr int NL = kTile * CPT / NT;       // 16-byte chunks of K (and of V) that a lane brings
   constexpr int CH = D / 16;                 // products of QK
   constexpr int E = D / 32;                  // elements of V that a lane reads of a token
+  constexpr int SETS = WAVES == 8 ? 2 : 1;
   static_assert(NL * NT == kTile * CPT, "whole chunks");
   __shared__ uint4 sk[2][kTile * CPT], sv[2][kTile * CPT];
 
@@ -41,52 +47,62 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
   const int s = at.seq, hk = at.head, split = at.split / p.tiles, tile0 = at.split - split * p.tiles;
   const bool shared = p.max_blocks < 0;
   const int max_blocks = shared ? -p.max_blocks : p.max_blocks;
-  const int32_t* bt = p.block_table + (int64_t)(shared ? s : at.row) * max_blocks;
+  // (read only while the launch runs: scalar loads, which the barriers would otherwise forbid)
+  const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(p.block_table + (int64_t)(shared ? s : at.row) * max_blocks));
   const int drafts = drafts_of(p, s), rows = drafts * group, row0 = tile0 * ROWS;
   if (row0 >= rows) return;
   const int len = length_of(p, s, max_blocks, log2_block);
   const int cached = len / kTile + (len % kTile != 0), tiles = cached + 1;
 
-  // ---- staging: a thread's chunks of a tile ----------------------------------------------------------------------------
-  const int c_of = tid % CPT, t_of = tid / CPT;  // chunk, and token of the first one; the others are NT / CPT tokens further on
-  const uint32_t token_vecs = (uint32_t)(shared ? p.num_kv_heads * CPT : CPT), draft_vecs = (uint32_t)p.num_kv_heads * CPT;
+  // ---- staging ------------------------------------------------------------------------------------------------------------
+  // A wave brings NL runs of K and of V of a tile, TPL token rows each, which lie in one page: its place is looked up with scalar loads.
+  constexpr int TPL = kWave / CPT;
+  const int t_lane = lane / CPT, c_of = lane % CPT;
+  const uint32_t token_bytes = (uint32_t)(shared ? p.num_kv_heads : 1) * (D * 2), draft_bytes = (uint32_t)p.num_kv_heads * (D * 2);
+  const uint32_t lane_off = (uint32_t)t_lane * token_bytes + (uint32_t)c_of * 16u;
+  const auto run_of = [&](int i) { return (i * WAVES + wave) * TPL; };  // the first token of run i in its tile
   int ids[NL];
-  const auto lookup = [&](int tile) {
+  const auto lookup = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int64_t j = ((int64_t)tile * kTile + t_of + i * (NT / CPT)) >> log2_block;
-      ids[i] = bt[j < max_blocks ? (int)j : max_blocks - 1];
+      const int64_t j = ((int64_t)tile * kTile + run_of(i)) >> log2_block;
+      ids[i] = table[j < max_blocks ? (int)j : max_blocks - 1];
     }
   };
-  uint4 kr[NL], vr[NL];
-  const auto fetch = [&](int tile) {  // (what is no token, or no tile, reads one that is)
+  // With eight waves two tiles are on their way, each set of registers belongs to every other tile of this workgroup; fewer waves have as
+  // many bytes on their way with one.
+  uint4 kr[SETS][NL], vr[SETS][NL];
+  const auto fetch = [&](int tile, uint4 (&k)[NL], uint4 (&v)[NL]) __attribute__((always_inline)) {  // (what is no token, or no tile, reads one that is)
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int t = t_of + i * (NT / CPT);
-      int64_t vec;
-      const uint4 *k, *v;
-      if (tile < cached) {
-        const int slot = (int)(((int64_t)tile * kTile + t) & ((1 << log2_block) - 1));
-        vec = (((int64_t)(ids[i] < 0 ? 0 : ids[i]) << log2_block) + slot) * token_vecs + (shared ? hk * CPT : 0) + c_of;
-        k = static_cast<const uint4*>(p.k_pool), v = static_cast<const uint4*>(p.v_pool);
+      int64_t base;
+      uint32_t off = lane_off;
+      const bool pool = tile < cached;
+      if (pool) {
+        const int slot = (int)(((int64_t)tile * kTile + run_of(i)) & ((1 << log2_block) - 1));
+        base = (((int64_t)(ids[i] < 0 ? 0 : ids[i]) << log2_block) + slot) * token_bytes + (shared ? hk * (D * 2) : 0);
       } else {
-        vec = ((int64_t)s * p.drafts + (t < drafts ? t : 0)) * draft_vecs + hk * CPT + c_of;
-        k = static_cast<const uint4*>(p.k_draft), v = static_cast<const uint4*>(p.v_draft);
+        const int t = run_of(i) + t_lane;
+        off = (uint32_t)(t < drafts ? t : 0) * draft_bytes + (uint32_t)c_of * 16u;
+        base = (int64_t)s * p.drafts * draft_bytes + hk * (D * 2);
       }
-      kr[i] = k[vec];
-      vr[i] = v[vec];
+      k[i] = load_vec(static_cast<const char*>(pool ? p.k_pool : p.k_draft) + base + off, 0);
+      v[i] = load_vec(static_cast<const char*>(pool ? p.v_pool : p.v_draft) + base + off, 0);
     }
   };
-  const auto stage = [&](int tile, int buf) {
+  const auto stage = [&](int tile, int buf, const uint4 (&k)[NL], const uint4 (&v)[NL]) __attribute__((always_inline)) {
     const int end = tile < cached ? len - tile * kTile : drafts;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int t = t_of + i * (NT / CPT);
-      sk[buf][t * CPT + (c_of ^ (t & (CPT - 1)))] = kr[i];
-      sv[buf][t * CPT + c_of] = t < end ? vr[i] : make_uint4(0u, 0u, 0u, 0u);  // junk V must not meet the zeros of its probabilities
+      const int t = run_of(i) + t_lane;
+      sk[buf][t * CPT + (c_of ^ (t & (CPT - 1)))] = k[i];
+      const uint32_t keep = t < end ? ~0u : 0u;  // junk V must not meet the zeros of its probabilities
+      sv[buf][t * CPT + c_of] = make_uint4(v[i].x & keep, v[i].y & keep, v[i].z & keep, v[i].w & keep);
     }
   };
 
+  // The first two tiles' pages, and behind them the length that says whether there are such tiles.
   lookup(split);
   // ---- queries -----------------------------------------------------------------------------------------------------------
   const int num_q_heads = p.num_kv_heads * group;
@@ -114,50 +130,44 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
 
-  const bool works = row0 + 32 * wave < rows;  // (a wave without rows brings its chunks all the same)
-  int buf = 0;
-  if (split < tiles) {
-    fetch(split);
-    lookup(split + splits);
-    stage(split, 0);
+  const bool works = row0 + 32 * wave < rows;  // (a wave without rows brings its runs all the same)
+  // Tile i of this workgroup is number split + i * splits.  While one is computed, the next is in LDS (or on its way there) and the one behind
+  // it in registers (or on its way there).
+  const auto number = [&](int i) { return split + i * splits; };
+  fetch(number(0), kr[0], vr[0]);
+  lookup(number(1));
+  if constexpr (SETS == 2) {
+    fetch(number(1), kr[1], vr[1]);
+    lookup(number(2));
   }
-  for (int tile = split; tile < tiles; tile += splits, buf ^= 1) {
-    __syncthreads();  // this tile is in LDS, and nobody reads the other half any more
-    const bool more = tile + splits < tiles;
-    if (more) {
-      fetch(tile + splits);
-      lookup(tile + 2 * splits);
-    }
-    if (works) {
-      f32x16_t x[2];
+  stage(number(0), 0, kr[0], vr[0]);
+  fetch(number(SETS), kr[0], vr[0]);
+  lookup(number(SETS + 1));
+  const auto compute = [&](int tile, int buf) __attribute__((always_inline)) {
+    const uint4* kt = &sk[buf][n * CPT];
+    const uint32_t* vt = reinterpret_cast<const uint32_t*>(&sv[buf][0]) + 4 * h * (D / 2) + n * (E / 2);
+    const int end = tile < cached ? len - tile * kTile : drafts;
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub)
+    for (int sub = 0; sub < 2; ++sub) {  // 32 tokens
+      f32x16_t x;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[sub][i] = 0.f;
-      const uint4* kt = &sk[buf][n * CPT];
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < CH; ++j)
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          const uint4 k = kt[sub * 32 * CPT + ((2 * j) ^ (h ^ (n & (CPT - 1))))];
-          x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), q[j], x[sub], 0, 0, 0);
-        }
-      const int end = tile < cached ? len - tile * kTile : drafts;
+      for (int j = 0; j < CH; ++j) {
+        const uint4 k = kt[sub * 32 * CPT + ((2 * j) ^ (h ^ (n & (CPT - 1))))];
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), q[j], x, 0, 0, 0);
+      }
       if (end < kTile || tile >= cached) {
         const uint64_t mine = (tile < cached ? ~0ull : sees) >> (4 * h);
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = 32 * sub + 8 * (i / 4) + i % 4;  // and 4 h
-            if (t + 4 * h >= end || ((mine >> t) & 1u) == 0) x[sub][i] = kNegInf;
-          }
+        for (int i = 0; i < 16; ++i) {
+          const int t = 32 * sub + 8 * (i / 4) + i % 4;  // and 4 h
+          if (t + 4 * h >= end || ((mine >> t) & 1u) == 0) x[i] = kNegInf;
+        }
       }
       float mx = kNegInf;
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[sub][i]);
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[i]);
       mx *= scale;
       if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0ull) {
         mx = halves_max(mx);
@@ -170,12 +180,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
         m_run = m_new;
         m_ref = ref;
       }
-      const uint32_t* vt = reinterpret_cast<const uint32_t*>(&sv[buf][0]) + 4 * h * (D / 2) + n * (E / 2);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {  // 16 tokens
+      for (int c = 0; c < 2; ++c) {  // 16 tokens
         float pr[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(fmaf(x[c / 2][8 * (c % 2) + i], scale, -m_ref));
+        for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(fmaf(x[8 * c + i], scale, -m_ref));
         l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
         uint32_t hw[4], lw[4];
 #pragma unroll
@@ -190,7 +199,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
         uint32_t vb[8][E / 2];
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          const uint32_t* from = vt + (16 * c + (t / 4) * 8 + t % 4) * (D / 2);
+          const uint32_t* from = vt + (32 * sub + 16 * c + (t / 4) * 8 + t % 4) * (D / 2);
           if constexpr (E == 4) {
             const uint2 v = *reinterpret_cast<const uint2*>(from);
             vb[t][0] = v.x, vb[t][1] = v.y;
@@ -213,7 +222,19 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
         for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[e], lo, acc[e], 0, 0, 0);
       }
     }
-    if (more) stage(tile + splits, buf ^ 1);
+  };
+  // Tile i is in LDS half i % 2 and was in registers i % SETS.
+  const auto turn = [&](int i, auto parity) __attribute__((always_inline)) {
+    constexpr int kNow = decltype(parity)::value, kNext = kNow ^ 1, kSet = kNext % SETS;
+    __syncthreads();  // this tile is in LDS, and nobody reads the other half any more
+    stage(number(i + 1), kNext, kr[kSet], vr[kSet]);
+    fetch(number(i + 1 + SETS), kr[kSet], vr[kSet]);
+    lookup(number(i + 2 + SETS));
+    if (works && number(i) < tiles) compute(number(i), kNow);
+  };
+  for (int i = 0; number(i) < tiles; i += 2) {  // (always both: on a way out between them the loads that are waited for next would be the last)
+    turn(i, Parity<0>{});
+    turn(i + 1, Parity<1>{});
   }
 
   // ---- every wave has its rows' whole states: lane (h, n) rows m = 8*(i/4) + 4*h + i%4 of C, elements m*E + e of query n ------------
