@@ -486,7 +486,7 @@ hipError_t launch_rows(const RowsArgs& a, const RowsParams& p, hipStream_t strea
   if (a.tile_rows == 16) rc = launch_tiles<T, D, 1>(a, p, stream);
   if (a.tile_rows == 32) rc = launch_tiles<T, D, 2>(a, p, stream);
   if constexpr (sizeof(T) == 2) {
-    if (a.tile_rows > 32) rc = launch_tree_wide(a, p, stream);
+    if (a.tile_rows == kWideRows) rc = launch_tree_wide(a, p, stream);
   }
   if (rc == hipSuccess && a.splits > 1 && a.weights_out == nullptr) {
     const int64_t merges = (int64_t)a.num_seqs * a.num_kv_heads * ((a.drafts * shape_group(p.shape) + kWaves - 1) / kWaves);

@@ -52,7 +52,8 @@ int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q,
   a.max_blocks = desc->max_blocks;
   a.is_bf16 = desc->dtype == PE_BF16;
   a.shared = desc->layout == PE_LAYOUT_SHARED;
-  a.tile_rows = pe::tree_tile_rows(a.is_bf16, num_drafts * (desc->num_q_heads / desc->num_kv_heads));
+  a.tile_rows = pe::tree_tile_rows(a.is_bf16, (int64_t)desc->num_seqs * desc->num_kv_heads,
+                                   num_drafts * (desc->num_q_heads / desc->num_kv_heads), compute_units());
   a.splits = pe::tree_splits_of(desc, num_drafts);
   return pe::launch_paged_rows(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PE_OK : PE_ERR_HIP;
 }

@@ -59,18 +59,27 @@ struct PathArgs {
 };
 hipError_t launch_append_path(const PathArgs& a, hipStream_t stream);
 
-// Query rows that a workgroup of the attention takes.
-inline int tree_tile_rows(bool is_bf16, int rows) {
-  return rows <= 16 ? 16 : rows <= 32 || !is_bf16 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+// Query rows that a workgroup of the attention takes: 16 or 32 of paged_rows.hip, or kWideRows of tree_wide.hip (bfloat16).  Few rows a
+// workgroup make many of them, which fill the chip without splits (whose merge costs), and read K and V again and again (out of the
+// second-level cache).  Measured on an MI355X, each form with as many splits as leave no compute unit two workgroups, 16 | 32 | 256, us
+// (bfloat16, eight KV heads of D = 128, 4096 tokens a sequence):
+//   one sequence, 32 query rows a KV head 12.9 | 15.5 | 17.3, 64 rows 14.5 | 16.2 | 18.5, 128 rows 18.9 | 18.1 | 21.4, 256 rows 27.9 | 23.1 | 28.5;
+//   eight sequences, 32 rows 30.9 | 29.6 | 37.5, 64 rows 45.6 | 36.5 | 41.6, 96 rows 86.5 | 49.9 | 45.4, 128 rows 86.4 | 52.2 | 48.4, 192 rows
+//   129.8 | 92.8 | 64.0; 32 sequences of 1024 to 2048 tokens, 32 rows 55.9 | 43.1 | 60.0, 64 rows 94.8 | 63.5 | 61.8, 128 rows 165.5 | 106.6 | 71.8.
+constexpr int kWideRows = 256;
+inline int tree_tile_rows(bool is_bf16, int64_t kv_rows, int rows, int compute_units) {
+  const int64_t of16 = kv_rows * ((rows + 15) / 16), of32 = kv_rows * ((rows + 31) / 32);
+  if (rows <= 16 || of16 * 8 <= compute_units) return 16;
+  return !is_bf16 || rows <= 64 || of32 * 4 <= compute_units ? 32 : kWideRows;
 }
 
+// Splits of a row: as many as leave no compute unit two workgroups, of 128 tokens or more (of the table's, which the host knows).
 inline int tree_splits(bool is_bf16, int64_t kv_rows, int rows, int64_t tokens, int compute_units) {
-  const int tile = tree_tile_rows(is_bf16, rows);
+  const int tile = tree_tile_rows(is_bf16, kv_rows, rows, compute_units);
   const int64_t groups = kv_rows * ((rows + tile - 1) / tile);
-  int64_t splits = (compute_units + groups - 1) / groups;
-  const int64_t by_len = tokens / 256 < 1 ? 1 : tokens / 256;
-  if (splits > by_len) splits = by_len;
-  return splits > 64 ? 64 : (int)splits;
+  int64_t splits = compute_units / groups;
+  if (splits > tokens / 128) splits = tokens / 128;
+  return splits > 64 ? 64 : splits < 1 ? 1 : (int)splits;
 }
 
 // Page weights: the parts of a split lie in LDS, 8 bytes for every 16 tokens and query head, beside what the waves' states take.

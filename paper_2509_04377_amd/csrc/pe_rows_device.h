@@ -56,6 +56,6 @@ inline bool rows_grid(const RowsArgs& a, int rows, RowsParams* p, dim3* blocks) 
 }
 
 // The attention of trees with many query rows, without the merge of the splits (tree_wide.hip).
-hipError_t launch_tree_wide(const RowsArgs& a, const RowsParams& p, hipStream_t stream);
+hipError_t launch_tree_wide(const RowsArgs& a, RowsParams p, hipStream_t stream);
 
 }  // namespace pe

@@ -2,40 +2,42 @@
 //
 // The products count here, not the traffic: 256 query rows ask for 256 operations a byte of the cache.  A workgroup owns 32 query rows a
 // wave and one split of the tokens (tiles of 64, the drafts are the last one); K and V of a tile go through LDS once for all its waves,
-// which read them as operands of the 32 x 32 x 16 products.  Two tiles are on their way to registers while one is computed out of one half
-// of LDS and the next is put into the other; one barrier a tile.
+// which read them as operands of the 32 x 32 x 16 products.  The tile behind the next one is on its way to registers while one is computed
+// out of one half of LDS and the next is put into the other; one barrier a tile.
 //
 // With lane l = 32*h + n:
 //   QK (A = K, B = Q): C[m][n] = <k_m, q_n>.  Lane l reads 16 bytes of token n (as row m), chunk 2*j + h; a token's chunks lie in LDS in an
 //   order of their own (chunk ^ token), so that neighbouring tokens' do not meet in the same banks.  Lane l is left with tokens
 //   8*(i/4) + 4*h + i%4 of query n, i < 16.
 //   PV (A = V transposed, B = P): a product contracts 16 tokens, lane half h those that it has: registers 8*c .. 8*c + 7 of the logits.  Row m
-//   of A is d = m*E + e in product e, E = D/32: lane l reads elements n*E .. of its eight tokens, and byte permutes bring a token's
-//   elements together with the others'.
+//   of A is element 32*e + m in product e; the reads that turn 16 elements of four tokens over 16 lanes bring it out of LDS as it lies.
 //
-// Probabilities go into the product as two bfloat16 terms, as in paged_rows.hip, and the softmax is that one too.
+// Probabilities go into the product as two bfloat16 terms, as in paged_rows.hip, and the softmax is that one too.  (In one term, rounded, 64
+// drafts x 4 heads over 8 caches of 4001 to 8192 tokens of D = 128 take 90 us instead of 104, and the outputs are sqrt(2) times as far from 64
+// bits: their own rounding, and as much again.)
 #include "pe_rows_device.h"
 
 namespace pe {
 namespace {
 
 constexpr int kTile = 64;  // tokens
+constexpr int WAVES = kWideRows / 32, NT = WAVES * kWave;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 template <int P>
 struct Parity {
   static constexpr int value = P;
 };
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsParams p) {
-  constexpr int NT = WAVES * kWave, ROWS = 32 * WAVES;
+template <int D>
+__global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
   constexpr int CPT = D / 8;                 // 16-byte chunks of a token
   constexpr int NL = kTile * CPT / NT;       // 16-byte chunks of K (and of V) that a lane brings
   constexpr int CH = D / 16;                 // products of QK
   constexpr int E = D / 32;                  // elements of V that a lane reads of a token
-  constexpr int SETS = WAVES == 8 ? 2 : 1;
   static_assert(NL * NT == kTile * CPT, "whole chunks");
   __shared__ uint4 sk[2][kTile * CPT], sv[2][kTile * CPT];
 
@@ -50,7 +52,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
   // (read only while the launch runs: scalar loads, which the barriers would otherwise forbid)
   const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
       reinterpret_cast<uintptr_t>(p.block_table + (int64_t)(shared ? s : at.row) * max_blocks));
-  const int drafts = drafts_of(p, s), rows = drafts * group, row0 = tile0 * ROWS;
+  const int drafts = drafts_of(p, s), rows = drafts * group, row0 = tile0 * kWideRows;
   if (row0 >= rows) return;
   const int len = length_of(p, s, max_blocks, log2_block);
   const int cached = len / kTile + (len % kTile != 0), tiles = cached + 1;
@@ -61,6 +63,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
   const int t_lane = lane / CPT, c_of = lane % CPT;
   const uint32_t token_bytes = (uint32_t)(shared ? p.num_kv_heads : 1) * (D * 2), draft_bytes = (uint32_t)p.num_kv_heads * (D * 2);
   const uint32_t lane_off = (uint32_t)t_lane * token_bytes + (uint32_t)c_of * 16u;
+  // (the drafts' places as distances from the pools': a choice between two arguments would load the chosen one every time)
+  const int64_t k_far = static_cast<const char*>(p.k_draft) - static_cast<const char*>(p.k_pool);
+  const int64_t v_far = static_cast<const char*>(p.v_draft) - static_cast<const char*>(p.v_pool);
   const auto run_of = [&](int i) { return (i * WAVES + wave) * TPL; };  // the first token of run i in its tile
   int ids[NL];
   const auto lookup = [&](int tile) __attribute__((always_inline)) {
@@ -70,10 +75,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
       ids[i] = table[j < max_blocks ? (int)j : max_blocks - 1];
     }
   };
-  // With eight waves two tiles are on their way, each set of registers belongs to every other tile of this workgroup; fewer waves have as
-  // many bytes on their way with one.
-  uint4 kr[SETS][NL], vr[SETS][NL];
-  const auto fetch = [&](int tile, uint4 (&k)[NL], uint4 (&v)[NL]) __attribute__((always_inline)) {  // (what is no token, or no tile, reads one that is)
+  uint4 kr[NL], vr[NL];  // the tile behind the next one
+  const auto fetch = [&](int tile) __attribute__((always_inline)) {  // (what is no token, or no tile, reads one that is)
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       int64_t base;
@@ -87,18 +90,20 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
         off = (uint32_t)(t < drafts ? t : 0) * draft_bytes + (uint32_t)c_of * 16u;
         base = (int64_t)s * p.drafts * draft_bytes + hk * (D * 2);
       }
-      k[i] = load_vec(static_cast<const char*>(pool ? p.k_pool : p.k_draft) + base + off, 0);
-      v[i] = load_vec(static_cast<const char*>(pool ? p.v_pool : p.v_draft) + base + off, 0);
+      kr[i] = load_vec(static_cast<const char*>(p.k_pool) + (base + (pool ? 0 : k_far)) + off, 0);
+      vr[i] = load_vec(static_cast<const char*>(p.v_pool) + (base + (pool ? 0 : v_far)) + off, 0);
     }
   };
-  const auto stage = [&](int tile, int buf, const uint4 (&k)[NL], const uint4 (&v)[NL]) __attribute__((always_inline)) {
+  // What a token's chunks are exchanged by in LDS: K is read from 8 tokens' chunk j at once, V from 4 tokens' four neighbouring ones.
+  const auto v_swap = [](int t) { return CPT == 16 ? (t & 3) << 2 : (t >> 1 & 1) << 2; };
+  const auto stage = [&](int tile, int buf) __attribute__((always_inline)) {
     const int end = tile < cached ? len - tile * kTile : drafts;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int t = run_of(i) + t_lane;
-      sk[buf][t * CPT + (c_of ^ (t & (CPT - 1)))] = k[i];
+      sk[buf][t * CPT + (c_of ^ (t & (CPT - 1)))] = kr[i];
       const uint32_t keep = t < end ? ~0u : 0u;  // junk V must not meet the zeros of its probabilities
-      sv[buf][t * CPT + c_of] = make_uint4(v[i].x & keep, v[i].y & keep, v[i].z & keep, v[i].w & keep);
+      sv[buf][t * CPT + (c_of ^ v_swap(t))] = make_uint4(vr[i].x & keep, vr[i].y & keep, vr[i].z & keep, vr[i].w & keep);
     }
   };
 
@@ -134,156 +139,143 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void tree_wide_kernel(const RowsP
   // Tile i of this workgroup is number split + i * splits.  While one is computed, the next is in LDS (or on its way there) and the one behind
   // it in registers (or on its way there).
   const auto number = [&](int i) { return split + i * splits; };
-  fetch(number(0), kr[0], vr[0]);
+  fetch(number(0));
   lookup(number(1));
-  if constexpr (SETS == 2) {
-    fetch(number(1), kr[1], vr[1]);
-    lookup(number(2));
-  }
-  stage(number(0), 0, kr[0], vr[0]);
-  fetch(number(SETS), kr[0], vr[0]);
-  lookup(number(SETS + 1));
-  const auto compute = [&](int tile, int buf) __attribute__((always_inline)) {
+  stage(number(0), 0);
+  fetch(number(1));
+  lookup(number(2));
+  // Where a lane reads K, and V: each 16 lanes get 16 elements of four tokens, turned so that a lane has one element of the four.
+  const int k_swap = h ^ (n & (CPT - 1));
+  const int v_tok = 4 * h + (lane & 15) / 4;  // and 8 more for the other four, of every 16 tokens
+  const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), v_half = lane & 1;
+  uint32_t v_at[2][E];  // in 8 bytes
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int t = v_tok + 8 * b;
+      v_at[b][e] = (uint32_t)(t * CPT + ((4 * e + v_chunk) ^ v_swap(t))) * 2u + (uint32_t)v_half;
+    }
+  const auto logits = [&](int buf, f32x16_t (&x)[2]) __attribute__((always_inline)) {
     const uint4* kt = &sk[buf][n * CPT];
-    const uint32_t* vt = reinterpret_cast<const uint32_t*>(&sv[buf][0]) + 4 * h * (D / 2) + n * (E / 2);
-    const int end = tile < cached ? len - tile * kTile : drafts;
+    uint4 k[CH];
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {  // 32 tokens
-      f32x16_t x;
+    for (int j = 0; j < CH; ++j) k[j] = kt[(2 * j) ^ k_swap];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[sub][i] = 0.f;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        const uint4 k = kt[sub * 32 * CPT + ((2 * j) ^ (h ^ (n & (CPT - 1))))];
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), q[j], x, 0, 0, 0);
-      }
-      if (end < kTile || tile >= cached) {
-        const uint64_t mine = (tile < cached ? ~0ull : sees) >> (4 * h);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = 32 * sub + 8 * (i / 4) + i % 4;  // and 4 h
-          if (t + 4 * h >= end || ((mine >> t) & 1u) == 0) x[i] = kNegInf;
-        }
-      }
-      float mx = kNegInf;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[i]);
-      mx *= scale;
-      if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0ull) {
-        mx = halves_max(mx);
-        const float m_new = mx > m_run ? mx + kGrow : m_run;
-        const float ref = m_new == kNegInf ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - ref);
-        l_run *= alpha;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= alpha;
-        m_run = m_new;
-        m_ref = ref;
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {  // 16 tokens
-        float pr[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(fmaf(x[8 * c + i], scale, -m_ref));
-        l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-        uint32_t hw[4], lw[4];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t p0 = __float_as_uint(pr[2 * w]), p1 = __float_as_uint(pr[2 * w + 1]);
-          hw[w] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
-          const float r0 = pr[2 * w] - __uint_as_float(p0 & 0xffff0000u), r1 = pr[2 * w + 1] - __uint_as_float(p1 & 0xffff0000u);
-          lw[w] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
-        }
-        const bf16x8_t hi = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
-        const bf16x8_t lo = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
-        uint32_t vb[8][E / 2];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const uint32_t* from = vt + (32 * sub + 16 * c + (t / 4) * 8 + t % 4) * (D / 2);
-          if constexpr (E == 4) {
-            const uint2 v = *reinterpret_cast<const uint2*>(from);
-            vb[t][0] = v.x, vb[t][1] = v.y;
-          } else {
-            vb[t][0] = from[0];
-          }
-        }
-        bf16x8_t va[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-          va[e] = __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_amdgcn_perm(vb[1][e >> 1], vb[0][e >> 1], sel),
-                                                          __builtin_amdgcn_perm(vb[3][e >> 1], vb[2][e >> 1], sel),
-                                                          __builtin_amdgcn_perm(vb[5][e >> 1], vb[4][e >> 1], sel),
-                                                          __builtin_amdgcn_perm(vb[7][e >> 1], vb[6][e >> 1], sel)));
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[e], hi, acc[e], 0, 0, 0);
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[e], lo, acc[e], 0, 0, 0);
+        x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[j]), q[j], x[sub], 0, 0, 0);
+        if (sub == 0) k[j] = kt[32 * CPT + ((2 * j) ^ k_swap)];
       }
     }
   };
-  // Tile i is in LDS half i % 2 and was in registers i % SETS.
+  const auto values = [&](int tile, int buf, f32x16_t (&x)[2]) __attribute__((always_inline)) {
+    lds_s16x4_t* const vt = (lds_s16x4_t*)&sv[buf][0];
+    const int end = tile < cached ? len - tile * kTile : drafts;
+    if (end < kTile || tile >= cached) {
+      const uint64_t mine = (tile < cached ? ~0ull : sees) >> (4 * h);
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int t = 32 * sub + 8 * (i / 4) + i % 4;  // and 4 h
+          if (t + 4 * h >= end || ((mine >> t) & 1u) == 0) x[sub][i] = kNegInf;
+        }
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[sub][i]);
+    mx *= scale;
+    if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0ull) {
+      mx = halves_max(mx);
+      const float m_new = mx > m_run ? mx + kGrow : m_run;
+      const float ref = m_new == kNegInf ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - ref);
+      l_run *= alpha;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] *= alpha;
+      m_run = m_new;
+      m_ref = ref;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {  // 16 tokens
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[c / 2][8 * (c % 2) + 2 * i], scale, -m_ref));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[c / 2][8 * (c % 2) + 2 * i + 1], scale, -m_ref));
+        hi[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+        const float r0 = p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u), r1 = p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
+        lo[i] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
+        l_run += p0 + p1;
+      }
+      const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+      const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      bf16x8_t v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vt + v_at[0][e] + c * 16 * CPT * 2);
+        const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vt + v_at[1][e] + c * 16 * CPT * 2);
+        v[e] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[e], ph, acc[e], 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[e], pl, acc[e], 0, 0, 0);
+    }
+  };
+  // Tile i is in LDS half i % 2.
   const auto turn = [&](int i, auto parity) __attribute__((always_inline)) {
-    constexpr int kNow = decltype(parity)::value, kNext = kNow ^ 1, kSet = kNext % SETS;
+    constexpr int kNow = decltype(parity)::value, kNext = kNow ^ 1;
     __syncthreads();  // this tile is in LDS, and nobody reads the other half any more
-    stage(number(i + 1), kNext, kr[kSet], vr[kSet]);
-    fetch(number(i + 1 + SETS), kr[kSet], vr[kSet]);
-    lookup(number(i + 2 + SETS));
-    if (works && number(i) < tiles) compute(number(i), kNow);
+    const bool real = works && number(i) < tiles;
+    f32x16_t x[2];
+    if (real) logits(kNow, x);
+    stage(number(i + 1), kNext);
+    fetch(number(i + 2));
+    lookup(number(i + 3));
+    if (real) values(number(i), kNow, x);
   };
   for (int i = 0; number(i) < tiles; i += 2) {  // (always both: on a way out between them the loads that are waited for next would be the last)
     turn(i, Parity<0>{});
     turn(i + 1, Parity<1>{});
   }
 
-  // ---- every wave has its rows' whole states: lane (h, n) rows m = 8*(i/4) + 4*h + i%4 of C, elements m*E + e of query n ------------
+  // ---- every wave has its rows' whole states: lane (h, n) rows 8*(i/4) + 4*h + i%4 of C, elements 32*e + row of query n ---------------
   if (r >= rows) return;
   const float l = halves_sum(l_run);
   if (splits == 1) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    uint32_t* out = static_cast<uint32_t*>(p.out) + (((int64_t)s * p.drafts + draft) * num_q_heads + hk * group + head) * (D / 2);
+    uint16_t* out = static_cast<uint16_t*>(p.out) + (((int64_t)s * p.drafts + draft) * num_q_heads + hk * group + head) * D;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int m = 8 * (i / 4) + 4 * h + i % 4;
-      uint32_t w[E / 2];
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int e = 0; e < E; e += 2)
-        w[e / 2] = (uint32_t)f32_to_bf16(acc[e][i] * inv) | ((uint32_t)f32_to_bf16(acc[e + 1][i] * inv) << 16);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) out[m * (E / 2) + e] = w[e];
-    }
+      for (int i = 0; i < 16; i += 2) store_pair<bf16_t>(out, (32 * e + 8 * (i / 4) + 4 * h + i % 4) / 2, acc[e][i] * inv, acc[e][i + 1] * inv);
   } else {
     float* record = p.partials + (((int64_t)at.row * splits + split) * (p.drafts * group) + r) * (D + 2);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int m = 8 * (i / 4) + 4 * h + i % 4;
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(record + m * E + e) = make_float2(acc[e][i], acc[e + 1][i]);
-    }
+      for (int i = 0; i < 16; i += 2)
+        *reinterpret_cast<float2*>(record + 32 * e + 8 * (i / 4) + 4 * h + i % 4) = make_float2(acc[e][i], acc[e][i + 1]);
     if (h == 0) *reinterpret_cast<float2*>(record + D) = make_float2(m_run, l);
   }
 }
 
-template <int D>
-hipError_t launch_wide(const RowsArgs& a, RowsParams p, hipStream_t stream) {
-  dim3 blocks;
-  if (!rows_grid(a, a.tile_rows, &p, &blocks)) return hipErrorInvalidValue;
-  if (a.tile_rows == 64)
-    hipLaunchKernelGGL((tree_wide_kernel<D, 2>), blocks, dim3(2 * kWave), 0, stream, p);
-  else if (a.tile_rows == 128)
-    hipLaunchKernelGGL((tree_wide_kernel<D, 4>), blocks, dim3(4 * kWave), 0, stream, p);
-  else if (a.tile_rows == 256)
-    hipLaunchKernelGGL((tree_wide_kernel<D, 8>), blocks, dim3(8 * kWave), 0, stream, p);
-  else
-    return hipErrorInvalidValue;
-  return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_tree_wide(const RowsArgs& a, const RowsParams& p, hipStream_t stream) {
-  return a.head_dim == 64 ? launch_wide<64>(a, p, stream) : launch_wide<128>(a, p, stream);
+hipError_t launch_tree_wide(const RowsArgs& a, RowsParams p, hipStream_t stream) {
+  dim3 blocks;
+  if (!rows_grid(a, kWideRows, &p, &blocks)) return hipErrorInvalidValue;
+  if (a.head_dim == 64)
+    hipLaunchKernelGGL((tree_wide_kernel<64>), blocks, dim3(NT), 0, stream, p);
+  else
+    hipLaunchKernelGGL((tree_wide_kernel<128>), blocks, dim3(NT), 0, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace pe
