@@ -81,18 +81,20 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParam
   const int split = WEIGHTS || tiles == 1 ? at.split : at.split / tiles, tile = at.split - split * tiles;
   const bool shared = p.max_blocks < 0;
   const int max_blocks = shared ? -p.max_blocks : p.max_blocks;
-  const int32_t* bt = p.block_table + (int64_t)(shared ? s : at.row) * max_blocks;
+  // (read only while the launch runs: scalar loads, also behind a barrier or a store)
+  const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(p.block_table + (int64_t)(shared ? s : at.row) * max_blocks));
 
   // Step k of this wave: its round and the first token in it.
   const auto round_of = [&](int k) { return split + k / PER * splits; };
   const auto inside = [&](int k) { return k % PER * (kWaves * STEP) + wave * STEP; };
   // Pages of its parts (scalar loads; clamped to the table row, nothing here depends on the row's length).
-  const auto lookup = [&](int k, int (&ids)[PARTS]) {
+  const auto lookup = [&](int k, int (&ids)[PARTS]) __attribute__((always_inline)) {
     const int64_t tok = (int64_t)round_of(k) * kRoundTokens + inside(k);
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) {
       const int64_t j = (tok + part * 16) >> log2_block;
-      ids[part] = __builtin_amdgcn_readfirstlane(bt[j < max_blocks ? (int)j : max_blocks - 1]);
+      ids[part] = table[j < max_blocks ? (int)j : max_blocks - 1];
     }
   };
   int ids[PARTS], ids_next[PARTS];
@@ -108,28 +110,28 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParam
   uint32_t vb[PARTS][4][VD];
   const uint32_t token_bytes = (uint32_t)(shared ? p.num_kv_heads : 1) * (D * (uint32_t)sizeof(T));   // of a page
   const uint32_t draft_bytes = (uint32_t)p.num_kv_heads * (D * (uint32_t)sizeof(T));
-  const auto load = [&](int k, const int (&id)[PARTS], bool keys) {
+  // (the drafts' places as distances from the pools': a choice between two arguments would load the chosen one every time)
+  const int64_t k_far = WEIGHTS ? 0 : static_cast<const char*>(p.k_draft) - static_cast<const char*>(p.k_pool);
+  const int64_t v_far = WEIGHTS ? 0 : static_cast<const char*>(p.v_draft) - static_cast<const char*>(p.v_pool);
+  const auto load = [&](int k, const int (&id)[PARTS], bool keys) __attribute__((always_inline)) {
     const int round = round_of(k);
     const bool pool = WEIGHTS || round < cached;
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) {
       int tok = inside(k) + part * 16;   // of the round; what is no token reads one that is
-      const char* base;
-      uint32_t stride, last = 15u;
-      if (pool) {
-        const bool in = round < cached;  // (a part behind the row's end lies in its table row, or is replaced)
-        const int page = id[part] < 0 || !in ? 0 : id[part];
-        const int slot = (int)(((int64_t)round * kRoundTokens + tok) & ((1 << log2_block) - 1));
-        stride = token_bytes;
-        base = static_cast<const char*>(keys ? p.k_pool : p.v_pool) + (((int64_t)page << log2_block) + slot) * token_bytes +
-               (shared ? hk * (D * (int)sizeof(T)) : 0);
-      } else {
+      uint32_t stride = token_bytes, last = 15u;
+      const bool in = round < cached;  // (a part behind the row's end lies in its table row, or is replaced)
+      const int page = id[part] < 0 || !in ? 0 : id[part];
+      const int slot = (int)(((int64_t)round * kRoundTokens + tok) & ((1 << log2_block) - 1));
+      int64_t from = (((int64_t)page << log2_block) + slot) * token_bytes + (shared ? hk * (D * (int)sizeof(T)) : 0);
+      if (!pool) {
         const int end = round == cached ? drafts : 1;
         tok = tok < end ? tok : 0;
         last = (uint32_t)(end - 1 - tok < 15 ? end - 1 - tok : 15);
         stride = draft_bytes;
-        base = static_cast<const char*>(keys ? p.k_draft : p.v_draft) + ((int64_t)s * p.drafts + tok) * draft_bytes + hk * (D * (int)sizeof(T));
+        from = ((int64_t)s * p.drafts + tok) * draft_bytes + hk * (D * (int)sizeof(T)) + (keys ? k_far : v_far);
       }
+      const char* base = static_cast<const char*>(keys ? p.k_pool : p.v_pool) + from;
       if (keys) {
         const uint32_t off = ((uint32_t)n < last ? (uint32_t)n : last) * stride + (uint32_t)g * 16u;
 #pragma unroll
@@ -427,39 +429,74 @@ __global__ __launch_bounds__(kThreads) void rows_merge_kernel(const RowsParams p
   merge_row<T, D>(p, row, r, most, shape_splits(p.shape), ((int64_t)s * p.drafts + draft) * (p.num_kv_heads * group) + hk * group + h, lane_id());
 }
 
-// The splits of a row and the weights of its pages, one workgroup a row.
+// The splits of a row and the weights of its pages, one workgroup a row.  A head's (m, l) of all splits are read at once, a split a lane, and
+// a thread's first page while they are.
+template <int M = 1>
+__device__ __forceinline__ float wave_max(float v) {
+  if constexpr (M == 16)
+    return rows_max(v);
+  else
+    return wave_max<M * 2>(fmaxf(v, lane_xor_f32<M>(v)));
+}
+template <int M = 1>
+__device__ __forceinline__ float wave_sum(float v) {
+  if constexpr (M == 16)
+    return rows_sum(v);
+  else
+    return wave_sum<M * 2>(v + lane_xor_f32<M>(v));
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void weights_merge_kernel(const RowsParams p) {
   __shared__ float factor[256][8];  // of a split and head: what turns its pages' sums into weights
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int group = shape_group(p.shape), splits = shape_splits(p.shape), log2_block = shape_log2_block(p.shape);
   const int row = (int)blockIdx.x, s = row / p.num_kv_heads;
   const bool shared = p.max_blocks < 0;
   const int max_blocks = shared ? -p.max_blocks : p.max_blocks;
   const int len = length_of(p, s, max_blocks, log2_block);
+  const int pages = (int)(((int64_t)len + (1 << log2_block) - 1) >> log2_block);
+  const int64_t row_at = (int64_t)row * max_blocks;
+  const auto sums_of = [&](int j, float (&sums)[8]) {
+#pragma unroll
+    for (int h = 0; h < 8; ++h) sums[h] = h < group && j < pages ? p.page_sums[(row_at + j) * group + h] : 0.f;
+  };
+  float sums[8];
+  sums_of((int)threadIdx.x, sums);
   for (int h = wave; h < group; h += kWaves) {
-    merge_row<T, D>(p, row, h, group, splits, (int64_t)row * group + h, lane_id());
     const float* ml = p.partials + ((int64_t)row * splits * group + h) * (D + 2) + D;
     const int64_t stride = (int64_t)group * (D + 2);
-    float m = kNegInf;
-    for (int i = 0; i < splits; ++i) m = fmaxf(m, ml[i * stride]);
+    float2 of[4];
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int split = i * kWave + lane;
+      of[i] = split < splits ? *reinterpret_cast<const float2*>(ml + split * stride) : make_float2(kNegInf, 0.f);
+      m = fmaxf(m, of[i].x);
+    }
+    merge_row<T, D>(p, row, h, group, splits, (int64_t)row * group + h, lane);
+    m = wave_max(m);
     const float ms = m == kNegInf ? 0.f : m;
-    float l = 0.f;
-    for (int i = 0; i < splits; ++i) l = fmaf(ml[i * stride + 1], __builtin_amdgcn_exp2f(ml[i * stride] - ms), l);
-    for (int i = lane_id(); i < splits; i += kWave) factor[i][h] = l > 0.f ? __builtin_amdgcn_exp2f(ml[i * stride] - ms) / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l = fmaf(of[i].y, __builtin_amdgcn_exp2f(of[i].x - ms), l);
+    l = wave_sum(l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i * kWave + lane < splits) factor[i * kWave + lane][h] = l > 0.f ? __builtin_amdgcn_exp2f(of[i].x - ms) / l : 0.f;
   }
   __syncthreads();
-  const int pages = (int)(((int64_t)len + (1 << log2_block) - 1) >> log2_block);
   for (int j = (int)threadIdx.x; j < max_blocks; j += kThreads) {
-    const int64_t at = (int64_t)row * max_blocks + j;
+    if (j != (int)threadIdx.x) sums_of(j, sums);
     if (j >= pages) {
-      p.weights_out[at] = __builtin_inff();
+      p.weights_out[row_at + j] = __builtin_inff();
       continue;
     }
     const int split = (int)((((int64_t)j << log2_block) / kRoundTokens) % splits);
     float got = 0.f;
-    for (int h = 0; h < group; ++h) got = fmaf(p.page_sums[at * group + h], factor[split][h], got);
-    put_weight(p, at, got);
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (h < group) got = fmaf(sums[h], factor[split][h], got);
+    put_weight(p, row_at + j, got);
   }
 }
 
