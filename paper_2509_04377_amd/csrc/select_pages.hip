@@ -32,12 +32,17 @@ __global__ __launch_bounds__(kWaves * kWave) void page_bounds_kernel(const uint4
   int j = (int)(unit / (uint32_t)chunks);
   const int c = (int)(unit - (uint32_t)j * (uint32_t)chunks);
   const int len = seq_lens[(uint32_t)row / (uint32_t)rows_per_seq];
-  int full = len > 0 ? len >> log2_block : 0;
-  full = full < max_blocks ? full : max_blocks;
   if (j >= per_row) return;
-  if (recent) j += full - per_row;
-  if (j < 0 || j >= full) return;
-  const int page = block_table[row * max_blocks + j];
+  int page;
+  if (recent) {
+    const int full = len > 0 ? len >> log2_block : 0;
+    j += (full < max_blocks ? full : max_blocks) - per_row;
+    if (j < 0) return;
+    page = block_table[row * max_blocks + j];
+  } else {  // (the length and the page travel together)
+    page = block_table[row * max_blocks + j];
+    if (len >> log2_block <= j) return;
+  }
   if (page < 0) return;
   const uint4* from = k_pool + (((int64_t)page << log2_block) * chunks + c);
   float lo[EPL], hi[EPL];
@@ -70,27 +75,30 @@ __global__ __launch_bounds__(kWaves * kWave) void page_bounds_kernel(const uint4
 }
 
 // ---- scores --------------------------------------------------------------------------------------------------------------
-// A wave scores 16 * 64 / LPB pages at a time: the 2 D bounds of a page and head are LPB lanes' 16 bytes, lo in the lower half of them and hi
-// in the upper.  Sixteen loads are in flight; their sums meet in a reduce-scatter.
-template <typename T, int D>
+// A wave scores NL * 64 / LPB pages at a time: the 2 D bounds of a page and head are LPB lanes' 16 bytes, lo in the lower half of them and hi
+// in the upper.  NL loads are in flight; their sums meet in a reduce-scatter.
+template <typename T, int D, int NL = 16>
 struct Scorer {
-  static constexpr int EPL = Elem<T>::kPerVec, LPB = 2 * D / EPL, PPL = kWave / LPB, NL = 16, kPages = NL * PPL;
+  static constexpr int EPL = Elem<T>::kPerVec, LPB = 2 * D / EPL, PPL = kWave / LPB, kPages = NL * PPL;
 
   // The page (behind `base`) whose score the lane is left with, if it is left with one.
-  static __device__ __forceinline__ int page_of(int lane) { return bit_reverse<4>(lane & 15) * PPL + lane / LPB; }
+  static __device__ __forceinline__ int page_of(int lane) { return bit_reverse<ilog2(NL)>(lane & (NL - 1)) * PPL + lane / LPB; }
   static __device__ __forceinline__ bool has_page(int lane) { return lane % LPB < NL; }
-
-  // Scores of pages base .. base + kPages - 1 (of n), over the heads head, head + step, ... of the row's `heads` (first of them: q_head).
-  static __device__ __forceinline__ double score(const uint4* q, const uint4* bounds, const int32_t* bt, int64_t q_head, int group, int heads,
-                                                 int head, int step, int base, int n, int lane) {
+  // Places of a lane's part of its pages' bounds (an entry that is none is replaced by page 0: its score goes nowhere).
+  static __device__ __forceinline__ void look_up(const int32_t* bt, int base, int last, int heads, int lane, int64_t (&at)[NL]) {
     const int u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
-    int64_t at[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int j = base + i * PPL + lane / LPB;
-      const int page = bt[j < n ? j : n - 1];
+      const int page = bt[j < last ? j : last];
       at[i] = ((int64_t)(page < 0 ? 0 : page) * 2 + up) * heads * (LPB / 2) + v;
     }
+  }
+
+  // Scores of those pages, over the heads head, head + step, ... of the row's `heads` (first of them: q_head).
+  static __device__ __forceinline__ double score(const uint4* q, const uint4* bounds, const int64_t (&at)[NL], int64_t q_head, int group, int heads,
+                                                 int head, int step, int lane) {
+    const int u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
     double sum[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) sum[i] = 0.0;
@@ -145,20 +153,22 @@ __global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t in = blockIdx.x / (uint32_t)parts;
   const int part = (int)(blockIdx.x - in * (uint32_t)parts);
+  const int base = (heads > 1 ? part : part * kWaves + wave) * SC::kPages;
+  if (base >= max_blocks) return;
+  int64_t at[16];
+  SC::look_up(block_table + (first_row + in) * max_blocks, base, max_blocks - 1, heads, lane, at);  // (travels together with the length)
   const Row r = row_at(first_row + in, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int n = r.all - 1;  // candidates
-  const int base = (heads > 1 ? part : part * kWaves + wave) * SC::kPages;
   if (n < pages || base >= n) return;  // (with n + 1 <= pages every page is taken; several heads: the same in all waves)
-  const int32_t* bt = block_table + r.row * max_blocks;
   const int j = base + SC::page_of(lane);
   float* to = scores + r.row * max_blocks + j;
   const bool mine = SC::has_page(lane) && j < n;
   if (heads == 1) {
-    const double total = SC::score(q, bounds, bt, r.row, group, 1, 0, 1, base, n, lane);
+    const double total = SC::score(q, bounds, at, r.row, group, 1, 0, 1, lane);
     if (mine) *to = (float)total;
     return;
   }
-  of_heads[wave][lane] = SC::score(q, bounds, bt, r.row * heads, group, heads, wave, kWaves, base, n, lane);
+  of_heads[wave][lane] = SC::score(q, bounds, at, r.row * heads, group, heads, wave, kWaves, lane);
   __syncthreads();
   if (wave != 0 || !mine) return;
   double total = of_heads[0][lane];
@@ -178,22 +188,32 @@ __device__ __forceinline__ uint32_t order_of(float f) {
   const uint32_t b = __float_as_uint(f + 0.f);  // (-0 is 0)
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-template <int M = 1>
-__device__ __forceinline__ void least_and_most(uint32_t& lo, uint32_t& hi) {
-  if constexpr (M < kWave) {
-    const uint32_t a = (uint32_t)lane_xor_i32<M>((int)lo), b = (uint32_t)lane_xor_i32<M>((int)hi);
-    lo = a < lo ? a : lo;
-    hi = b > hi ? b : hi;
-    least_and_most<M * 2>(lo, hi);
-  }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+// Over the lanes of a wave, in every lane.
+template <typename F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t v, F f) {
+  v = f(v, dpp_u32<0xB1>(v));    // quad_perm [1,0,3,2]
+  v = f(v, dpp_u32<0x4E>(v));    // quad_perm [2,3,0,1]
+  v = f(v, dpp_u32<0x124>(v));   // row_ror:4
+  v = f(v, dpp_u32<0x128>(v));   // row_ror:8
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(r[0], r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(h[0], h[1]);
 }
 
 template <int WAVES>
 struct SelectState {
-  alignas(16) uint32_t count[2][kParts];
-  uint32_t lo[WAVES], hi[WAVES];
+  alignas(16) uint32_t count[2][kParts];  // part p at place_of(p)
+  alignas(16) uint32_t lo[WAVES], hi[WAVES];
   int above[WAVES], equal[WAVES];
 };
+
+// Lane l has the parts from 1023 - 16 l down, in four reads that its neighbours' lie beside.
+__device__ __forceinline__ uint32_t place_of(uint32_t part) { return (part & 12u) << 6 | (63u - (part >> 4)) << 2 | (part & 3u); }
 
 // Of n scores the `need` < n highest (of equal ones the first), in their order: table entries and indices.
 template <int WAVES>
@@ -219,7 +239,8 @@ __device__ __forceinline__ void select_row(const float* sc, int n, int need, con
       lo = k < lo ? k : lo;
       hi = k > hi ? k : hi;
     }
-  least_and_most(lo, hi);
+  lo = over_wave(lo, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+  hi = over_wave(hi, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
   if (lane == 0) {
     sm.lo[wave] = lo;
     sm.hi[wave] = hi;
@@ -239,7 +260,7 @@ __device__ __forceinline__ void select_row(const float* sc, int n, int need, con
     const uint32_t range = hi - lo;
     const int bits = 32 - __builtin_clz(range), shift = bits > 10 ? bits - 10 : 0;
     const auto add = [&](uint32_t k) {
-      if (k - lo <= range) atomicAdd(&count[(k - lo) >> shift], 1u);
+      if (k - lo <= range) atomicAdd(&count[place_of((k - lo) >> shift)], 1u);
     };
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
@@ -247,11 +268,11 @@ __device__ __forceinline__ void select_row(const float* sc, int n, int need, con
     for (int i = kHeld; i < each; ++i)
       if (at(i) < n) add(key(i));
     __syncthreads();
-    // lane l has the parts from 1023 - 16 l down; every wave finds the same one
+    // every wave finds the same part
     uint32_t part[16], sum = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint4 c = *reinterpret_cast<const uint4*>(&count[kParts - 16 * (lane + 1) + 4 * i]);
+      const uint4 c = *reinterpret_cast<const uint4*>(&count[i * 256 + lane * 4]);
       part[4 * i] = c.x, part[4 * i + 1] = c.y, part[4 * i + 2] = c.z, part[4 * i + 3] = c.w;
       sum += (c.x + c.y) + (c.z + c.w);
     }
@@ -365,7 +386,7 @@ __global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4
                                                                      const int32_t* seq_lens, int32_t* table_out, int32_t* lens_out,
                                                                      int32_t* idx_out, int rows_per_seq, int heads, int group, int log2_block,
                                                                      int max_blocks, int pages, int64_t first_row) {
-  using SC = Scorer<T, D>;
+  using SC = Scorer<T, D, 8>;
   __shared__ SelectState<WAVES> sm;
   extern __shared__ float sc[];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -375,7 +396,9 @@ __global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4
   if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
   const int n = r.all - 1;
   for (int base = wave * SC::kPages; base < n; base += WAVES * SC::kPages) {
-    const double total = SC::score(q, bounds, bt, r.row * heads, group, heads, 0, 1, base, n, lane);
+    int64_t at[8];
+    SC::look_up(bt, base, n - 1, heads, lane, at);
+    const double total = SC::score(q, bounds, at, r.row * heads, group, heads, 0, 1, lane);
     const int j = base + SC::page_of(lane);
     if (SC::has_page(lane) && j < n) sc[j] = (float)total;
   }
