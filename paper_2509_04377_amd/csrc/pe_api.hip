@@ -225,7 +225,7 @@ void tag_attention(const pe_cache_desc* d, pe::DecodeArgs* a) {
 
 extern "C" {
 
-int pe_version(void) { return 300; }  // 0.3.0: per-descriptor launch shape replaces the process-wide options
+int pe_version(void) { return 400; }  // 0.4.0: trees of drafts, selected pages, page weights
 
 const char* pe_status_string(int status) {
   switch (status) {

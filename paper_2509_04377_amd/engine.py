@@ -11,8 +11,12 @@ Multi-layer driver: all layers' pages live in one physical pool; the block table
 dimension").  Scoring, eviction and the prefill prune see the folded table in ONE launch each; append and
 attention are launched per layer, in layer order, because in a model layer l+1's query depends on layer l's
 output.
+
+Beside the paper's step there are three more: a verification of drafted tokens (tree_decode, then accept_path, which scores and
+evicts between the accepted tokens where single steps would have), attention over the pages with the highest bounds
+(select_pages) and eviction by the attention that pages got (evict_by_attention).
 """
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import List, Optional
 
 import torch
@@ -71,6 +75,8 @@ class PagedCache:
     host_scored: list = None       # per sequence: full pages whose score is in `scores` (host bookkeeping)
     evict_opts: pe.pe_evict_opts = None  # eviction variant (policy, protected pages, shared heads); None = Alg. 3
     fused_evict: bool = False  # score + evict of a trigger step in one pass over the pages (pe_score_evict)
+    selection: "Selection" = None  # attend to selected pages only (select_pages)
+    attention: "Attention" = None  # `scores` are the attention that pages got (evict_by_attention)
 
     @staticmethod
     def create(dtype, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device="cuda",
@@ -119,6 +125,10 @@ class PagedCache:
     def set_host_lens(self, prompt_lens):
         """Tell the host mirror what the prune was given: cached length = min(L, C)."""
         self.host_lens = [min(int(L), self.budget) for L in prompt_lens]
+        if self.selection is not None:
+            self.selection.seen = None
+        if self.attention is not None:
+            self.attention.started = False
 
     def triggers(self) -> List[bool]:
         return triggers(self.host_lens, self.desc.block_size, self.budget)
@@ -140,17 +150,33 @@ class PagedCache:
         """One decode iteration of one layer (Alg. 3): score + evict when some sequence's newest page has
         filled at budget, append the new token, attend.  Which steps trigger follows from the lengths
         alone, so the host decides it without reading anything back."""
-        B = self.desc.block_size
         trig = self.triggers()
+        if self.selection is not None:
+            self.bound_pages()
         if any(trig):
+            if self.attention is not None and not self.attention.started:   # nothing seen yet: this step's queries look first
+                self.paged_decode_weights(q, out, softmax_scale)
             self.score_and_evict()
-            self.host_lens = [n - B if t else n for n, t in zip(self.host_lens, trig)]
-        if fused:
+            self.evicted(trig)
+        self.append_and_attend(new_k, new_v, q, out, softmax_scale, fused)
+        self.host_lens = [n + 1 for n in self.host_lens]
+
+    def evicted(self, which):
+        """Bookkeeping behind an eviction of these sequences."""
+        self.host_lens = [n - self.desc.block_size if t else n for n, t in zip(self.host_lens, which)]
+        if self.selection is not None and self.selection.seen is not None:
+            self.selection.seen = [n - t for n, t in zip(self.selection.seen, which)]
+
+    def append_and_attend(self, new_k, new_v, q, out, softmax_scale=None, fused=True):
+        """What a step launches behind an eviction.  Selected pages and attention weights have no fused form."""
+        if self.selection is not None or self.attention is not None:
+            self.append_kv(new_k, new_v)
+            (self.selected_decode if self.selection is not None else self.paged_decode_weights)(q, out, softmax_scale)
+        elif fused:
             self.append_paged_decode(new_k, new_v, q, out, softmax_scale)
         else:
             self.append_kv(new_k, new_v)
             self.paged_decode(q, out, softmax_scale)
-        self.host_lens = [n + 1 for n in self.host_lens]
 
     def score_blocks(self):
         _launch(pe.pe_score_blocks, self.desc, self.k_pool, self.v_pool, self.block_table, self.seq_lens, self.scores)
@@ -167,6 +193,14 @@ class PagedCache:
         """Score + evict of a trigger step.  With cached scores only the pages filled since the last call are
         scored (all of them the first time) and the eviction keeps the score rows aligned with the table."""
         B = self.desc.block_size
+        if self.attention is not None:   # the scores are there; the newest page, which has had no time to be attended to, stays
+            if not self.attention.started:
+                raise RuntimeError("no attention step before the first eviction: nothing to choose a page by")
+            o = self.evict_opts or pe.pe_evict_opts(pe.PE_POLICY_LOWEST_SCORE, 0, 1, 0, 0)
+            opts = pe.pe_evict_opts(o.policy, o.protect_first, o.protect_last, o.share_heads, 1)
+            _launch(pe.pe_evict_blocks_ex, self.desc, opts, self.scores, self.block_table, self.seq_lens, self.budget,
+                    self.evicted_logical, self.freed_phys)
+            return
         if self.evict_opts is not None:
             o = self.evict_opts
             opts = pe.pe_evict_opts(o.policy, o.protect_first, o.protect_last, o.share_heads, 0)
@@ -206,6 +240,152 @@ class PagedCache:
                 out, self.decode_ws)
 
 
+    # ---- verification of drafted tokens ----
+
+    def tree_decode(self, q, k_draft, v_draft, tree_mask, out, draft_lens=None, softmax_scale=None, workspace=None):
+        """Attention of q [S, T, Hq, D] over the cache and the drafts that tree_mask [S, T] names (int64 words); the cache is read only."""
+        if softmax_scale is None:
+            softmax_scale = float(self.desc.head_dim) ** -0.5
+        T = int(q.shape[1])
+        if workspace is None:
+            workspace = pe.alloc_workspace(pe.PE_OP_TREE_DECODE, self.desc, T, device=q.device)
+        _launch(pe.pe_tree_decode, self.desc, T, q, k_draft, v_draft, draft_lens, tree_mask, self.k_pool, self.v_pool,
+                self.block_table, self.seq_lens, softmax_scale, out, workspace)
+
+    def accept_path(self, k_draft, v_draft, path, path_lens, host_path_lens):
+        """Append the drafts path[s][:path_lens[s]] (path [S, P] and path_lens [S] int32 on the device, host_path_lens the latter's
+        values, at most P; every named draft exists).  The effect on the cache is that of as many single steps: before a token joins a
+        sequence whose newest page is full and which is at budget, a page of that sequence goes, and of no other: a sequence
+        whose path ends with a full page keeps its pages until it goes on."""
+        B = self.desc.block_size
+        left = [int(n) for n in host_path_lens]
+        if len(left) != len(self.host_lens) or min(left) < 0 or max(left) > path.shape[-1]:
+            raise ValueError("host_path_lens: one length per sequence, 0 to path.shape[-1]")
+        path_done = torch.zeros_like(path_lens)
+        while any(left):
+            trig = self.triggers()
+            now = [t and n > 0 for t, n in zip(trig, left)]
+            if any(now):
+                if now == trig:
+                    self.score_and_evict()
+                else:
+                    self._score_and_evict_of(now)
+                self.evicted(now)
+            _launch(pe.pe_append_path, self.desc, k_draft, v_draft, path, path_lens, path_done, self.k_pool, self.v_pool,
+                    self.block_table, self.seq_lens, self.freed_phys, self.spare, self.spare_used)
+            taken = [min(m, B - n % B) for n, m in zip(self.host_lens, left)]
+            self.host_lens = [n + t for n, t in zip(self.host_lens, taken)]
+            left = [m - t for m, t in zip(left, taken)]
+
+    def _score_and_evict_of(self, now):
+        """score_and_evict for some sequences only: a call for each run of neighbours."""
+        if self.cached_scores and self.host_scored is None and self.evict_opts is None and self.attention is None:
+            self.score_blocks()
+            self.host_scored = [n // self.desc.block_size for n in self.host_lens]
+        first = 0
+        while first < len(now):
+            end = first + 1
+            while end < len(now) and now[end] == now[first]:
+                end += 1
+            if now[first]:
+                part = self.rows(first, end)
+                part.score_and_evict()
+                if part.host_scored is not None:
+                    self.host_scored[first:end] = part.host_scored
+            first = end
+
+    def rows(self, first, end):
+        """The same cache's sequences first .. end - 1, as a cache (views; host_lens and host_scored are copies)."""
+        d, sl = self.desc, slice(first, end)
+        fields = {name: getattr(d, name) for name, _ in d._fields_}
+        views = {name: getattr(self, name)[sl] for name in ("block_table", "seq_lens", "spare", "spare_used", "freed_phys",
+                                                            "evicted_logical", "scores", "host_lens")}
+        return replace(self, desc=pe.pe_cache_desc(**{**fields, "num_seqs": end - first}), **views, seq_lens_alt=None, selection=None,
+                       host_scored=None if self.host_scored is None else self.host_scored[sl])
+
+    # ---- attention over selected pages ----
+
+    def select_pages(self, num_pages, bounds=None):
+        """From now on a step attends to the num_pages pages with the highest bounds only (the newest among them); 0: to all.
+        bounds: as pe_page_bounds keeps them (several layers of one pool share them)."""
+        if num_pages and self.attention is not None:
+            raise ValueError("attention weights are kept over all pages, not over selected ones")
+        self.selection = Selection.create(self, int(num_pages), bounds) if num_pages else None
+
+    def bound_pages(self):
+        """Bounds of the pages that have filled since the last call (the first time: of all full ones).  Due before a selection that
+        has a newer page; a selection never asks for the newest page's."""
+        sel, B = self.selection, self.desc.block_size
+        recent = sel.recent(self.host_lens, B)
+        if recent != 0:
+            _launch(pe.pe_page_bounds, self.desc, self.k_pool, self.block_table, self.seq_lens, max(recent, 0), sel.bounds)
+        sel.seen = [n // B for n in self.host_lens]
+
+    def selected_decode(self, q, out, softmax_scale=None):
+        if softmax_scale is None:
+            softmax_scale = float(self.desc.head_dim) ** -0.5
+        sel = self.selection
+        _launch(pe.pe_select_pages, self.desc, q, sel.bounds, self.block_table, self.seq_lens, sel.num_pages, sel.table, sel.lens,
+                None, sel.select_ws)
+        _launch(pe.pe_paged_decode, sel.desc, q, self.k_pool, self.v_pool, sel.table, sel.lens, softmax_scale, out, sel.decode_ws)
+
+    # ---- eviction by the attention that pages got ----
+
+    def evict_by_attention(self, decay=1.0):
+        """From now on `scores` hold the attention weight of each page (decay: what is left of it a step later), and the page with
+        the least goes.  The choice, protected pages and shared heads are evict_opts'; without them the newest page is protected."""
+        if self.selection is not None:
+            raise ValueError("attention weights are kept over all pages, not over selected ones")
+        self.attention = Attention(float(decay), pe.alloc_workspace(pe.PE_OP_DECODE_WEIGHTS, self.desc, device=self.k_pool.device))
+
+    def paged_decode_weights(self, q, out, softmax_scale=None):
+        if softmax_scale is None:
+            softmax_scale = float(self.desc.head_dim) ** -0.5
+        att = self.attention
+        _launch(pe.pe_paged_decode_weights, self.desc, q, self.k_pool, self.v_pool, self.block_table, self.seq_lens, softmax_scale,
+                att.decay, self.scores if att.started else None, self.scores, out, att.workspace)
+        att.started = True
+
+
+@dataclass
+class Selection:
+    """What a step over selected pages keeps."""
+    num_pages: int
+    bounds: torch.Tensor       # [P, 2, D] (shared: [P, 2, Hk, D])
+    table: torch.Tensor        # [S, Hk, num_pages] int32 (shared: [S, num_pages])
+    lens: torch.Tensor         # [S] int32
+    desc: pe.pe_cache_desc     # of the cache with that table
+    select_ws: torch.Tensor
+    decode_ws: torch.Tensor
+    seen: list = None          # full pages per sequence at the last bound_pages; None before the first
+
+    @staticmethod
+    def create(cache, num_pages, bounds=None):
+        d, dev = cache.desc, cache.k_pool.device
+        desc = pe.pe_cache_desc(**{**{name: getattr(d, name) for name, _ in d._fields_}, "max_blocks": num_pages})
+        if bounds is None:
+            heads = (d.num_kv_heads,) if cache.shared else ()
+            bounds = torch.empty((d.num_phys_blocks, 2) + heads + (d.head_dim,), dtype=cache.k_pool.dtype, device=dev)
+        return Selection(num_pages, bounds, torch.empty(cache.block_table.shape[:-1] + (num_pages,), dtype=torch.int32, device=dev),
+                         torch.empty_like(cache.seq_lens), desc, pe.alloc_workspace(pe.PE_OP_SELECT_PAGES, d, device=dev),
+                         pe.alloc_workspace(pe.PE_OP_PAGED_DECODE, desc, device=dev))
+
+    def recent(self, lens, B):
+        """How many of the newest full pages may have no bounds; -1: all.  (An eviction takes one off both counts, so that it is one
+        too many where a page without bounds went.)"""
+        if self.seen is None:
+            return -1
+        return max([n // B - s for n, s in zip(lens, self.seen)] + [0])
+
+
+@dataclass
+class Attention:
+    """What a step that keeps attention weights needs beside the scores."""
+    decay: float
+    workspace: torch.Tensor
+    started: bool = False      # the scores hold weights
+
+
 class LayeredCache:
     def __init__(self, dtype, layers, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget,
                  device="cuda", shared=False, decode_opts=None):
@@ -242,6 +422,8 @@ class LayeredCache:
 
     def set_host_lens(self, prompt_lens):
         self.host_lens = [min(int(L), self.budget) for L in prompt_lens]
+        for c in [self.folded] + self.per_layer:
+            c.set_host_lens(list(prompt_lens) * (self.layers if c is self.folded else 1))
 
     def _triggers(self):
         return triggers(self.host_lens, self.B, self.budget)
@@ -249,13 +431,21 @@ class LayeredCache:
     def decode_step(self, new_k, new_v, q, out, softmax_scale: Optional[float] = None, layer_hook=None):
         """new_k, new_v [layers, S, Hk, D]; q, out [layers, S, Hq, D].  One decode iteration of all layers."""
         trig = self._triggers()
+        f = self.folded
+        f.host_lens = self.host_lens * self.layers
+        if f.selection is not None:
+            f.bound_pages()
         if any(trig):
-            self.folded.host_lens = self.host_lens * self.layers
-            self.folded.score_and_evict()
-            self.host_lens = [n - self.B if t else n for n, t in zip(self.host_lens, trig)]
-        if self.fused and self.native_layers:
+            if f.attention is not None and not f.attention.started:
+                for l, c in enumerate(self.per_layer):
+                    c.paged_decode_weights(q[l], out[l], softmax_scale)
+                f.attention.started = True
+            f.score_and_evict()
+            f.evicted(trig * self.layers)
+            self.host_lens = f.host_lens[:self.S]
+        fused = self.fused and f.selection is None and f.attention is None
+        if fused and self.native_layers:
             # one native call issues the fused append + attention launch of every layer, in layer order
-            f = self.folded
             if layer_hook is not None:
                 layer_hook(0, 0)
             _launch(pe.pe_append_paged_decode_layers, self.per_layer[0].desc, self.layers, new_k, new_v, q, f.k_pool, f.v_pool,
@@ -266,11 +456,11 @@ class LayeredCache:
                 layer_hook(self.layers - 1, 1)
             for c in self.per_layer:
                 c.seq_lens, c.seq_lens_alt = c.seq_lens_alt, c.seq_lens
-        for l, c in enumerate(self.per_layer if not (self.fused and self.native_layers) else ()):
-            if self.fused:
+        for l, c in enumerate(self.per_layer if not (fused and self.native_layers) else ()):
+            if fused or f.selection is not None or f.attention is not None:
                 if layer_hook is not None:
                     layer_hook(l, 0)
-                c.append_paged_decode(new_k[l], new_v[l], q[l], out[l], softmax_scale)
+                c.append_and_attend(new_k[l], new_v[l], q[l], out[l], softmax_scale)
             else:
                 c.append_kv(new_k[l], new_v[l])
                 if layer_hook is not None:
@@ -278,10 +468,39 @@ class LayeredCache:
                 c.paged_decode(q[l], out[l], softmax_scale)
             if layer_hook is not None:
                 layer_hook(l, 1)
-        if self.fused:   # every layer wrote its new lengths into the other array
-            self.folded.seq_lens, self.folded.seq_lens_alt = self.folded.seq_lens_alt, self.folded.seq_lens
+        if f.attention is not None:
+            f.attention.started = True
+        if fused:   # every layer wrote its new lengths into the other array
+            f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens
         self.host_lens = [n + 1 for n in self.host_lens]
         return any(trig)
+
+    def tree_decode_layer(self, layer, q, k_draft, v_draft, tree_mask, out, draft_lens=None, softmax_scale=None, workspace=None):
+        self.per_layer[layer].tree_decode(q, k_draft, v_draft, tree_mask, out, draft_lens, softmax_scale, workspace)
+
+    def accept_path(self, k_draft, v_draft, path, path_lens, host_path_lens):
+        """PagedCache.accept_path in every layer at once: k_draft, v_draft [layers, S, T, Hk, D]; path [S, P], path_lens [S]."""
+        f = self.folded
+        f.host_lens = self.host_lens * self.layers
+        f.accept_path(k_draft.flatten(0, 1), v_draft.flatten(0, 1), path.repeat(self.layers, 1), path_lens.repeat(self.layers),
+                      list(host_path_lens) * self.layers)
+        self.host_lens = f.host_lens[:self.S]
+
+    def select_pages(self, num_pages):
+        """PagedCache.select_pages in every layer; the pool's bounds are kept by one launch for all of them."""
+        self.folded.select_pages(num_pages)
+        one = None
+        if num_pages:   # launches are ordered on one stream: one set of tables and workspaces serves every layer
+            one = Selection.create(self.per_layer[0], int(num_pages), self.folded.selection.bounds)
+        for c in self.per_layer:
+            c.selection = one
+
+    def evict_by_attention(self, decay=1.0):
+        """PagedCache.evict_by_attention in every layer."""
+        self.folded.evict_by_attention(decay)
+        one = pe.alloc_workspace(pe.PE_OP_DECODE_WEIGHTS, self.per_layer[0].desc, device=self.device)
+        for c in self.per_layer:
+            c.attention = Attention(float(decay), one)
 
 
 class GraphedStepper:
@@ -306,7 +525,9 @@ class GraphedStepper:
                 recent = -1
             else:
                 recent = max(n // e.B - sc for n, sc in zip(e.host_lens * e.layers, f.host_scored))
-        return (f.seq_lens.data_ptr(), trig, e.fused, f.cached_scores, f.fused_evict, recent)
+        fresh = None if f.selection is None else (f.selection.num_pages, f.selection.recent(e.host_lens * e.layers, e.B))
+        seen = None if f.attention is None else f.attention.started
+        return (f.seq_lens.data_ptr(), trig, e.fused, f.cached_scores, f.fused_evict, recent, fresh, seen)
 
     def step(self) -> bool:
         key = self._key()
