@@ -84,24 +84,27 @@ struct Scorer {
   // The page (behind `base`) whose score the lane is left with, if it is left with one.
   static __device__ __forceinline__ int page_of(int lane) { return bit_reverse<ilog2(NL)>(lane & (NL - 1)) * PPL + lane / LPB; }
   static __device__ __forceinline__ bool has_page(int lane) { return lane % LPB < NL; }
-  // Places of a lane's part of its pages' bounds (an entry that is none is replaced by page 0: its score goes nowhere).
-  static __device__ __forceinline__ void look_up(const int32_t* bt, int base, int last, int heads, int lane, int64_t (&at)[NL]) {
-    const int u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
+  // The pages of a lane's parts, as the table has them up to entry `last`.
+  static __device__ __forceinline__ void look_up(const int32_t* bt, int base, int last, int lane, int32_t (&page)[NL]) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int j = base + i * PPL + lane / LPB;
-      const int page = bt[j < last ? j : last];
-      at[i] = ((int64_t)(page < 0 ? 0 : page) * 2 + up) * heads * (LPB / 2) + v;
+      page[i] = bt[j < last ? j : last];
     }
   }
 
-  // Scores of those pages, over the heads head, head + step, ... of the row's `heads` (first of them: q_head).
-  static __device__ __forceinline__ double score(const uint4* q, const uint4* bounds, const int64_t (&at)[NL], int64_t q_head, int group, int heads,
-                                                 int head, int step, int lane) {
+  // Scores of those of them that are candidates (below n), over the heads head, head + step, ... of the row's `heads` (first of them:
+  // q_head).  In the others' place page 0 is read: their scores go nowhere.
+  static __device__ __forceinline__ double score(const uint4* q, const uint4* bounds, const int32_t (&page)[NL], int base, int n, int64_t q_head,
+                                                 int group, int heads, int head, int step, int lane) {
     const int u = lane % LPB, up = u / (LPB / 2), v = u % (LPB / 2);
     double sum[NL];
+    int64_t at[NL];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) sum[i] = 0.0;
+    for (int i = 0; i < NL; ++i) {
+      sum[i] = 0.0;
+      at[i] = ((int64_t)(base + i * PPL + lane / LPB < n && page[i] > 0 ? page[i] : 0) * 2 + up) * heads * (LPB / 2) + v;
+    }
     for (int h = head; h < heads; h += step) {
       uint4 b[NL];
 #pragma unroll
@@ -155,8 +158,8 @@ __global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4
   const int part = (int)(blockIdx.x - in * (uint32_t)parts);
   const int base = (heads > 1 ? part : part * kWaves + wave) * SC::kPages;
   if (base >= max_blocks) return;
-  int64_t at[16];
-  SC::look_up(block_table + (first_row + in) * max_blocks, base, max_blocks - 1, heads, lane, at);  // (travels together with the length)
+  int32_t page[16];
+  SC::look_up(block_table + (first_row + in) * max_blocks, base, max_blocks - 1, lane, page);  // (they travel together with the length)
   const Row r = row_at(first_row + in, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int n = r.all - 1;  // candidates
   if (n < pages || base >= n) return;  // (with n + 1 <= pages every page is taken; several heads: the same in all waves)
@@ -164,11 +167,11 @@ __global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4
   float* to = scores + r.row * max_blocks + j;
   const bool mine = SC::has_page(lane) && j < n;
   if (heads == 1) {
-    const double total = SC::score(q, bounds, at, r.row, group, 1, 0, 1, lane);
+    const double total = SC::score(q, bounds, page, base, n, r.row, group, 1, 0, 1, lane);
     if (mine) *to = (float)total;
     return;
   }
-  of_heads[wave][lane] = SC::score(q, bounds, at, r.row * heads, group, heads, wave, kWaves, lane);
+  of_heads[wave][lane] = SC::score(q, bounds, page, base, n, r.row * heads, group, heads, wave, kWaves, lane);
   __syncthreads();
   if (wave != 0 || !mine) return;
   double total = of_heads[0][lane];
@@ -344,6 +347,59 @@ __device__ __forceinline__ void select_row(const float* sc, int n, int need, con
   for (int i = kHeld; i < each; ++i) put(i, key(i), at(i) < n ? bt[at(i)] : -1);
 }
 
+// The same of at most 64 * kHeld scores in LDS, by one wave and without a barrier: the smallest one that is taken by halving the range, a
+// ballot for every 64 scores and turn (about log2 n turns and a few more, as it ends where a half's count is right).
+__device__ __forceinline__ void select_short_row(const float* sc, int n, int need, const int32_t (&page)[kHeld], int32_t* to, int32_t* idx) {
+  const int lane = lane_id(), each = (n + kWave - 1) / kWave;
+  uint32_t held[kHeld], lo = ~0u, hi = 0u;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const bool in = i * kWave + lane < n;
+    held[i] = in ? order_of(sc[i * kWave + lane]) : 0u;
+    lo = in && held[i] < lo ? held[i] : lo;
+    hi = in && held[i] > hi ? held[i] : hi;
+  }
+  lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)over_wave(lo, [](uint32_t a, uint32_t b) { return a < b ? a : b; }));
+  hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)over_wave(hi, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+  const auto above = [&](uint32_t least) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) c += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(held[i] > least));
+    return c;
+  };
+  int ties = need;
+  while (lo != hi) {  // fewer than `need` are above hi, and `need` or more are lo or above
+    const uint32_t mid = lo + (hi - lo) / 2;
+    const int c = above(mid);
+    if (c == need) {
+      lo = mid;
+      break;
+    }
+    if (c > need)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  ties -= above(lo);
+  int pos = 0, equal = 0;  // taken, and equal ones met, in what lies before
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (i >= each) break;
+    const bool in = i * kWave + lane < n;
+    const uint64_t gt = __builtin_amdgcn_ballot_w64(in && held[i] > lo), eq = __builtin_amdgcn_ballot_w64(in && held[i] == lo);
+    const uint64_t below = (1ull << lane) - 1;
+    const int before = equal + (int)__builtin_popcountll(eq & below);
+    const uint64_t take = gt | __builtin_amdgcn_ballot_w64((eq >> lane & 1u) != 0 && before < ties);
+    if (take >> lane & 1u) {
+      const int at = pos + (int)__builtin_popcountll(take & below);
+      to[at] = page[i];
+      if (idx != nullptr) idx[at] = i * kWave + lane;
+    }
+    pos += (int)__builtin_popcountll(take);
+    equal += (int)__builtin_popcountll(eq);
+  }
+}
+
 // What of a row's outputs does not depend on scores; true if that is everything.
 template <int WAVES>
 __device__ __forceinline__ bool frame_row(const Row& r, const int32_t* bt, int32_t* to, int32_t* idx, int32_t* lens_out, bool first_head,
@@ -387,23 +443,27 @@ __global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4
                                                                      int32_t* idx_out, int rows_per_seq, int heads, int group, int log2_block,
                                                                      int max_blocks, int pages, int64_t first_row) {
   using SC = Scorer<T, D, 8>;
-  __shared__ SelectState<WAVES> sm;
-  extern __shared__ float sc[];
+  __shared__ float sc[kHeld * kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const Row r = row_at(first_row + blockIdx.x, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int32_t* bt = block_table + r.row * max_blocks;
   int32_t *to = table_out + r.row * pages, *idx = idx_out != nullptr ? idx_out + r.row * pages : nullptr;
   if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
   const int n = r.all - 1;
+  int32_t entry[kHeld];
+  if (wave == 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) entry[i] = i * kWave + lane < n ? bt[i * kWave + lane] : -1;
+  }
   for (int base = wave * SC::kPages; base < n; base += WAVES * SC::kPages) {
-    int64_t at[8];
-    SC::look_up(bt, base, n - 1, heads, lane, at);
-    const double total = SC::score(q, bounds, at, r.row * heads, group, heads, 0, 1, lane);
+    int32_t page[8];
+    SC::look_up(bt, base, n - 1, lane, page);
+    const double total = SC::score(q, bounds, page, base, n, r.row * heads, group, heads, 0, 1, lane);
     const int j = base + SC::page_of(lane);
     if (SC::has_page(lane) && j < n) sc[j] = (float)total;
   }
   __syncthreads();
-  select_row<WAVES>(sc, n, pages - 1, bt, to, idx, sm);
+  if (wave == 0) select_short_row(sc, n, pages - 1, entry, to, idx);
 }
 
 template <typename T>
@@ -443,10 +503,10 @@ hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.num_seqs * rows_per_seq;
   const int group = a.num_q_heads / a.num_kv_heads;
   constexpr int64_t kRows = 1 << 21;
-  if ((int64_t)a.max_blocks * heads * 2 * D * (int64_t)sizeof(T) <= select_one_launch_bytes()) {
+  if ((int64_t)a.max_blocks * heads * 2 * D * (int64_t)sizeof(T) <= select_one_launch_bytes() && a.max_blocks <= kHeld * kWave) {
     for (int64_t row = 0; row < rows; row += kRows)
       hipLaunchKernelGGL((score_select_kernel<T, D, 8>), dim3((unsigned)(rows - row < kRows ? rows - row : kRows)), dim3(8 * kWave),
-                         (size_t)a.max_blocks * sizeof(float), stream, (const uint4*)a.q, (const uint4*)a.bounds, a.block_table, a.seq_lens,
+                         0, stream, (const uint4*)a.q, (const uint4*)a.bounds, a.block_table, a.seq_lens,
                          a.table_out, a.lens_out, a.idx_out, rows_per_seq, heads, group, log2_block, a.max_blocks, a.pages, row);
     return hipGetLastError();
   }
