@@ -35,9 +35,6 @@ struct SelectArgs {
 };
 hipError_t launch_select_pages(const SelectArgs& a, hipStream_t stream);
 
-// Scores and selection in one launch: up to so many bytes of bounds in a table row (a workgroup reads a row by itself then).
-inline int64_t select_one_launch_bytes() { return 128 << 10; }
-
 // One score for every table entry.
 inline size_t select_workspace_bytes(const pe_cache_desc* d) {
   const int64_t rows = d->layout == PE_LAYOUT_SHARED ? d->num_seqs : (int64_t)d->num_seqs * d->num_kv_heads;

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4
 // range, and there in one of 1024 parts of that, and so on: a count of each part in LDS, then the part in which the sum from above
 // reaches what is needed.  (Scores of about the same size differ in their low bits alone: parts of their range hold about as many each,
 // digits of the numbers would not.)  A wave holds consecutive pages, so that one exchange tells where its first one goes.
-constexpr int kParts = 1024, kHeld = 8;
+constexpr int kParts = 1024, kHeld = 8, kShort = kHeld * kWave;
 
 __device__ __forceinline__ uint32_t order_of(float f) {
   const uint32_t b = __float_as_uint(f + 0.f);  // (-0 is 0)
@@ -347,7 +347,13 @@ __device__ __forceinline__ void select_row(const float* sc, int n, int need, con
   for (int i = kHeld; i < each; ++i) put(i, key(i), at(i) < n ? bt[at(i)] : -1);
 }
 
-// The same of at most 64 * kHeld scores in LDS, by one wave and without a barrier: the smallest one that is taken by halving the range, a
+__device__ __forceinline__ void entries_of(const int32_t* bt, int n, int32_t (&entry)[kHeld]) {
+  const int lane = lane_id();
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) entry[i] = i * kWave + lane < n ? bt[i * kWave + lane] : -1;
+}
+
+// The same of at most kShort scores, by one wave and without a barrier: the smallest one that is taken by halving the range, a
 // ballot for every 64 scores and turn (about log2 n turns and a few more, as it ends where a half's count is right).
 __device__ __forceinline__ void select_short_row(const float* sc, int n, int need, const int32_t (&page)[kHeld], int32_t* to, int32_t* idx) {
   const int lane = lane_id(), each = (n + kWave - 1) / kWave;
@@ -428,22 +434,33 @@ template <int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void select_pages_kernel(const float* scores, const int32_t* block_table, const int32_t* seq_lens,
                                                                      int32_t* table_out, int32_t* lens_out, int32_t* idx_out, int rows_per_seq,
                                                                      int log2_block, int max_blocks, int pages, int64_t first_row) {
-  __shared__ SelectState<WAVES> sm;
   const Row r = row_at(first_row + blockIdx.x, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int32_t* bt = block_table + r.row * max_blocks;
   int32_t *to = table_out + r.row * pages, *idx = idx_out != nullptr ? idx_out + r.row * pages : nullptr;
   if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
-  select_row<WAVES>(scores + r.row * max_blocks, r.all - 1, pages - 1, bt, to, idx, sm);
+  if constexpr (WAVES == 1) {
+    int32_t entry[kHeld];
+    entries_of(bt, r.all - 1, entry);
+    select_short_row(scores + r.row * max_blocks, r.all - 1, pages - 1, entry, to, idx);
+  } else {
+    __shared__ SelectState<WAVES> sm;
+    select_row<WAVES>(scores + r.row * max_blocks, r.all - 1, pages - 1, bt, to, idx, sm);
+  }
 }
 
-// Scores and selection in one launch, for rows that one workgroup reads soon enough.
+// Scores and selection in one launch, for rows of one head that one workgroup reads soon enough.  (bf16, 32 query heads over 8, one launch /
+// two: 1 sequence with 16 KiB of bounds a row 5.6 / 8.4 us, with 64 KiB 7.1 / 9.3, with 128 KiB 9.7 / 9.9, with 256 KiB 16.1 / 10.4; 32
+// sequences 6.4 / 9.4, 9.3 / 12.4, 13.5 / 16.4 and 22.6 / 24.8.  Eight heads a decision, 64 pages of 128 KiB: 14.1 / 10.5, as a wave would
+// have to take one head after the other.)
+constexpr int64_t kOneLaunchBytes = 128 << 10;
+
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4* q, const uint4* bounds, const int32_t* block_table,
                                                                      const int32_t* seq_lens, int32_t* table_out, int32_t* lens_out,
-                                                                     int32_t* idx_out, int rows_per_seq, int heads, int group, int log2_block,
+                                                                     int32_t* idx_out, int rows_per_seq, int group, int log2_block,
                                                                      int max_blocks, int pages, int64_t first_row) {
   using SC = Scorer<T, D, 8>;
-  __shared__ float sc[kHeld * kWave];
+  __shared__ float sc[kShort];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const Row r = row_at(first_row + blockIdx.x, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int32_t* bt = block_table + r.row * max_blocks;
@@ -451,14 +468,11 @@ __global__ __launch_bounds__(WAVES * kWave) void score_select_kernel(const uint4
   if (frame_row<WAVES>(r, bt, to, idx, lens_out, r.row == (int64_t)r.s * rows_per_seq, log2_block, pages)) return;
   const int n = r.all - 1;
   int32_t entry[kHeld];
-  if (wave == 0) {
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) entry[i] = i * kWave + lane < n ? bt[i * kWave + lane] : -1;
-  }
+  if (wave == 0) entries_of(bt, n, entry);
   for (int base = wave * SC::kPages; base < n; base += WAVES * SC::kPages) {
     int32_t page[8];
     SC::look_up(bt, base, n - 1, lane, page);
-    const double total = SC::score(q, bounds, page, base, n, r.row * heads, group, heads, 0, 1, lane);
+    const double total = SC::score(q, bounds, page, base, n, r.row, group, 1, 0, 1, lane);
     const int j = base + SC::page_of(lane);
     if (SC::has_page(lane) && j < n) sc[j] = (float)total;
   }
@@ -503,11 +517,11 @@ hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.num_seqs * rows_per_seq;
   const int group = a.num_q_heads / a.num_kv_heads;
   constexpr int64_t kRows = 1 << 21;
-  if ((int64_t)a.max_blocks * heads * 2 * D * (int64_t)sizeof(T) <= select_one_launch_bytes() && a.max_blocks <= kHeld * kWave) {
+  if (heads == 1 && a.max_blocks <= kShort && (int64_t)a.max_blocks * 2 * D * (int64_t)sizeof(T) <= kOneLaunchBytes) {
     for (int64_t row = 0; row < rows; row += kRows)
       hipLaunchKernelGGL((score_select_kernel<T, D, 8>), dim3((unsigned)(rows - row < kRows ? rows - row : kRows)), dim3(8 * kWave),
                          0, stream, (const uint4*)a.q, (const uint4*)a.bounds, a.block_table, a.seq_lens,
-                         a.table_out, a.lens_out, a.idx_out, rows_per_seq, heads, group, log2_block, a.max_blocks, a.pages, row);
+                         a.table_out, a.lens_out, a.idx_out, rows_per_seq, group, log2_block, a.max_blocks, a.pages, row);
     return hipGetLastError();
   }
   constexpr int kPages = Scorer<T, D>::kPages;
@@ -522,7 +536,9 @@ hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
                          a.pages, (int)parts, row);
     }
   }
-  if (a.max_blocks <= 4 * kWave * kHeld)
+  if (a.max_blocks <= kShort / 2)
+    launch_select_of<1>(a, rows_per_seq, log2_block, rows, stream);
+  else if (a.max_blocks <= 4 * kWave * kHeld)
     launch_select_of<4>(a, rows_per_seq, log2_block, rows, stream);
   else
     launch_select_of<16>(a, rows_per_seq, log2_block, rows, stream);
