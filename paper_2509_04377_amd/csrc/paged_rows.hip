@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParam
         store_pair<T>(p.out, (head * D + d) / 2, lsum > 0.f ? o0 / lsum : 0.f, lsum > 0.f ? o1 / lsum : 0.f);
       } else {
         const int most = (WEIGHTS ? 1 : p.drafts) * group;
-        float* record = p.partials + (((int64_t)at.row * splits + split) * most + r) * (D + 2);
+        float* record = p.partials + ((((int64_t)hk * p.num_seqs + s) * splits + split) * most + r) * (D + 2);
         *reinterpret_cast<float2*>(record + d) = make_float2(o0, o1);
         if (d == 0) *reinterpret_cast<float2*>(record + D) = make_float2(m, lsum);
       }
@@ -392,11 +392,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParam
   }
 }
 
-// The splits of a query row, one wave each, added in their order.
+// The splits of a query row, one wave each, added in their order: records from number `first` on.
 template <typename T, int D>
-__device__ __forceinline__ void merge_row(const RowsParams& p, int row, int r, int most, int splits, int64_t head, int lane) {
+__device__ __forceinline__ void merge_row(const RowsParams& p, int64_t first, int r, int most, int splits, int64_t head, int lane) {
   constexpr int E = D / kWave;
-  const float* base = p.partials + ((int64_t)row * splits * most + r) * (D + 2);
+  const float* base = p.partials + (first * most + r) * (D + 2);
   float o[E];
   merge_splits<E>(splits, o, [&](int split, float2& ml, float (&v)[E]) {
     const float* record = base + (int64_t)split * most * (D + 2);
@@ -425,8 +425,11 @@ __global__ __launch_bounds__(kThreads) void rows_merge_kernel(const RowsParams p
   const int row = (int)(blockIdx.x / (uint32_t)tiles), r = ((int)blockIdx.x - row * tiles) * kWaves + wave;
   const int s = row / p.num_kv_heads, hk = row - s * p.num_kv_heads;
   if (r >= drafts_of(p, s) * group) return;
-  const int draft = r / group, h = r - draft * group;
-  merge_row<T, D>(p, row, r, most, shape_splits(p.shape), ((int64_t)s * p.drafts + draft) * (p.num_kv_heads * group) + hk * group + h, lane_id());
+  const int draft = r / group, h = r - draft * group, lane = lane_id();
+  int splits = shape_splits(p.shape), first = s * splits;
+  const int64_t head = (int64_t)hk * p.num_seqs * splits;
+  if (p.shares != nullptr) first = (int)p.shares[2 * s], splits = (int)p.shares[2 * s + 1];
+  merge_row<T, D>(p, head + first, r, most, splits, ((int64_t)s * p.drafts + draft) * (p.num_kv_heads * group) + hk * group + h, lane);
 }
 
 // The splits of a row and the weights of its pages, one workgroup a row.  A head's (m, l) of all splits are read at once, a split a lane, and
@@ -452,6 +455,7 @@ __global__ __launch_bounds__(kThreads) void weights_merge_kernel(const RowsParam
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int group = shape_group(p.shape), splits = shape_splits(p.shape), log2_block = shape_log2_block(p.shape);
   const int row = (int)blockIdx.x, s = row / p.num_kv_heads;
+  const int64_t first = ((int64_t)(row - s * p.num_kv_heads) * p.num_seqs + s) * splits;
   const bool shared = p.max_blocks < 0;
   const int max_blocks = shared ? -p.max_blocks : p.max_blocks;
   const int len = length_of(p, s, max_blocks, log2_block);
@@ -464,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void weights_merge_kernel(const RowsParam
   float sums[8];
   sums_of((int)threadIdx.x, sums);
   for (int h = wave; h < group; h += kWaves) {
-    const float* ml = p.partials + ((int64_t)row * splits * group + h) * (D + 2) + D;
+    const float* ml = p.partials + (first * group + h) * (D + 2) + D;
     const int64_t stride = (int64_t)group * (D + 2);
     float2 of[4];
     float m = kNegInf, l = 0.f;
@@ -474,7 +478,7 @@ __global__ __launch_bounds__(kThreads) void weights_merge_kernel(const RowsParam
       of[i] = split < splits ? *reinterpret_cast<const float2*>(ml + split * stride) : make_float2(kNegInf, 0.f);
       m = fmaxf(m, of[i].x);
     }
-    merge_row<T, D>(p, row, h, group, splits, (int64_t)row * group + h, lane);
+    merge_row<T, D>(p, first, h, group, splits, (int64_t)row * group + h, lane);
     m = wave_max(m);
     const float ms = m == kNegInf ? 0.f : m;
 #pragma unroll
@@ -543,7 +547,7 @@ hipError_t launch_paged_rows(const RowsArgs& a, hipStream_t stream) {
   int log2_block = 0;
   while ((1 << log2_block) < a.block_size) ++log2_block;
   p.shape = (uint32_t)log2_block | (uint32_t)(a.num_q_heads / a.num_kv_heads) << 3 | (uint32_t)a.splits << 9;
-  p.drafts = a.drafts;
+  p.drafts = a.drafts, p.num_seqs = a.num_seqs, p.shares = a.shares;
   p.q = a.q;
   p.scale_log2e = a.scale * 1.4426950408889634f;
   p.decay = a.decay;

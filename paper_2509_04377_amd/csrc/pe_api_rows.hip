@@ -55,6 +55,8 @@ int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q,
   a.tile_rows = pe::tree_tile_rows(a.is_bf16, (int64_t)desc->num_seqs * desc->num_kv_heads,
                                    num_drafts * (desc->num_q_heads / desc->num_kv_heads), compute_units());
   a.splits = pe::tree_splits_of(desc, num_drafts);
+  if (pe::tree_shares_splits(desc, num_drafts, a.splits))
+    a.shares = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + pe::tree_partials_bytes(desc, num_drafts, a.splits));
   return pe::launch_paged_rows(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PE_OK : PE_ERR_HIP;
 }
 

@@ -21,11 +21,12 @@ struct RowsArgs {
   const int32_t* block_table;
   const int32_t* seq_lens;
   void* out;
-  float* partials;  // [rows][splits][drafts * G][D + 2] fp32 (unused when splits == 1)
+  float* partials;  // [KV head][sequence][splits][drafts * G][D + 2] fp32 (unused when splits == 1)
   float scale;
   int num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, max_blocks;
   int tile_rows, splits;
   bool is_bf16, shared;
+  uint32_t* shares = nullptr;  // [num_seqs][2] where the splits are shared out by the sequences' lengths: a sequence's first one and their number
   // trees of drafts
   int drafts = 1;
   const void* k_draft = nullptr;
@@ -66,7 +67,7 @@ hipError_t launch_append_path(const PathArgs& a, hipStream_t stream);
 //   one sequence, 32 query rows a KV head 12.9 | 15.5 | 17.3, 64 rows 14.5 | 16.2 | 18.5, 128 rows 18.9 | 18.1 | 21.4, 256 rows 27.9 | 23.1 | 28.5;
 //   eight sequences, 32 rows 30.9 | 29.6 | 37.5, 64 rows 45.6 | 36.5 | 41.6, 96 rows 86.5 | 49.9 | 45.4, 128 rows 86.4 | 52.2 | 48.4, 192 rows
 //   129.8 | 92.8 | 64.0; 32 sequences of 1024 to 2048 tokens, 32 rows 55.9 | 43.1 | 60.0, 64 rows 94.8 | 63.5 | 61.8, 128 rows 165.5 | 106.6 | 71.8.
-constexpr int kWideRows = 256;
+constexpr int kWideRows = 256, kWideTile = 64;  // and tokens of a step
 inline int tree_tile_rows(bool is_bf16, int64_t kv_rows, int rows, int compute_units) {
   const int64_t of16 = kv_rows * ((rows + 15) / 16), of32 = kv_rows * ((rows + 31) / 32);
   if (rows <= 16 || of16 * 8 <= compute_units) return 16;
@@ -112,10 +113,19 @@ inline int tree_splits_of(const pe_cache_desc* d, int drafts) {
   return tree_splits(d->dtype == PE_BF16, (int64_t)d->num_seqs * d->num_kv_heads, drafts * (d->num_q_heads / d->num_kv_heads),
                      (int64_t)d->max_blocks * d->block_size, host::compute_units());
 }
+inline size_t tree_partials_bytes(const pe_cache_desc* d, int drafts, int splits) {
+  return splits > 1 ? (size_t)d->num_seqs * d->num_q_heads * drafts * splits * (d->head_dim + 2) * sizeof(float) : 0;
+}
+// Up to 64 sequences of tree_wide.hip have their splits shared out among them (a lane looks at a sequence; pe_rows_device.h).
+inline bool tree_shares_splits(const pe_cache_desc* d, int drafts, int splits) {
+  return d->num_seqs > 1 && d->num_seqs <= 64 && splits > 1 &&
+         tree_tile_rows(d->dtype == PE_BF16, (int64_t)d->num_seqs * d->num_kv_heads, drafts * (d->num_q_heads / d->num_kv_heads),
+                        host::compute_units()) == kWideRows;
+}
 inline size_t tree_workspace_bytes(const pe_cache_desc* d, int64_t drafts) {
   if (drafts < 1 || drafts > kMostDrafts) return 0;
   const int splits = tree_splits_of(d, (int)drafts);
-  return splits > 1 ? (size_t)d->num_seqs * d->num_q_heads * drafts * splits * (d->head_dim + 2) * sizeof(float) : 0;
+  return tree_partials_bytes(d, (int)drafts, splits) + (tree_shares_splits(d, (int)drafts, splits) ? (size_t)d->num_seqs * 2 * sizeof(uint32_t) : 0);
 }
 
 }  // namespace pe

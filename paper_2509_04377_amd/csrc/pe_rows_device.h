@@ -31,6 +31,8 @@ struct RowsParams {
   const float* weights_in;       // or null
   float* weights_out;
   float* page_sums;              // [rows][max_blocks][G], where there are several splits
+  int num_seqs;
+  uint32_t* shares;              // [num_seqs][2], or null: every sequence has the same number of splits
 };
 
 __device__ __forceinline__ int drafts_of(const RowsParams& p, int s) {
@@ -42,6 +44,22 @@ __device__ __forceinline__ int length_of(const RowsParams& p, int s, int max_blo
   const int len = p.seq_lens[s];
   const int64_t most = (int64_t)max_blocks << log2_block;  // (a longer row is a caller error: its table ends here)
   return len < 0 ? 0 : len < most ? len : (int)most;
+}
+
+// Splits by the lengths of up to 64 sequences: of the num_seqs * splits that the launch has for a KV head a sequence gets one for every t of
+// its tiles of kTile tokens (the drafts are one), with the smallest t (or a few percent more, in the long run) for which they suffice.  The
+// lengths are on the device, so every wave works this out for itself: a few steps, as t begins where they would suffice without remainders.
+// The launch that merges the splits reads what the first of a sequence's notes.
+// The splits up to and including those of sequence `lane`.
+__device__ __forceinline__ uint32_t splits_upto(const RowsParams& p, int max_blocks, int log2_block, int tile, int lane) {
+  uint32_t units = 0u;
+  if (lane < p.num_seqs && drafts_of(p, lane) > 0) units = ((uint32_t)length_of(p, lane, max_blocks, log2_block) + tile - 1) / tile + 1u;
+  const uint32_t have = (uint32_t)(p.num_seqs * shape_splits(p.shape));
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum_u32(units), kWave - 1);
+  for (uint32_t t = all > have ? (all + have - 1) / have : 1u;; t += 1u + (t >> 5)) {  // (with t the most tiles of all, one a sequence suffices)
+    const uint32_t upto = wave_prefix_sum_u32((units + t - 1u) / t);
+    if ((uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1) <= have) return upto;
+  }
 }
 
 // The grid for `rows` query rows a workgroup, and what of the arguments goes with it.

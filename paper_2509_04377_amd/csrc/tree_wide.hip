@@ -20,7 +20,7 @@
 namespace pe {
 namespace {
 
-constexpr int kTile = 64;  // tokens
+constexpr int kTile = kWideTile;
 constexpr int WAVES = kWideRows / 32, NT = WAVES * kWave;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -43,15 +43,29 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
 
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int h = lane >> 5, n = lane & 31, tid = (int)threadIdx.x;
-  const int log2_block = shape_log2_block(p.shape), group = shape_group(p.shape), splits = shape_splits(p.shape);
+  const int log2_block = shape_log2_block(p.shape), group = shape_group(p.shape);
+  int splits = shape_splits(p.shape);
   const Place at = place_at(blockIdx.x, blockIdx.y, (p.shape & kShapeXcd) != 0, (p.shape & kShapeLinear) != 0, splits * p.tiles, p.num_kv_heads,
                             p.inv_heads);
-  const int s = at.seq, hk = at.head, split = at.split / p.tiles, tile0 = at.split - split * p.tiles;
-  const bool shared = p.max_blocks < 0;
+  const bool shared = p.max_blocks < 0, several = splits > 1;
   const int max_blocks = shared ? -p.max_blocks : p.max_blocks;
+  const int hk = at.head;
+  int s = at.seq, split = at.split / p.tiles;
+  const int tile0 = at.split - split * p.tiles;
+  const int64_t slot = ((int64_t)hk * p.num_seqs + s) * splits + split;  // of its record
+  if (p.shares != nullptr) {
+    const uint32_t mine = (uint32_t)(s * splits + split);
+    const uint32_t upto = splits_upto(p, max_blocks, log2_block, kTile, lane);
+    s = (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= mine));
+    if (s >= p.num_seqs) return;  // more than are needed
+    const uint32_t first = s > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, s - 1) : 0u;
+    splits = (int)((uint32_t)__builtin_amdgcn_readlane((int)upto, s) - first);
+    split = (int)(mine - first);
+    if (split == 0 && at.head == 0 && threadIdx.x == 0) *reinterpret_cast<uint2*>(p.shares + 2 * s) = make_uint2(first, (uint32_t)splits);
+  }
   // (read only while the launch runs: scalar loads, which the barriers would otherwise forbid)
   const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
-      reinterpret_cast<uintptr_t>(p.block_table + (int64_t)(shared ? s : at.row) * max_blocks));
+      reinterpret_cast<uintptr_t>(p.block_table + (shared ? (int64_t)s : (int64_t)s * p.num_kv_heads + hk) * max_blocks));
   const int drafts = drafts_of(p, s), rows = drafts * group, row0 = tile0 * kWideRows;
   if (row0 >= rows) return;
   const int len = length_of(p, s, max_blocks, log2_block);
@@ -248,7 +262,7 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
   // ---- every wave has its rows' whole states: lane (h, n) rows 8*(i/4) + 4*h + i%4 of C, elements 32*e + row of query n ---------------
   if (r >= rows) return;
   const float l = halves_sum(l_run);
-  if (splits == 1) {
+  if (!several) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     uint16_t* out = static_cast<uint16_t*>(p.out) + (((int64_t)s * p.drafts + draft) * num_q_heads + hk * group + head) * D;
 #pragma unroll
@@ -256,7 +270,7 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
 #pragma unroll
       for (int i = 0; i < 16; i += 2) store_pair<bf16_t>(out, (32 * e + 8 * (i / 4) + 4 * h + i % 4) / 2, acc[e][i] * inv, acc[e][i + 1] * inv);
   } else {
-    float* record = p.partials + (((int64_t)at.row * splits + split) * (p.drafts * group) + r) * (D + 2);
+    float* record = p.partials + (slot * (p.drafts * group) + r) * (D + 2);
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
