@@ -56,11 +56,11 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
   if (p.shares != nullptr) {
     const uint32_t mine = (uint32_t)(s * splits + split);
     const uint32_t upto = splits_upto(p, max_blocks, log2_block, kTile, lane);
-    s = (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= mine));
+    s = __builtin_amdgcn_readfirstlane((int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= mine)));
     if (s >= p.num_seqs) return;  // more than are needed
     const uint32_t first = s > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, s - 1) : 0u;
-    splits = (int)((uint32_t)__builtin_amdgcn_readlane((int)upto, s) - first);
-    split = (int)(mine - first);
+    splits = __builtin_amdgcn_readfirstlane((int)((uint32_t)__builtin_amdgcn_readlane((int)upto, s) - first));
+    split = __builtin_amdgcn_readfirstlane((int)(mine - first));
     if (split == 0 && at.head == 0 && threadIdx.x == 0) *reinterpret_cast<uint2*>(p.shares + 2 * s) = make_uint2(first, (uint32_t)splits);
   }
   // (read only while the launch runs: scalar loads, which the barriers would otherwise forbid)
@@ -178,10 +178,8 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[sub][i] = 0.f;
-#pragma unroll
       for (int j = 0; j < CH; ++j) {
-        x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[j]), q[j], x[sub], 0, 0, 0);
+        x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[j]), q[j], j == 0 ? f32x16_t{} : x[sub], 0, 0, 0);
         if (sub == 0) k[j] = kt[32 * CPT + ((2 * j) ^ k_swap)];
       }
     }
