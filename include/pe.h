@@ -1,13 +1,15 @@
 /*
  * pe.h -- C ABI of libpe: the data-parallel hot path of PagedEviction on one AMD MI355X (gfx950).
  *
- * The path has three parts over a paged KV cache (Sec. 2.4: fixed-size blocks of B tokens, a block
+ * The paper's path has three parts over a paged KV cache (Sec. 2.4: fixed-size blocks of B tokens, a block
  * table that maps logical to physical blocks):
  *   1. attention-free importance scores from the cached K/V (Alg. 1), one per block;
  *   2. structured eviction: token-level pruning of the prompt to the budget C before it is split
  *      into pages (Alg. 2), then, during decode, dropping the lowest-scoring block of a row whenever
  *      its newest block has filled, and compacting the block table (Alg. 3);
  *   3. the single-query paged attention that reads what is left (Eq. 1; Alg. 3 "PagedAttention").
+ * Beside it, on the same cache: attention of trees of drafted tokens and the accepted ones' way into the cache (5), attention
+ * over the pages that a query can need most (6), and attention that keeps the weight each page got, to evict by (7).
  *
  * Granularity: every decision is taken per ROW = one (sequence, KV head).  A row owns one row of the
  * block table and its own pages; a page holds B x D elements of K (and a sibling page of V, same
@@ -353,7 +355,8 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
  *     q, the drafts in use and the tokens attended to are finite; what lies behind a row's end or behind a sequence's last
  *     draft may be anything.  A draft in use is finite even where no mask names it.
  *     `out` may be q itself and must not otherwise overlap what is read.  desc->decode_splits is the number of splits of a row here too (0: the
- *     library's choice); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
+ *     library's choice; with many query rows the sequences share them out by their lengths, so that an output's last bits can depend on
+ *     the other sequences' lengths); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
  *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29, at most 65536 KV heads.
  *     workspace: pe_workspace_bytes(PE_OP_TREE_DECODE, desc, num_drafts) (split partials).
  *     shared: block_table [S][max_blocks].

@@ -261,6 +261,9 @@ class PagedCache:
         left = [int(n) for n in host_path_lens]
         if len(left) != len(self.host_lens) or min(left) < 0 or max(left) > path.shape[-1]:
             raise ValueError("host_path_lens: one length per sequence, 0 to path.shape[-1]")
+        room = self.desc.max_blocks * B
+        if self.budget > room and any(n + m > room for n, m in zip(self.host_lens, left)):
+            raise ValueError("the path is longer than what is left of a table row, and nothing is evicted below the budget")
         path_done = torch.zeros_like(path_lens)
         while any(left):
             trig = self.triggers()

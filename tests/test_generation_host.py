@@ -65,6 +65,23 @@ def test_path_lengths_that_are_refused():
     assert cache.host_lens == [10, 20]
 
 
+def test_a_path_that_leaves_the_table_is_refused():
+    """Without evictions (a budget beyond the table) a row holds what its table holds; at a budget it never gets that far."""
+    cache = _cache([10, 20], 64)
+    drafts, path, n = torch.zeros((2, 64, 2, 64)), torch.zeros((2, 64), dtype=torch.int32), [54, 44]
+    cache.budget = 10 ** 6
+    assert cache.desc.max_blocks * B == 64
+    with host_only():
+        with pytest.raises(ValueError, match="left of a table row"):
+            cache.accept_path(drafts, drafts, path, torch.tensor([50, 45], dtype=torch.int32), [50, 45])
+        assert cache.host_lens == [10, 20]
+        cache.accept_path(drafts, drafts, path, torch.tensor(n, dtype=torch.int32), n)
+        assert cache.host_lens == [64, 64]
+        cache.budget = 64
+        cache.accept_path(drafts, drafts, path, torch.tensor([64, 64], dtype=torch.int32), [64, 64])
+    assert cache.host_lens == [_one_by_one(64, 64, 64)] * 2
+
+
 @pytest.mark.parametrize("seed", range(3))
 def test_every_page_behind_the_newest_has_bounds(monkeypatch, seed):
     """A model of the pages: which have bounds is noted by the launch that would have made them; an eviction takes any."""

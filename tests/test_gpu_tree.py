@@ -286,3 +286,27 @@ def test_append_path_leaves_full_tables_and_negative_lengths_alone():
     for a, b in zip((kp, vp, table, lens), before):
         assert torch.equal(a.nan_to_num(9.0) if a.is_floating_point() else a, b.nan_to_num(9.0) if b.is_floating_point() else b)
     assert int(done.sum()) == 0 and int(used.sum()) == 0
+
+
+@pytest.mark.parametrize("splits", [0, 2, 5])
+@pytest.mark.parametrize("D,shared", [(128, False), (64, True)])
+def test_many_query_rows_of_sequences_of_very_different_lengths(D, shared, splits):
+    """Eight query heads and 64 drafts a sequence; one long sequence, short and empty ones, and some without a draft: a sequence's share of
+    the splits goes by its length, and none at all to one without a query."""
+    print("case shares", D, shared, splits, flush=True)
+    lens, counts, T, G = [0, 1, 64, 3000, 5, 700, 63, 65, 2000, 0], [64, 64, 5, 64, 0, 33, 64, 1, 0, 0], 64, 8
+    c, q, kd, vd, sees, words = _case(31 + splits, lens, counts, T, 1, G, D, 16, torch.bfloat16, shared)
+    want, bound = _want(c, q, kd, vd, sees, counts, G)
+    _check(_run(c, q, kd, vd, words, counts, T, splits), want, bound, counts, torch.bfloat16)
+
+
+@pytest.mark.parametrize("S", [2, 64, 65])
+def test_many_query_rows_of_many_sequences(S):
+    """As many sequences as have their splits shared out, one more, and two."""
+    print("case sequences", S, flush=True)
+    T, Hk, G = (40, 8, 8) if S == 2 else (33, 1, 4)
+    lens, counts = [(37 * s) % 300 for s in range(S)], [T - s % 3 for s in range(S)]
+    c, q, kd, vd, sees, words = _case(S, lens, counts, T, Hk, G, 64, 32, torch.bfloat16, False)
+    want, bound = _want(c, q, kd, vd, sees, counts, G)
+    for splits in (0, 3):
+        _check(_run(c, q, kd, vd, words, counts, T, splits), want, bound, counts, torch.bfloat16)
