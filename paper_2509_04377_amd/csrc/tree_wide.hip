@@ -1,6 +1,8 @@
 // Attention of a tree of drafted tokens over a paged bfloat16 cache, for many query rows: more than 32 share the K and V of a row.
 //
-// The products count here, not the traffic: 256 query rows ask for 256 operations a byte of the cache.  A workgroup owns 32 query rows a
+// The products count here, not the traffic: 256 query rows ask for 256 operations a byte of the cache.  (64 drafts x 4 heads over eight caches of
+// 4001 to 8192 tokens of D = 128, eight KV heads: 88 us and 10 for the merge, 500 TFLOP/s and half as many again for the low terms; the matrix
+// units are busy for 45 % of it at the 1.8 GHz that are left of the clock.)  A workgroup owns 32 query rows a
 // wave and one split of the tokens (tiles of 64, the drafts are the last one); K and V of a tile go through LDS once for all its waves,
 // which read them as operands of the 32 x 32 x 16 products.  The tile behind the next one is on its way to registers while one is computed
 // out of one half of LDS and the next is put into the other; one barrier a tile.
@@ -12,9 +14,10 @@
 //   PV (A = V transposed, B = P): a product contracts 16 tokens, lane half h those that it has: registers 8*c .. 8*c + 7 of the logits.  Row m
 //   of A is element 32*e + m in product e; the reads that turn 16 elements of four tokens over 16 lanes bring it out of LDS as it lies.
 //
-// Probabilities go into the product as two bfloat16 terms, as in paged_rows.hip, and the softmax is that one too.  (In one term, rounded, 64
-// drafts x 4 heads over 8 caches of 4001 to 8192 tokens of D = 128 take 90 us instead of 104, and the outputs are sqrt(2) times as far from 64
-// bits: their own rounding, and as much again.)
+// Probabilities go into the product as two bfloat16 terms, as in paged_rows.hip, and the softmax is that one too.  (In one term, rounded, those
+// drafts took 90 us where two took 104, and the outputs were sqrt(2) times as far from 64 bits: their own rounding, and as much again.)
+// Measured against it and not better: tiles of 128 tokens (144 us where 64 took 123), two workgroups of four waves a compute unit (the
+// same), half of the waves a phase behind the others (109 / 99), the low terms by dot products (103 / 98).
 #include "pe_rows_device.h"
 
 namespace pe {
