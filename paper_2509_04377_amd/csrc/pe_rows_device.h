@@ -50,6 +50,8 @@ __device__ __forceinline__ int length_of(const RowsParams& p, int s, int max_blo
 // its tiles of kTile tokens (the drafts are one), with the smallest t (or a few percent more, in the long run) for which they suffice.  The
 // lengths are on the device, so every wave works this out for itself: a few steps, as t begins where they would suffice without remainders.
 // The launch that merges the splits reads what the first of a sequence's notes.
+// (64 drafts x 4 heads, eight sequences of 4001 to 8192 tokens, eight KV heads of D = 128: the longest of the 256 workgroups has 27 tiles where
+// four splits a sequence give it 32, 98.8 us instead of 105.6.)
 // The splits up to and including those of sequence `lane`.
 __device__ __forceinline__ uint32_t splits_upto(const RowsParams& p, int max_blocks, int log2_block, int tile, int lane) {
   uint32_t units = 0u;
