@@ -31,8 +31,10 @@
 // What bounds it is reading K and V: eight heads of D = 128, 32 sequences, 8 drafts x 4 heads over 1024 to 2048 tokens 42.5 us (4.8 TB/s; the
 // last workgroups have the longest rows to themselves), one query with weights over 2033 to 2048 tokens 45 (5.9 TB/s).  Few rows are bound by
 // the chain of a launch (length, page, K, products, merge): one sequence of 1000 tokens, 4 x 4 heads of D = 64, 6 us and 2.4 for the merge of
-// its splits.  fp32 with few query rows a KV head is bound by its products, of whose 16 columns it uses few (2 of D = 128, 300 tokens a
-// split: 14 us).  Eight waves instead of four were not faster over 20 shapes (42.5 / 44 and 10.1 / 10.6 us).
+// its splits: 0.8 until the length is there, as much again for the first K, 0.6 for the step, 0.9 each for the drafts' and the end.  fp32 of
+// D = 128 takes 1.7 us a step (16 tokens a wave).  Not faster, over 20 shapes: eight waves (42.5 / 44 and 10.1 / 10.6 us), two steps of a
+// wave on their way (8.6 / 9.4 for the 1000 tokens, 45 / 46 for the weights: what a wave asks for behind its last step costs more than the
+// wait saves), no loads behind the last step (8.6 / 8.2, but 44 / 46.5 for the batch), fp32 products of four columns (18.5 / 18.6).
 #include "pe_rows_device.h"
 
 namespace pe {
