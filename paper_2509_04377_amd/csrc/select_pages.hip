@@ -80,8 +80,8 @@ __global__ __launch_bounds__(kWaves * kWave) void page_bounds_kernel(const uint4
 // ---- scores --------------------------------------------------------------------------------------------------------------
 // A wave scores NL * 64 / LPB pages at a time: the 2 D bounds of a page and head are LPB lanes' 16 bytes, lo in the lower half of them and hi
 // in the upper.  NL loads are in flight; their sums meet in a reduce-scatter.  4 sequences of 60001 to 65536 tokens (32 rows of 4096 pages,
-// 64 MB of bounds) take 16 us: ten at the rate of a large read, then the launch, and the way from the length to the pages to their bounds.
-template <typename T, int D, int NL = 16>
+// 64 MB of bounds) take 14 us: ten at the rate of a large read, then the launch, and the way from the length to the pages to their bounds.
+template <typename T, int D, int NL>
 struct Scorer {
   static constexpr int EPL = Elem<T>::kPerVec, LPB = 2 * D / EPL, PPL = kWave / LPB, kPages = NL * PPL;
 
@@ -150,19 +150,18 @@ __device__ __forceinline__ Row row_at(int64_t row, const int32_t* seq_lens, int 
 }
 
 // Scores of a row's pages but the newest, for a launch behind this one.  A workgroup has its four waves' pages, or with several heads a
-// decision those of one wave, of which each wave takes every fourth head.
-template <typename T, int D>
-__global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4* q, const uint4* bounds, const int32_t* block_table,
-                                                                     const int32_t* seq_lens, float* scores, int rows_per_seq, int heads, int group,
-                                                                     int log2_block, int max_blocks, int pages, int parts, int64_t first_row) {
-  using SC = Scorer<T, D>;
-  __shared__ double of_heads[kWaves][kWave];
+// decision (HEADS) those of one wave, of which each wave takes every fourth head.
+template <typename T, int D, int NL, bool HEADS>
+__global__ __launch_bounds__(kWaves * kWave, NL == 16 ? 4 : 1) void score_pages_kernel(
+    const uint4* q, const uint4* bounds, const int32_t* block_table, const int32_t* seq_lens, float* scores, int rows_per_seq, int heads, int group,
+    int log2_block, int max_blocks, int pages, int parts, int64_t first_row) {
+  using SC = Scorer<T, D, NL>;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t in = blockIdx.x / (uint32_t)parts;
   const int part = (int)(blockIdx.x - in * (uint32_t)parts);
-  const int base = (heads > 1 ? part : part * kWaves + wave) * SC::kPages;
+  const int base = (HEADS ? part : part * kWaves + wave) * SC::kPages;
   if (base >= max_blocks) return;
-  int32_t page[16];
+  int32_t page[NL];
   SC::look_up(block_table + (first_row + in) * max_blocks, base, max_blocks - 1, lane, page);  // (they travel together with the length)
   const Row r = row_at(first_row + in, seq_lens, rows_per_seq, log2_block, max_blocks);
   const int n = r.all - 1;  // candidates
@@ -170,18 +169,19 @@ __global__ __launch_bounds__(kWaves * kWave) void score_pages_kernel(const uint4
   const int j = base + SC::page_of(lane);
   float* to = scores + r.row * max_blocks + j;
   const bool mine = SC::has_page(lane) && j < n;
-  if (heads == 1) {
+  if constexpr (!HEADS) {
     const double total = SC::score(q, bounds, page, base, n, r.row, group, 1, 0, 1, lane);
     if (mine) *to = (float)total;
-    return;
-  }
-  of_heads[wave][lane] = SC::score(q, bounds, page, base, n, r.row * heads, group, heads, wave, kWaves, lane);
-  __syncthreads();
-  if (wave != 0 || !mine) return;
-  double total = of_heads[0][lane];
+  } else {
+    __shared__ double of_heads[kWaves][kWave];
+    of_heads[wave][lane] = SC::score(q, bounds, page, base, n, r.row * heads, group, heads, wave, kWaves, lane);
+    __syncthreads();
+    if (wave != 0 || !mine) return;
+    double total = of_heads[0][lane];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) total += of_heads[w][lane];
-  *to = (float)total;
+    for (int w = 1; w < kWaves; ++w) total += of_heads[w][lane];
+    *to = (float)total;
+  }
 }
 
 // ---- selection -----------------------------------------------------------------------------------------------------------
@@ -517,6 +517,24 @@ void launch_select_of(const SelectArgs& a, int rows_per_seq, int log2_block, int
                        row);
 }
 
+// Sixteen loads a wave, in registers that leave four waves a SIMD, where there are two such workgroups a compute unit or more; eight where there
+// are fewer, or several heads a decision.  (bf16, D = 128, the whole call with sixteen / eight: 32 rows of 4096 pages 25.8 / 27.6 us, 256 of 1024
+// 39.6 / 43.4, 8 of 4096 17.0 / 17.2, 8 of 1024 11.7 / 10.6; eight heads a decision, 2 rows of 2048 22.0 / 16.0.)
+template <typename T, int D, int NL, bool HEADS>
+hipError_t launch_scores(const SelectArgs& a, int rows_per_seq, int heads, int group, int log2_block, int64_t rows, hipStream_t stream) {
+  constexpr int64_t kEach = Scorer<T, D, NL>::kPages * (HEADS ? 1 : kWaves);
+  const int64_t parts = (a.max_blocks + kEach - 1) / kEach;
+  const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / parts;
+  if (some < 1) return hipErrorInvalidValue;
+  for (int64_t row = 0; row < rows; row += some) {
+    const int64_t now = rows - row < some ? rows - row : some;
+    hipLaunchKernelGGL((score_pages_kernel<T, D, NL, HEADS>), dim3((unsigned)(now * parts)), dim3(kWaves * kWave), 0, stream, (const uint4*)a.q,
+                       (const uint4*)a.bounds, a.block_table, a.seq_lens, a.scores, rows_per_seq, heads, group, log2_block, a.max_blocks,
+                       a.pages, (int)parts, row);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
   int log2_block = 0;
@@ -532,17 +550,16 @@ hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
                          a.table_out, a.lens_out, a.idx_out, rows_per_seq, group, log2_block, a.max_blocks, a.pages, row);
     return hipGetLastError();
   }
-  constexpr int kPages = Scorer<T, D>::kPages;
-  const int64_t each = heads > 1 ? kPages : kPages * kWaves, parts = (a.max_blocks + each - 1) / each;
   if (a.max_blocks > a.pages && a.pages > 1) {
-    const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / parts;
-    if (some < 1) return hipErrorInvalidValue;
-    for (int64_t row = 0; row < rows; row += some) {
-      const int64_t now = rows - row < some ? rows - row : some;
-      hipLaunchKernelGGL((score_pages_kernel<T, D>), dim3((unsigned)(now * parts)), dim3(kWaves * kWave), 0, stream, (const uint4*)a.q,
-                         (const uint4*)a.bounds, a.block_table, a.seq_lens, a.scores, rows_per_seq, heads, group, log2_block, a.max_blocks,
-                         a.pages, (int)parts, row);
-    }
+    hipError_t e;
+    constexpr int64_t kEach16 = Scorer<T, D, 16>::kPages * kWaves;
+    if (heads > 1)
+      e = launch_scores<T, D, 8, true>(a, rows_per_seq, heads, group, log2_block, rows, stream);
+    else if (rows * ((a.max_blocks + kEach16 - 1) / kEach16) >= 2 * host::compute_units())
+      e = launch_scores<T, D, 16, false>(a, rows_per_seq, heads, group, log2_block, rows, stream);
+    else
+      e = launch_scores<T, D, 8, false>(a, rows_per_seq, heads, group, log2_block, rows, stream);
+    if (e != hipSuccess) return e;
   }
   if (a.max_blocks <= kShort / 2)
     launch_select_of<1>(a, rows_per_seq, log2_block, rows, stream);
