@@ -74,13 +74,26 @@ inline int tree_tile_rows(bool is_bf16, int64_t kv_rows, int rows, int compute_u
   return !is_bf16 || rows <= 64 || of32 * 4 <= compute_units ? 32 : kWideRows;
 }
 
-// Splits of a row: as many as leave no compute unit two workgroups, of 128 tokens or more (of the table's, which the host knows).
+// Splits of a row: as many as leave no compute unit two workgroups, of 128 tokens or more (of the table's, which the host knows).  More than half
+// as many workgroups as compute units, or a few more than there are, leave many of these idle in the end; long rows are cut in two or three then,
+// where the compute units' turns (of whole workgroups, each a part of a row) become three quarters or less.  (One / that many, us, bfloat16,
+// D = 128, one query with weights: rows of 4096 tokens, 136 of them 60.3 / 54.4, 160 64.0 / 61.9, 288 135 / 115, 320 137 / 122, 384 151 / 139;
+// the same down to half the length, 8192: 110 / 85.8, 114 / 96.9, 203 / 174, 212 / 183, 234 / 215.  Not with rows of 1024: 136 of them
+// 18.5 / 21.9.  192 rows, which only four parts would even out: 69.8 / 72.8.  Rows of 700 tokens in such tables, eight drafts: 136 of them
+// 20.3 / 23.3, 288 35.2 / 39.2.)
+constexpr int kLongTokens = 4096;
 inline int tree_splits(bool is_bf16, int64_t kv_rows, int rows, int64_t tokens, int compute_units) {
   const int tile = tree_tile_rows(is_bf16, kv_rows, rows, compute_units);
   const int64_t groups = kv_rows * ((rows + tile - 1) / tile);
   int64_t splits = compute_units / groups;
   if (splits > tokens / 128) splits = tokens / 128;
-  return splits > 64 ? 64 : splits < 1 ? 1 : (int)splits;
+  if (splits > 1) return splits > 64 ? 64 : (int)splits;
+  const auto turns = [&](int64_t parts) { return (groups * parts + compute_units - 1) / compute_units; };
+  int64_t best = 1;
+  if (tile != kWideRows && tokens >= kLongTokens)
+    for (int64_t parts = 2; parts <= 3; ++parts)
+      if (turns(parts) * 4 <= turns(1) * parts * 3 && turns(parts) * best < turns(best) * parts) best = parts;
+  return (int)best;
 }
 
 // Page weights: the parts of a split lie in LDS, 8 bytes for every 16 tokens and query head, beside what the waves' states take.
