@@ -348,7 +348,8 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
  *     mask need not describe a tree: a chain's word is (2 << i) - 1):
  *     out[s][i][h][:] = sum_a softmax_a(softmax_scale * <q[s][i][h], k_a>) v_a over those tokens a, with the keys and values of
  *     row (s, h / (Hq/Hk)) of the cache and of head h / (Hq/Hk) of the drafts.  A query that attends to nothing gives zeros.
- *     fp32 accumulation, output rounded to desc->dtype.
+ *     fp32 accumulation, output rounded to desc->dtype.  bf16: a softmax weight goes into its product with V rounded to within 2^-17
+ *     of it (pe_paged_decode keeps all of its bits); the sum that it is divided by has the weights as they were.
  *     q, out: [S][num_drafts][Hq][D].  k_draft, v_draft: [S][num_drafts][Hk][D], read only, not part of the cache.
  *     draft_lens: [S] int32, or NULL where every sequence has num_drafts (values are taken as if clamped to 0..num_drafts);
  *     rows of `out` behind a sequence's last draft are left as they were.  tree_mask: [S][num_drafts] 64-bit words.
@@ -415,7 +416,7 @@ int pe_select_pages(const pe_cache_desc* desc, const void* q, const void* bounds
 /*
  * (7) Paged decode attention that also keeps the weight each page got -- for an eviction by accumulated attention (the kind of
  *     importance that the paper's attention-free score is the alternative to: Sec. 3), with the eviction calls of (3).
- *     `out` as pe_paged_decode.  For every row and every page j < n = ceil(seq_lens[s] / B):
+ *     `out` as pe_paged_decode, but for the rounding of bf16 weights that (5) has.  For every row and every page j < n = ceil(seq_lens[s] / B):
  *        weights_out[s][hk][j] = decay * before + sum over the row's query heads h, sum over the page's tokens t of
  *                                softmax_t(softmax_scale * <q[s][h], K_t>),
  *     before = weights_in[s][hk][j] where that is finite, else 0 (a page's first step); entries j >= n become +INF.  fp32.

@@ -17,8 +17,8 @@
 //   (fp32: d = 64*(e/4) + 4*m + e%4): lane l loads those of row n of its tokens 4*g + r, whole runs of a token for 16 lanes.
 //   bfloat16 products contract 32 tokens (two parts), fp32 ones four, one for each r.
 //
-// bfloat16: a probability goes into the product as two bfloat16 terms, p = hi + lo + less than 2^-16 p (hi the upper half of its
-// bits, lo what they leave): one product more of each, and no rounding of the probabilities beside that of the output.
+// bfloat16: a probability goes into the product as two bfloat16 terms, within 2^-17 of it (terms_of): one product more of each, and a
+// rounding of the probabilities that is small beside that of the output.
 //
 // Softmax: online, base 2, a reference per query row and wave that is set kGrow above the largest logit and moves only when one
 // exceeds it, so that rescaling is rare.  What no row attends to (a token behind the row's end, a draft behind the sequence's
@@ -284,10 +284,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_rows_kernel(const RowsParam
         uint32_t hw[4], lw[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const uint32_t p0 = __float_as_uint(x[a][w / 2][w % 2 * 2]), p1 = __float_as_uint(x[a][w / 2][w % 2 * 2 + 1]);
-          hw[w] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
-          const float r0 = __uint_as_float(p0) - __uint_as_float(p0 & 0xffff0000u), r1 = __uint_as_float(p1) - __uint_as_float(p1 & 0xffff0000u);
-          lw[w] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
+          const Terms t = terms_of(x[a][w / 2][w % 2 * 2], x[a][w / 2][w % 2 * 2 + 1]);
+          hw[w] = t.hi;
+          lw[w] = t.lo;
         }
         hi[a] = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
         lo[a] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));

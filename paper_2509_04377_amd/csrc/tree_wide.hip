@@ -224,9 +224,9 @@ __global__ __launch_bounds__(NT, 2) void tree_wide_kernel(const RowsParams p) {
       for (int i = 0; i < 4; ++i) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(x[c / 2][8 * (c % 2) + 2 * i], scale, -m_ref));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(x[c / 2][8 * (c % 2) + 2 * i + 1], scale, -m_ref));
-        hi[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
-        const float r0 = p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u), r1 = p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
-        lo[i] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
+        const Terms t = terms_of(p0, p1);
+        hi[i] = t.hi;
+        lo[i] = t.lo;
         l_run += p0 + p1;
       }
       const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
