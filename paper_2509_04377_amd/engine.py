@@ -511,13 +511,16 @@ class GraphedStepper:
 
     The inputs live in fixed buffers (new_k, new_v, q, out), as a serving loop would keep them.  A step's
     launch sequence depends only on host-side integers (which lengths array is current, whether this is a
-    trigger step, how many pages the cached-score mode has to score), so that tuple keys the graph.  The
-    first step with a new key is captured and then replayed; later ones advance the host bookkeeping with
-    the launches switched off and replay the stored graph."""
+    trigger step, how many pages the cached-score mode has to score) and on what select_pages and evict_by_attention
+    have put into the caches, so that these key the graph.  The first step with a new key is captured and then
+    replayed; later ones advance the host bookkeeping with the launches switched off and replay the stored graph.
+    A graph's selection or attention, whose tensors it points into, is held beside it; when another one (or none) has
+    taken its place, the next step lets go of both."""
 
     def __init__(self, eng: "LayeredCache", new_k, new_v, q, out, softmax_scale: Optional[float] = None):
         self.eng, self.args = eng, (new_k, new_v, q, out, softmax_scale)
-        self.graphs = {}
+        self.graphs = {}   # key: (graph, selections and attentions of all caches)
+        self.modes = (None, None)   # the folded cache's at the last step: they change in all caches together
 
     def _key(self):
         e, f = self.eng, self.eng.folded
@@ -528,18 +531,32 @@ class GraphedStepper:
                 recent = -1
             else:
                 recent = max(n // e.B - sc for n, sc in zip(e.host_lens * e.layers, f.host_scored))
-        fresh = None if f.selection is None else (f.selection.num_pages, f.selection.recent(e.host_lens * e.layers, e.B))
-        seen = None if f.attention is None else f.attention.started
-        return (f.seq_lens.data_ptr(), trig, e.fused, f.cached_scores, f.fused_evict, recent, fresh, seen)
+        fresh = None if f.selection is None else (id(f.selection), f.selection.recent(e.host_lens * e.layers, e.B))
+        seen = None if f.attention is None else (id(f.attention), f.attention.decay, f.attention.started)
+        opts = f.evict_opts and tuple(getattr(f.evict_opts, name) for name, _ in f.evict_opts._fields_)
+        return (f.seq_lens.data_ptr(), trig, e.fused, f.cached_scores, f.fused_evict, recent, fresh, seen, opts)
+
+    def _forget(self):
+        """Drop the graphs that point into a selection or an attention that is no longer in use."""
+        f = self.eng.folded
+        if f.selection is self.modes[0] and f.attention is self.modes[1]:
+            return
+        self.modes = (f.selection, f.attention)
+        stale = [k for k, (_, of) in self.graphs.items() if any(m is not None and m is not now for m, now in zip(of, self.modes))]
+        if stale:
+            torch.cuda.synchronize()   # a replay may be on its way
+            for k in stale:
+                del self.graphs[k]
 
     def step(self) -> bool:
+        self._forget()
         key = self._key()
-        g = self.graphs.get(key)
+        g, _ = self.graphs.get(key, (None, None))
         if g is None:
             g = torch.cuda.CUDAGraph()
             with torch.cuda.graph(g):
                 trig = self.eng.decode_step(*self.args)
-            self.graphs[key] = g
+            self.graphs[key] = (g, [m for c in [self.eng.folded] + self.eng.per_layer for m in (c.selection, c.attention)])
         else:
             with host_only():
                 trig = self.eng.decode_step(*self.args)
