@@ -52,6 +52,12 @@ def triggers(host_lens, block_size: int, budget: int) -> List[bool]:
     return [n > 0 and n % block_size == 0 and n >= budget for n in host_lens]
 
 
+def evicts_within(n, tokens, block_size: int, budget: int) -> bool:
+    """Whether a sequence of n cached tokens that takes on so many more is to lose a page on the way."""
+    full = max(-(-max(n, budget) // block_size), 1) * block_size   # the first length from n on at which a page goes
+    return tokens > full - n
+
+
 @dataclass
 class PagedCache:
     """Device-side state of one paged KV cache (one layer, or several layers folded into num_seqs).
@@ -256,7 +262,8 @@ class PagedCache:
         """Append the drafts path[s][:path_lens[s]] (path [S, P] and path_lens [S] int32 on the device, host_path_lens the latter's
         values, at most P; every named draft exists).  The effect on the cache is that of as many single steps: before a token joins a
         sequence whose newest page is full and which is at budget, a page of that sequence goes, and of no other: a sequence
-        whose path ends with a full page keeps its pages until it goes on."""
+        whose path ends with a full page keeps its pages until it goes on.  With evict_by_attention a decode step has to come before
+        a path on which pages go (a tree leaves no weights); what is refused leaves the cache as it was."""
         B = self.desc.block_size
         left = [int(n) for n in host_path_lens]
         if len(left) != len(self.host_lens) or min(left) < 0 or max(left) > path.shape[-1]:
@@ -264,6 +271,9 @@ class PagedCache:
         room = self.desc.max_blocks * B
         if self.budget > room and any(n + m > room for n, m in zip(self.host_lens, left)):
             raise ValueError("the path is longer than what is left of a table row, and nothing is evicted below the budget")
+        if self.attention is not None and not self.attention.started and any(evicts_within(n, m, B, self.budget)
+                                                                             for n, m in zip(self.host_lens, left)):
+            raise RuntimeError("no attention step before the first eviction: nothing to choose a page by")
         path_done = torch.zeros_like(path_lens)
         while any(left):
             trig = self.triggers()
@@ -336,7 +346,8 @@ class PagedCache:
 
     def evict_by_attention(self, decay=1.0):
         """From now on `scores` hold the attention weight of each page (decay: what is left of it a step later), and the page with
-        the least goes.  The choice, protected pages and shared heads are evict_opts'; without them the newest page is protected."""
+        the least goes.  The choice, protected pages and shared heads are evict_opts'; without them the newest page is protected.
+        The weights are those of decode steps (one that has to evict before there are any looks with its own queries first)."""
         if self.selection is not None:
             raise ValueError("attention weights are kept over all pages, not over selected ones")
         self.attention = Attention(float(decay), pe.alloc_workspace(pe.PE_OP_DECODE_WEIGHTS, self.desc, device=self.k_pool.device))
@@ -485,9 +496,11 @@ class LayeredCache:
         """PagedCache.accept_path in every layer at once: k_draft, v_draft [layers, S, T, Hk, D]; path [S, P], path_lens [S]."""
         f = self.folded
         f.host_lens = self.host_lens * self.layers
-        f.accept_path(k_draft.flatten(0, 1), v_draft.flatten(0, 1), path.repeat(self.layers, 1), path_lens.repeat(self.layers),
-                      list(host_path_lens) * self.layers)
-        self.host_lens = f.host_lens[:self.S]
+        try:
+            f.accept_path(k_draft.flatten(0, 1), v_draft.flatten(0, 1), path.repeat(self.layers, 1), path_lens.repeat(self.layers),
+                          list(host_path_lens) * self.layers)
+        finally:
+            self.host_lens = f.host_lens[:self.S]
 
     def select_pages(self, num_pages):
         """PagedCache.select_pages in every layer; the pool's bounds are kept by one launch for all of them."""
