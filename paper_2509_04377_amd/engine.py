@@ -161,7 +161,7 @@ class PagedCache:
             self.bound_pages()
         if any(trig):
             if self.attention is not None and not self.attention.started:   # nothing seen yet: this step's queries look first
-                self.paged_decode_weights(q, out, softmax_scale)
+                self.paged_decode_weights(q, torch.empty_like(q), softmax_scale)   # (out may be q, which is needed again)
             self.score_and_evict()
             self.evicted(trig)
         self.append_and_attend(new_k, new_v, q, out, softmax_scale, fused)
@@ -452,7 +452,7 @@ class LayeredCache:
         if any(trig):
             if f.attention is not None and not f.attention.started:
                 for l, c in enumerate(self.per_layer):
-                    c.paged_decode_weights(q[l], out[l], softmax_scale)
+                    c.paged_decode_weights(q[l], torch.empty_like(q[l]), softmax_scale)   # (out may be q, which is needed again)
                 f.attention.started = True
             f.score_and_evict()
             f.evicted(trig * self.layers)
