@@ -358,7 +358,8 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
  *     `out` may be q itself and must not otherwise overlap what is read.  desc->decode_splits is the number of splits of a row here too (0: the
  *     library's choice; with many query rows the sequences share them out by their lengths, so that an output's last bits can depend on
  *     the other sequences' lengths); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
- *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29, at most 65536 KV heads.
+ *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29, at most 65536 KV heads; PE_ERR_UNSUPPORTED too where a launch
+ *     would take 2^32 threads in a row (with several splits 64 for a query row, of which a sequence and KV head has a multiple of four).
  *     workspace: pe_workspace_bytes(PE_OP_TREE_DECODE, desc, num_drafts) (split partials).
  *     shared: block_table [S][max_blocks].
  */
@@ -377,7 +378,8 @@ int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q,
  * A draft may be named more than once.  The path ends in front of an entry outside 0..num_drafts-1.
  * k_draft, v_draft: as in (5), not overlapping the pools.  path: [S][max_path] int32.  path_lens, path_done: [S] int32 (path_done
  * is 0 for a new path; values of path_lens above max_path count as max_path).  spare, spare_used, freed_phys as in
- * pe_append_kv; a sequence with seq_lens[s] >= max_blocks*B is left untouched.  At most 65536 KV heads.
+ * pe_append_kv; a sequence with seq_lens[s] >= max_blocks*B is left untouched.  At most 65536 KV heads and
+ * 2^23 - 1 sequences (else PE_ERR_UNSUPPORTED).
  * shared: as in pe_append_kv.
  */
 int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_draft, const void* v_draft, const int32_t* path,
@@ -395,6 +397,7 @@ int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_
  *     bounds[page][0][d] = min_i K[i][d], bounds[page][1][d] = max_i K[i][d] over the page's B tokens
  * for the pages block_table[s][hk][j], max(0, n - recent) <= j < n = seq_lens[s] / B, of every row; recent = 0: for every full
  * page.  Others are left as they were.  bounds: [num_phys_blocks][2][D], 16-byte aligned; shared: [num_phys_blocks][2][Hk][D].
+ * (max_blocks, or `recent` where that is less, times a token's 16-byte chunks of all heads of a page: at most 2^32 - 256, else PE_ERR_UNSUPPORTED.)
  *
  * pe_select_pages: of a row with n = ceil(seq_lens[s] / B) pages, the newest one (full or not) and the min(num_pages, n) - 1
  * others with the highest scores (ties: lowest index), in their order.  The score of page j is
@@ -403,7 +406,7 @@ int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_
  * Only the bounds of full pages other than the newest are read, and those only of rows with more than num_pages pages.
  *     q: [S][Hq][D].  block_table_out: [S][Hk][num_pages], the physical pages, -1 padded.  seq_lens_out: [S], the tokens in
  * them (the same for all heads).  page_idx_out: NULL, or [S][Hk][num_pages], their logical indices in block_table, ascending, -1
- * padded.  The outputs must not overlap block_table or seq_lens.
+ * padded.  The outputs must not overlap block_table or seq_lens.  max_blocks: at most 2^27 - 8 (else PE_ERR_UNSUPPORTED).
  *     workspace: pe_workspace_bytes(PE_OP_SELECT_PAGES, desc, 0) (the scores).
  *     shared: one selection per sequence, over the query heads of all KV heads; block_table_out, page_idx_out [S][num_pages].
  */
@@ -428,7 +431,8 @@ int pe_select_pages(const pe_cache_desc* desc, const void* q, const void* bounds
  *     weights_out itself; no other overlap with it, with q or with out.  out may be q itself.
  *     workspace: pe_workspace_bytes(PE_OP_DECODE_WEIGHTS, desc, 0).  desc->decode_splits is the number of splits of a row (0: the
  *     library's choice; more are used where a split would have over 61440 / (Hq/Hk) tokens of the table; tables for which 256 of
- *     those are too few are PE_ERR_UNSUPPORTED), the other decode_* fields are not looked at.  At most 65536 KV heads.
+ *     those are too few are PE_ERR_UNSUPPORTED), the other decode_* fields are not looked at.  At most 65536 KV heads;
+ *     PE_ERR_UNSUPPORTED too where a launch would take 2^32 threads in a row (256 for each sequence, KV head and split).
  *     shared: block_table [S][max_blocks]; the weights keep their shape (one row a head; evictions take the head mean).
  */
 int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void* k_pool, const void* v_pool,

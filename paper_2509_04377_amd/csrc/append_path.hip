@@ -11,7 +11,7 @@
 namespace pe {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = kPathThreads;
 constexpr int kMostTokens = 128;  // of a page
 
 __global__ __launch_bounds__(kThreads) void append_path_kernel(const uint4* __restrict__ k_draft, const uint4* __restrict__ v_draft,

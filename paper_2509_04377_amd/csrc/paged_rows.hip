@@ -42,6 +42,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
+static_assert(kThreads == kRowsThreads && kWaves == kMergeRows, "what the host counts with");
 
 // Row geometry: elements of a 16-byte K chunk, chunks a lane loads of a token, elements of V a lane loads of a token.
 template <typename T, int D>

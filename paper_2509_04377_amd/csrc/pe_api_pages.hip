@@ -15,6 +15,9 @@ int pe_page_bounds(const pe_cache_desc* desc, const void* k_pool, const int32_t*
   if (st != PE_OK) return st;
   if (!k_pool || !block_table || !seq_lens || !bounds_inout || recent < 0) return PE_ERR_INVALID_ARG;
   if (!aligned(k_pool, 16) || !aligned(bounds_inout, 16)) return PE_ERR_INVALID_ARG;
+  const int64_t chunks = (int64_t)desc->head_dim * (desc->dtype == PE_F32 ? 4 : 2) / 16 * (desc->layout == PE_LAYOUT_SHARED ? desc->num_kv_heads : 1);
+  if (chunks > 0x7fffffffLL || !one_launch(pe::bounds_groups(pe::bounds_per_row(recent, desc->max_blocks), (int)chunks), pe::kBoundsThreads))
+    return PE_ERR_UNSUPPORTED;
   pe::BoundsArgs a;
   a.k_pool = k_pool;
   a.block_table = block_table;
@@ -38,6 +41,7 @@ int pe_select_pages(const pe_cache_desc* desc, const void* q, const void* bounds
   if (st != PE_OK) return st;
   if (!q || !bounds || !block_table || !seq_lens || !block_table_out || !seq_lens_out || num_pages < 1) return PE_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(bounds, 16)) return PE_ERR_INVALID_ARG;
+  if (!one_launch(((int64_t)desc->max_blocks + pe::kFewestScored - 1) / pe::kFewestScored, pe::kScoreThreads)) return PE_ERR_UNSUPPORTED;
   const size_t rows = desc->layout == PE_LAYOUT_SHARED ? (size_t)desc->num_seqs : (size_t)desc->num_seqs * desc->num_kv_heads;
   const size_t in = rows * desc->max_blocks * 4, out = rows * num_pages * 4, lens = (size_t)desc->num_seqs * 4;
   // the rows of a sequence read what another one has already written

@@ -23,8 +23,11 @@ int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q,
     return PE_ERR_INVALID_ARG;
   if (!finite(softmax_scale)) return PE_ERR_INVALID_ARG;
   if (desc->num_kv_heads > 65536) return PE_ERR_UNSUPPORTED;
-  // the merge of the splits has a workgroup for every four query rows
   if ((int64_t)desc->num_seqs * desc->num_q_heads * num_drafts > 0x7fffffffLL / 4) return PE_ERR_UNSUPPORTED;
+  const int rows = num_drafts * (desc->num_q_heads / desc->num_kv_heads), splits = pe::tree_splits_of(desc, num_drafts);
+  const int tile_rows =
+      pe::tree_tile_rows(desc->dtype == PE_BF16, (int64_t)desc->num_seqs * desc->num_kv_heads, rows, compute_units());
+  if (!pe::rows_launches(desc, tile_rows, rows, splits, false)) return PE_ERR_UNSUPPORTED;
   const size_t head = (size_t)desc->num_seqs * num_drafts * desc->head_dim * (desc->dtype == PE_F32 ? 4 : 2);
   const size_t o = head * desc->num_q_heads, kv = head * desc->num_kv_heads;
   if ((out != q && overlap(out, o, q, o)) || overlap(out, o, k_draft, kv) || overlap(out, o, v_draft, kv)) return PE_ERR_INVALID_ARG;
@@ -52,11 +55,10 @@ int pe_tree_decode(const pe_cache_desc* desc, int32_t num_drafts, const void* q,
   a.max_blocks = desc->max_blocks;
   a.is_bf16 = desc->dtype == PE_BF16;
   a.shared = desc->layout == PE_LAYOUT_SHARED;
-  a.tile_rows = pe::tree_tile_rows(a.is_bf16, (int64_t)desc->num_seqs * desc->num_kv_heads,
-                                   num_drafts * (desc->num_q_heads / desc->num_kv_heads), compute_units());
-  a.splits = pe::tree_splits_of(desc, num_drafts);
-  if (pe::tree_shares_splits(desc, num_drafts, a.splits))
-    a.shares = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + pe::tree_partials_bytes(desc, num_drafts, a.splits));
+  a.tile_rows = tile_rows;
+  a.splits = splits;
+  if (pe::tree_shares_splits(desc, num_drafts, splits))
+    a.shares = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + pe::tree_partials_bytes(desc, num_drafts, splits));
   return pe::launch_paged_rows(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PE_OK : PE_ERR_HIP;
 }
 
@@ -72,7 +74,8 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
     return PE_ERR_INVALID_ARG;
   if (!finite(softmax_scale) || !(decay >= 0.f && decay <= 1.f)) return PE_ERR_INVALID_ARG;
   const int splits = pe::weights_splits_of(desc);
-  if (desc->num_kv_heads > 65536 || splits == 0) return PE_ERR_UNSUPPORTED;
+  if (desc->num_kv_heads > 65536 || splits == 0 || !pe::rows_launches(desc, 16, desc->num_q_heads / desc->num_kv_heads, splits, true))
+    return PE_ERR_UNSUPPORTED;
   const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * (desc->dtype == PE_F32 ? 4 : 2);
   const size_t w = (size_t)desc->num_seqs * desc->num_kv_heads * desc->max_blocks * 4;
   if ((out != q && overlap(out, o, q, o)) || overlap(weights_out, w, out, o) || overlap(weights_out, w, q, o)) return PE_ERR_INVALID_ARG;
@@ -113,7 +116,7 @@ int pe_append_path(const pe_cache_desc* desc, int32_t num_drafts, const void* k_
   const int st = check_desc(desc);
   if (st != PE_OK) return st;
   if (num_drafts < 1 || max_path < 1 || n_spare < 1) return PE_ERR_INVALID_ARG;
-  if (desc->num_kv_heads > 65536) return PE_ERR_UNSUPPORTED;
+  if (desc->num_kv_heads > 65536 || !one_launch(desc->num_seqs, pe::kPathThreads)) return PE_ERR_UNSUPPORTED;
   if (!k_draft || !v_draft || !path || !path_lens || !path_done || !k_pool || !v_pool || !block_table || !seq_lens || !freed_phys ||
       !spare || !spare_used)
     return PE_ERR_INVALID_ARG;

@@ -62,6 +62,9 @@ inline int compute_units() {
   return n;
 }
 
+// A row of workgroups has fewer than 2^32 threads.
+inline bool one_launch(int64_t workgroups, int threads) { return workgroups <= ((1LL << 32) - 1) / threads; }
+
 inline int check_workspace(const void* ws, size_t have, size_t need) {
   if (need == 0) return PE_OK;
   if (ws == nullptr || have < need || !aligned(ws, 256)) return PE_ERR_WORKSPACE;

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "pe_check.h"
+#include "pe_place.h"
 
 namespace pe {
 
@@ -94,6 +95,16 @@ inline int tree_splits(bool is_bf16, int64_t kv_rows, int rows, int64_t tokens, 
     for (int64_t parts = 2; parts <= 3; ++parts)
       if (turns(parts) * 4 <= turns(1) * parts * 3 && turns(parts) * best < turns(best) * parts) best = parts;
   return (int)best;
+}
+
+// Whether the attention and the merge of its splits are launches that the runtime takes (threads of paged_rows.hip, and of tree_wide.hip's two
+// waves for every 64 rows; the merge has a workgroup for four query rows, that of page weights one for a row).
+constexpr int kRowsThreads = 256, kPathThreads = 512, kMergeRows = 4;
+inline bool rows_launches(const pe_cache_desc* d, int tile_rows, int rows, int splits, bool weights) {
+  PlaceGrid grid;
+  if (!place_grid(d->num_seqs, d->num_kv_heads, splits * ((rows + tile_rows - 1) / tile_rows), true, &grid)) return false;
+  const int64_t kv_rows = (int64_t)d->num_seqs * d->num_kv_heads, merges = weights ? kv_rows : kv_rows * ((rows + kMergeRows - 1) / kMergeRows);
+  return host::one_launch(grid.x, tile_rows == kWideRows ? kWideRows * 2 : kRowsThreads) && (splits == 1 || host::one_launch(merges, kRowsThreads));
 }
 
 // Page weights: the parts of a split lie in LDS, 8 bytes for every 16 tokens and query head, beside what the waves' states take.

@@ -20,6 +20,14 @@ struct BoundsArgs {
 };
 hipError_t launch_page_bounds(const BoundsArgs& a, hipStream_t stream);
 
+// Workgroups for the pages of a row: a thread has 16 bytes of every token of one page.
+constexpr int kBoundsThreads = 256;
+inline int64_t bounds_groups(int per_row, int chunks) { return ((int64_t)per_row * chunks + kBoundsThreads - 1) / kBoundsThreads; }
+inline int bounds_per_row(int recent, int max_blocks) { return recent > 0 && recent < max_blocks ? recent : max_blocks; }
+
+// Pages of a row that can be scored: in workgroups of eight pages (fp32, D = 128, several heads a decision) the fewest.
+constexpr int kScoreThreads = 256, kFewestScored = 8;
+
 struct SelectArgs {
   const void* q;
   const void* bounds;

@@ -15,6 +15,7 @@ namespace pe {
 namespace {
 
 constexpr int kWaves = 4;
+static_assert(kWaves * kWave == kBoundsThreads && kWaves * kWave == kScoreThreads, "what the host counts with");
 
 // ---- bounds --------------------------------------------------------------------------------------------------------------
 // A lane has 16 bytes of every token of one page (head-shared: of one head too), so nothing is exchanged between lanes, and the lanes of
@@ -494,9 +495,8 @@ hipError_t launch_bounds_as(const BoundsArgs& a, hipStream_t stream) {
   while ((1 << log2_block) < a.block_size) ++log2_block;
   const int rows_per_seq = a.shared ? 1 : a.num_kv_heads;
   const int chunks = a.head_dim * (int)sizeof(T) / 16 * (a.shared ? a.num_kv_heads : 1);
-  const int per_row = a.recent > 0 && a.recent < a.max_blocks ? a.recent : a.max_blocks;
-  const int64_t units = (int64_t)per_row * chunks, rows = (int64_t)a.num_seqs * rows_per_seq;
-  const int64_t groups = (units + kWaves * kWave - 1) / (kWaves * kWave);
+  const int per_row = bounds_per_row(a.recent, a.max_blocks);
+  const int64_t rows = (int64_t)a.num_seqs * rows_per_seq, groups = bounds_groups(per_row, chunks);
   const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / groups;  // rows of a launch (of fewer than 2^32 threads)
   if (some < 1) return hipErrorInvalidValue;
   for (int64_t row = 0; row < rows; row += some) {
@@ -523,6 +523,7 @@ void launch_select_of(const SelectArgs& a, int rows_per_seq, int log2_block, int
 template <typename T, int D, int NL, bool HEADS>
 hipError_t launch_scores(const SelectArgs& a, int rows_per_seq, int heads, int group, int log2_block, int64_t rows, hipStream_t stream) {
   constexpr int64_t kEach = Scorer<T, D, NL>::kPages * (HEADS ? 1 : kWaves);
+  static_assert(kEach >= kFewestScored, "what the host counts with");
   const int64_t parts = (a.max_blocks + kEach - 1) / kEach;
   const int64_t some = ((1LL << 32) - 1) / (kWaves * kWave) / parts;
   if (some < 1) return hipErrorInvalidValue;

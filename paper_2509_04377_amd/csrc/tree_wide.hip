@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kTile = kWideTile;
 constexpr int WAVES = kWideRows / 32, NT = WAVES * kWave;
+static_assert(NT == kWideRows * 2, "what the host counts with");
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
