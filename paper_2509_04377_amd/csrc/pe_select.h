@@ -28,6 +28,18 @@ inline int bounds_per_row(int recent, int max_blocks) { return recent > 0 && rec
 // Pages of a row that can be scored: in workgroups of eight pages (fp32, D = 128, several heads a decision) the fewest.
 constexpr int kScoreThreads = 256, kFewestScored = 8;
 
+// Scores of rows of one head a decision: sixteen loads a wave, in registers that leave four waves a SIMD, where there are two such workgroups a
+// compute unit or more; eight where there are fewer, or several heads a decision.  (bf16, D = 128, the whole call with sixteen / eight: 32
+// rows of 4096 pages 25.8 / 27.6 us, 256 of 1024 39.6 / 43.4, 8 of 4096 17.0 / 17.2, 8 of 1024 11.7 / 10.6; eight heads a decision, 2 rows of
+// 2048 22.0 / 16.0.)
+constexpr int scored_by_sixteen(int head_dim, bool is_bf16) {  // pages of a workgroup: a load is 16 bytes a lane, a page's bounds 2 D elements
+  return kScoreThreads * 16 * 16 / (2 * head_dim * (is_bf16 ? 2 : 4));
+}
+inline bool many_scores(int64_t rows, int max_blocks, int head_dim, bool is_bf16, int compute_units) {
+  const int64_t each = scored_by_sixteen(head_dim, is_bf16);
+  return rows * ((max_blocks + each - 1) / each) >= 2 * compute_units;
+}
+
 struct SelectArgs {
   const void* q;
   const void* bounds;

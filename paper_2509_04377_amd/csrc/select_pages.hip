@@ -517,9 +517,6 @@ void launch_select_of(const SelectArgs& a, int rows_per_seq, int log2_block, int
                        row);
 }
 
-// Sixteen loads a wave, in registers that leave four waves a SIMD, where there are two such workgroups a compute unit or more; eight where there
-// are fewer, or several heads a decision.  (bf16, D = 128, the whole call with sixteen / eight: 32 rows of 4096 pages 25.8 / 27.6 us, 256 of 1024
-// 39.6 / 43.4, 8 of 4096 17.0 / 17.2, 8 of 1024 11.7 / 10.6; eight heads a decision, 2 rows of 2048 22.0 / 16.0.)
 template <typename T, int D, int NL, bool HEADS>
 hipError_t launch_scores(const SelectArgs& a, int rows_per_seq, int heads, int group, int log2_block, int64_t rows, hipStream_t stream) {
   constexpr int64_t kEach = Scorer<T, D, NL>::kPages * (HEADS ? 1 : kWaves);
@@ -552,11 +549,11 @@ hipError_t launch_select_as(const SelectArgs& a, hipStream_t stream) {
     return hipGetLastError();
   }
   if (a.max_blocks > a.pages && a.pages > 1) {
+    static_assert(Scorer<T, D, 16>::kPages * kWaves == scored_by_sixteen(D, sizeof(T) == 2), "what the rule counts with");
     hipError_t e;
-    constexpr int64_t kEach16 = Scorer<T, D, 16>::kPages * kWaves;
     if (heads > 1)
       e = launch_scores<T, D, 8, true>(a, rows_per_seq, heads, group, log2_block, rows, stream);
-    else if (rows * ((a.max_blocks + kEach16 - 1) / kEach16) >= 2 * host::compute_units())
+    else if (many_scores(rows, a.max_blocks, D, a.is_bf16, host::compute_units()))
       e = launch_scores<T, D, 16, false>(a, rows_per_seq, heads, group, log2_block, rows, stream);
     else
       e = launch_scores<T, D, 8, false>(a, rows_per_seq, heads, group, log2_block, rows, stream);
