@@ -357,7 +357,7 @@ int pe_append_paged_decode_layers(const pe_cache_desc* desc, int32_t num_layers,
  *     draft may be anything.  A draft in use is finite even where no mask names it.
  *     `out` may be q itself and must not otherwise overlap what is read.  desc->decode_splits is the number of splits of a row here too (0: the
  *     library's choice; with many query rows the sequences share them out by their lengths, so that an output's last bits can depend on
- *     the other sequences' lengths); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
+ *     the other sequences' lengths: not with one split, where they depend on the sequence alone as long as the shape is the same); the other decode_* fields are not looked at.  num_drafts: 1..PE_MAX_DRAFTS (else PE_ERR_INVALID_ARG
  *     below and PE_ERR_UNSUPPORTED above), S * Hq * num_drafts < 2^29, at most 65536 KV heads; PE_ERR_UNSUPPORTED too where a launch
  *     would take 2^32 threads in a row (with several splits 64 for a query row, of which a sequence and KV head has a multiple of four).
  *     workspace: pe_workspace_bytes(PE_OP_TREE_DECODE, desc, num_drafts) (split partials).

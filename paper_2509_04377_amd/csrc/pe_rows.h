@@ -81,7 +81,12 @@ inline int tree_tile_rows(bool is_bf16, int64_t kv_rows, int rows, int compute_u
 // D = 128, one query with weights: rows of 4096 tokens, 136 of them 60.3 / 54.4, 160 64.0 / 61.9, 288 135 / 115, 320 137 / 122, 384 151 / 139;
 // the same down to half the length, 8192: 110 / 85.8, 114 / 96.9, 203 / 174, 212 / 183, 234 / 215.  Not with rows of 1024: 136 of them
 // 18.5 / 21.9.  192 rows, which only four parts would even out: 69.8 / 72.8.  Rows of 700 tokens in such tables, eight drafts: 136 of them
-// 20.3 / 23.3, 288 35.2 / 39.2.)
+// 20.3 / 23.3, 288 35.2 / 39.2.  136, 288 and 384 rows of 4096 tokens, and of half to full 8192: eight drafts x 4 heads 65.1 / 58.6, 140 / 123,
+// 157 / 151, and 113 / 91.7, 206 / 182, 235 / 227; D = 64, weights, 33.1 / 31.8, 75.5 / 67.7, 84.2 / 81.5, and 64.5 / 53.4, 115 / 100, 133 / 126;
+// fp32, weights, 110 / 104, 263 / 216, 285 / 261, and 213 / 156, 394 / 325, 446 / 404; fp32, D = 64, eight drafts x 4 heads 93.3 / 66.7,
+// 163 / 132, 168 / 158, and 172 / 102, 249 / 196, 270 / 236.  Not the form with 256 query rows, whose records are many; 160 rows, 64 drafts x 4
+// heads, one / two / three: 1024 tokens, half to full 55.2 / 74.0 / 68.0, 2048 94.1 / 124 / 108, 4096 167 / 202 / 168; 240 rows of 4096 216 / 234 /
+// 246.  Where its rows are long and of unequal length three would help: 4096, half to full, 160 rows 156 / 168 / 140, 136 rows 156 / 156 / 126.)
 constexpr int kLongTokens = 4096;
 inline int tree_splits(bool is_bf16, int64_t kv_rows, int rows, int64_t tokens, int compute_units) {
   const int tile = tree_tile_rows(is_bf16, kv_rows, rows, compute_units);

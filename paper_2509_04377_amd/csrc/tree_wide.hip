@@ -2,7 +2,7 @@
 //
 // The products count here, not the traffic: 256 query rows ask for 256 operations a byte of the cache.  (64 drafts x 4 heads over eight caches of
 // 4001 to 8192 tokens of D = 128, eight KV heads: 88 us and 10 for the merge, 500 TFLOP/s and half as many again for the low terms; the matrix
-// units are busy for 45 % of it at the 1.8 GHz that are left of the clock.)  A workgroup owns 32 query rows a
+// units are busy for 48 % of it, as are the vector units, at the 1.7 GHz that are left of the clock.)  A workgroup owns 32 query rows a
 // wave and one split of the tokens (tiles of 64, the drafts are the last one); K and V of a tile go through LDS once for all its waves,
 // which read them as operands of the 32 x 32 x 16 products.  The tile behind the next one is on its way to registers while one is computed
 // out of one half of LDS and the next is put into the other; one barrier a tile.

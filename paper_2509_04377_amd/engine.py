@@ -249,7 +249,8 @@ class PagedCache:
     # ---- verification of drafted tokens ----
 
     def tree_decode(self, q, k_draft, v_draft, tree_mask, out, draft_lens=None, softmax_scale=None, workspace=None):
-        """Attention of q [S, T, Hq, D] over the cache and the drafts that tree_mask [S, T] names (int64 words); the cache is read only."""
+        """Attention of q [S, T, Hq, D] over the cache and the drafts that tree_mask [S, T] names (int64 words); the cache is read only,
+        and all of it also where steps attend to selected pages."""
         if softmax_scale is None:
             softmax_scale = float(self.desc.head_dim) ** -0.5
         T = int(q.shape[1])
