@@ -9,7 +9,9 @@
  *      its newest block has filled, and compacting the block table (Alg. 3);
  *   3. the single-query paged attention that reads what is left (Eq. 1; Alg. 3 "PagedAttention").
  * Beside it, on the same cache: attention of trees of drafted tokens and the accepted ones' way into the cache (5), attention
- * over the pages that a query can need most (6), and attention that keeps the weight each page got, to evict by (7).
+ * over the pages that a query can need most (6), and attention that keeps the weight each page got, to evict by (7).  What goes into a
+ * cache: tables, slots and positions from request lengths (8) and rotary positions (9).  And a cache in 8 bits, its pages (10) and the
+ * attention that reads it (11).
  *
  * Granularity: every decision is taken per ROW = one (sequence, KV head).  A row owns one row of the
  * block table and its own pages; a page holds B x D elements of K (and a sibling page of V, same
@@ -64,7 +66,8 @@ typedef enum {
   PE_OP_APPEND_PAGED_DECODE = 4,
   PE_OP_TREE_DECODE = 5,
   PE_OP_SELECT_PAGES = 6,
-  PE_OP_DECODE_WEIGHTS = 7
+  PE_OP_DECODE_WEIGHTS = 7,
+  PE_OP_QUANT_DECODE = 8
 } pe_op;
 
 /* Cache layout (Sec. 2.4 leaves the granularity open).
@@ -439,6 +442,129 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
                             const int32_t* block_table, const int32_t* seq_lens, float softmax_scale, float decay,
                             const float* weights_in, float* weights_out, void* out, void* workspace, size_t workspace_bytes,
                             void* stream);
+
+/*
+ * (8) The plan of a step: which pages, slots and positions the new tokens of each sequence get, from lengths that are on the device, so
+ *     that neither a batch of prompts nor a decode step waits for the host.  One launch.
+ *     Sequence s holds seq_lens[s] tokens in ceil(seq_lens[s] / B) pages of its row(s) of block_table and brings n = max(new_lens[s], 0)
+ *     more (packed: token i of s is token cu_seqlens_out[s] + i of the batch).  It is to hold after = seq_lens[s] + n tokens, or where
+ *     budget_tokens > 0 (a multiple of B) no more than budget_tokens (never less than it holds: what pe_prefill_prune keeps of a prompt).  Every one of its
+ *     rows gets the pages that this takes beyond those it has, and a sequence that begins (seq_lens[s] == 0, n > 0) n_spare pages
+ *     more a row into `spare` (NULL with n_spare 0: none), the list that pe_append_kv takes pages from.  Pages are dealt row by row, in the order
+ *     of the sequences: free_pages[free_used[0]], free_pages[free_used[0] + 1], ..., first those of the table, then the spare ones.
+ *     A sequence whose pages the list does not hold, or whose table row is too short, is left as it was, and so is every later one that
+ *     needs pages where it was the list: seq_lens_out[s] = seq_lens[s], its tokens' slots -1.
+ *     block_table: in/out, only the new entries are written.  seq_lens_out: [S], what each sequence holds then.  free_used_out: [1], the pages
+ *     dealt so far (free_used[0] taken as 0 where it is less, as num_free where it is more).
+ *     cu_seqlens_out: NULL, or [S+1], prefix sums of the n.  positions_out: NULL, or [total_tokens]: first_positions[s] + i, or where
+ *     first_positions is NULL (nothing has been evicted) seq_lens[s] + i.  slots_out: NULL, or [total_tokens][Hk] 64-bit: page * B + slot of
+ *     each token in each of its rows, -1 where the sequence was left as it was, where its table has no page, or where the budget leaves
+ *     less than all of its tokens (which those are the prune decides).  total_tokens: the room in these two, 0..2^31 - 1; what is behind
+ *     the last token gets position 0 and slot -1 (a padded batch), tokens that find no room are not written.
+ *     The outputs must not overlap the inputs or one another.  At most 65536 KV heads (else PE_ERR_UNSUPPORTED).
+ *     shared: block_table [S][max_blocks], spare [S][n_spare], slots_out [total_tokens].
+ */
+int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int32_t* new_lens, const int32_t* first_positions,
+                   int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free, const int32_t* free_used,
+                   int32_t* block_table, int32_t* spare, int32_t n_spare, int32_t* seq_lens_out, int32_t* free_used_out,
+                   int32_t* cu_seqlens_out, int32_t* positions_out, int64_t* slots_out, void* stream);
+
+/*
+ * (9) Rotary positions.  The first R = rotary_dim elements of a head are R/2 pairs, (i, i + R/2) (PE_ROPE_HALF) or (2i, 2i + 1)
+ *     (PE_ROPE_INTERLEAVED), and pair i of a token at position p is turned by the angle p f_i:
+ *        y_a = m (x_a cos(p f_i) - x_b sin(p f_i)),  y_b = m (x_b cos(p f_i) + x_a sin(p f_i)),   f_i = base^(-2i/R);
+ *     the elements behind them are copied.  For contexts longer than those a model was trained with
+ *        PE_ROPE_LINEAR    f_i / factor;
+ *        PE_ROPE_BY_PARTS  with r = original f_i / 2 pi (turns within the original context) and g = clamp((r - low) / (high - low), 0, 1):
+ *                          f_i (g + (1 - g) / factor) -- fast pairs as they are, slow ones as LINEAR.
+ *     and m = magnitude (1: none).  transpose != 0: angles -p f_i, the gradient of the inputs from that of the outputs (with the same m).
+ *     Computed in 32 bits from angles that are exact modulo a turn up to the last of 64 bits at any position, rounded once to desc->dtype.
+ *
+ * pe_rope_init fills a caller's structure on the host, once for a model: 1 <= rotary_dim / 2 <= 64, rotary_dim even; base > 1; factor >= 1;
+ * BY_PARTS: 0 <= low < high, original > 0 (not looked at otherwise); magnitude > 0; all finite.  Its fields are the library's.
+ *
+ * pe_rotate turns the queries and keys of num_tokens tokens (0: nothing to do) and, where slots are given, stores the turned keys and the
+ * values into the pages: token t of KV head h goes to slot slots[t][h] of the pools, counted in tokens (page * B + slot, as (8) gives
+ * them); slots outside 0 .. P*B - 1 are left out.  Of desc only dtype, heads, head_dim, block_size, num_phys_blocks and layout matter.
+ *     q: [num_tokens][Hq][D], k, v: [num_tokens][Hk][D], each token's heads dense, consecutive tokens q_stride, k_stride, v_stride
+ *     elements apart (a projection's output may hold all three side by side).  positions: [num_tokens] int32, any value.
+ *     q, q_out both NULL: no queries; k NULL: no keys (then k_out, slots too).  q_out, k_out: strides of their own; in place
+ *     (the same address and stride) or without overlap.  slots NULL: nothing is stored (v, pools not looked at); given, k_out may be NULL.
+ *     The pools must not overlap the other tensors.  shared: slots [num_tokens] (all heads of a token lie in one slot).
+ *     D must be at least rotary_dim; at most 65536 query and key heads.
+ */
+typedef enum { PE_ROPE_HALF = 0, PE_ROPE_INTERLEAVED = 1 } pe_rope_pairs;
+typedef enum { PE_ROPE_PLAIN = 0, PE_ROPE_LINEAR = 1, PE_ROPE_BY_PARTS = 2 } pe_rope_scaling;
+typedef struct pe_rope {
+  int32_t rotary_dim;
+  int32_t pairs;
+  float magnitude;
+  int32_t filled;      /* set by pe_rope_init */
+  uint64_t turns[64];  /* f_i / 2 pi in units of 2^-64 turns */
+} pe_rope;
+int pe_rope_init(pe_rope* rope, int32_t rotary_dim, int32_t pairs, double base, int32_t scaling, double factor, double low,
+                 double high, double original, double magnitude);
+int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose, int64_t num_tokens, const int32_t* positions,
+              const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+              int64_t q_out_stride, void* k_out, int64_t k_out_stride, const int64_t* slots, void* k_pool, void* v_pool, void* stream);
+
+/*
+ * (10) A cache in 8 bits.  Full pages hold e4m3 numbers (1 sign, 4 exponent, 3 mantissa bits, largest 448) with one scale for K and one
+ *      for V of every page and head; a token's element is number * scale.  The newest page of a row, as long as it is not full, is kept
+ *      as it is, in desc->dtype, in the row's tail.  Tables, lengths, spare lists and scores are those of the other calls, and pe_evict_blocks*
+ *      act on them unchanged (a page is linked when its first token comes).
+ *         k, v: [num_phys_blocks][B][D] (shared: [num_phys_blocks][B][Hk][D]) of one byte.
+ *         scales: [num_phys_blocks][2] fp32 (shared: [num_phys_blocks][Hk][2]): K's and V's.
+ *         k_tail, v_tail: [S][Hk][B][D] in desc->dtype (both layouts).
+ *      k, v and tails 16-byte aligned, scales 8.
+ *      Rounding a page: with a = the largest magnitude of its B x D elements of a head, the scale is the least power of two (2^-126 at
+ *      least) with a <= 448 scale (a = 0: 1), so that element / scale is exact and is rounded once, to the nearest e4m3 number (ties to
+ *      even); a floating-point number's precision does not depend on the scale, and a power of two leaves every element that is read back
+ *      exact in bfloat16.  The attention (11) takes any scales.  Magnitudes are finite and at most 2^127.
+ *
+ * pe_quant_pages: of every row, the full pages j < seq_lens[s] / B of a cache in desc->dtype (k_pool, v_pool by src_table, as all other calls have
+ * them; its pages' number is not looked at) rounded into the pages block_table[..][j] of `cache`, and the tokens behind them copied to
+ * the tail's first slots (others are left).  src_table, block_table: [S][Hk][max_blocks], may be the same.  scores_out: NULL, or
+ * [S][Hk][max_blocks] as pe_score_blocks gives them: the scores of the pages before their rounding (fp32: within one step of an
+ * fp32 number, as sums may be taken in another order), +INF behind them.  Entries of -1 are passed over.
+ *
+ * pe_quant_append: a decode step's new token of every sequence, as pe_append_kv but that it goes to slot seq_lens[s] % B of the row's tail; where
+ * that fills the page, the page is rounded into page seq_lens[s] / B of the row and, with scores not NULL, its score is written to
+ * scores[s][hk][seq_lens[s] / B].  A new page is linked (slot 0) as in pe_append_kv.  seq_lens is only read; seq_lens_out must not overlap
+ * it; a sequence with seq_lens[s] >= max_blocks*B (or < 0) is left untouched, with its length.
+ * rope not NULL: the new key, and q into q_out (may be q; both [S][Hq][D]), are turned on the way as by (9), positions: [S].  rope NULL: keys
+ * as they come; positions, q, q_out are not looked at.
+ * new_k, new_v: [S][Hk][D], 16-byte aligned, as q and q_out.  At most 65536 KV heads, and S * Hk < 2^23 (else
+ * PE_ERR_UNSUPPORTED).
+ */
+typedef struct pe_quant_cache {
+  void* k;
+  void* v;
+  float* scales;
+  void* k_tail;
+  void* v_tail;
+} pe_quant_cache;
+int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* k_pool, const void* v_pool,
+                   const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table, float* scores_out, void* stream);
+int pe_quant_append(const pe_cache_desc* desc, const pe_quant_cache* cache, const pe_rope* rope, const int32_t* positions, const void* q,
+                    void* q_out, const void* new_k, const void* new_v, int32_t* block_table, const int32_t* seq_lens,
+                    int32_t* seq_lens_out, int32_t* freed_phys, const int32_t* spare, int32_t* spare_used, int32_t n_spare,
+                    float* scores, void* stream);
+
+/*
+ * (11) Paged decode attention over a cache in 8 bits: pe_paged_decode's sum over the seq_lens[s] tokens of row (s, hk), the full pages by
+ *      block_table with their scales and the last seq_lens[s] % B tokens from the tail.  fp32 accumulation; queries, numbers and softmax
+ *      weights enter the products with all of their bits; output rounded to desc->dtype.  seq_lens[s] == 0 gives zeros.  (Behind an eviction
+ *      that comes before the next append no page is unfinished: lengths are multiples of B then.)
+ *      q, the tokens attended to and the scales of their pages are finite; what lies behind a row's end may be anything.
+ *      `out` may be q itself and must not otherwise overlap what is read; it is the library's until the call's launches are through, as in
+ *      pe_paged_decode.
+ *      desc->decode_splits is the number of splits of a row (0: the library's choice), the other decode_* fields are not looked at.
+ *      workspace: pe_workspace_bytes(PE_OP_QUANT_DECODE, desc, 0).
+ *      shared: block_table [S][max_blocks].
+ */
+int pe_quant_decode(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* q, const int32_t* block_table,
+                    const int32_t* seq_lens, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

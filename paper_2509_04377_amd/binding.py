@@ -22,7 +22,9 @@ PE_ERR_INVALID_ARG, PE_ERR_UNSUPPORTED, PE_ERR_WORKSPACE, PE_ERR_HIP = -1, -2, -
 PE_F32, PE_BF16 = 0, 1
 PE_OP_SCORE_BLOCKS, PE_OP_PREFILL_PRUNE, PE_OP_EVICT_BLOCKS, PE_OP_PAGED_DECODE = 0, 1, 2, 3
 PE_OP_APPEND_PAGED_DECODE = 4
-PE_OP_TREE_DECODE, PE_OP_SELECT_PAGES, PE_OP_DECODE_WEIGHTS = 5, 6, 7
+PE_OP_TREE_DECODE, PE_OP_SELECT_PAGES, PE_OP_DECODE_WEIGHTS, PE_OP_QUANT_DECODE = 5, 6, 7, 8
+PE_ROPE_HALF, PE_ROPE_INTERLEAVED = 0, 1
+PE_ROPE_PLAIN, PE_ROPE_LINEAR, PE_ROPE_BY_PARTS = 0, 1, 2
 PE_MAX_DRAFTS = 64
 PE_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -31,7 +33,8 @@ EXPORTS = ["pe_workspace_bytes", "pe_status_string", "pe_version", "pe_decode_sp
            "pe_append_paged_decode", "pe_score_recent_blocks", "pe_evict_blocks_cached", "pe_evict_blocks_ex", "pe_score_evict",
            "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers",
            "pe_tree_decode", "pe_append_path", "pe_page_bounds", "pe_select_pages",
-           "pe_paged_decode_weights"]
+           "pe_paged_decode_weights", "pe_plan_tokens", "pe_rope_init", "pe_rotate",
+           "pe_quant_pages", "pe_quant_append", "pe_quant_decode"]
 
 
 class pe_cache_desc(ctypes.Structure):
@@ -45,6 +48,18 @@ class pe_cache_desc(ctypes.Structure):
 class pe_evict_opts(ctypes.Structure):
     _fields_ = [("policy", ctypes.c_int32), ("protect_first", ctypes.c_int32), ("protect_last", ctypes.c_int32),
                 ("share_heads", ctypes.c_int32), ("cached_scores", ctypes.c_int32)]
+
+
+class pe_rope(ctypes.Structure):
+    """Filled by make_rope()."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("magnitude", ctypes.c_float), ("filled", ctypes.c_int32),
+                ("turns", ctypes.c_uint64 * 64)]
+
+
+class pe_quant_cache(ctypes.Structure):
+    """Made by make_quant_cache(), which keeps the tensors alive beside it."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("k_tail", ctypes.c_void_p),
+                ("v_tail", ctypes.c_void_p)]
 
 
 PE_POLICY_LOWEST_SCORE, PE_POLICY_OLDEST = 0, 1
@@ -149,6 +164,19 @@ def lib():
         L.pe_select_pages.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.pe_paged_decode_weights.restype = ctypes.c_int
         L.pe_paged_decode_weights.argtypes = [dp, vp, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+        dbl, rp, cp = ctypes.c_double, ctypes.POINTER(pe_rope), ctypes.POINTER(pe_quant_cache)
+        L.pe_plan_tokens.restype = ctypes.c_int
+        L.pe_plan_tokens.argtypes = [dp, vp, vp, vp, i64, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.pe_rope_init.restype = ctypes.c_int
+        L.pe_rope_init.argtypes = [rp, i32, i32, dbl, i32, dbl, dbl, dbl, dbl, dbl]
+        L.pe_rotate.restype = ctypes.c_int
+        L.pe_rotate.argtypes = [dp, rp, i32, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.pe_quant_pages.restype = ctypes.c_int
+        L.pe_quant_pages.argtypes = [dp, cp, vp, vp, vp, vp, vp, vp, vp]
+        L.pe_quant_append.restype = ctypes.c_int
+        L.pe_quant_append.argtypes = [dp, cp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.pe_quant_decode.restype = ctypes.c_int
+        L.pe_quant_decode.argtypes = [dp, cp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
@@ -471,3 +499,101 @@ def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, soft
                                            float(softmax_scale), float(decay), _addr_opt(weights_in, "weights_in", torch.float32),
                                            _addr(weights_out, "weights_out", torch.float32), _addr(out, "out"), wp, wn, _stream())
     check(status, "pe_paged_decode_weights")
+
+
+def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used, block_table, spare,
+                   seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out):
+    check(lib().pe_plan_tokens(ctypes.byref(desc), _addr(seq_lens, "seq_lens", torch.int32), _addr(new_lens, "new_lens", torch.int32),
+                               _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
+                               _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
+                               _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
+                               _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
+                               _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
+                               _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
+                               _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
+                               _stream()), "pe_plan_tokens")
+
+
+def make_rope(rotary_dim, base, interleaved=False, scaling=PE_ROPE_PLAIN, factor=1.0, low=1.0, high=4.0, original=8192.0, magnitude=1.0):
+    """The frequencies of rotary positions (pe_rope_init), made once for a model."""
+    rope = pe_rope()
+    check(lib().pe_rope_init(ctypes.byref(rope), int(rotary_dim), PE_ROPE_INTERLEAVED if interleaved else PE_ROPE_HALF, float(base),
+                             int(scaling), float(factor), float(low), float(high), float(original), float(magnitude)), "pe_rope_init")
+    return rope
+
+
+def _token_rows(t, name, tokens, heads, desc):
+    """Address and token stride of [tokens, heads, D] whose tokens may lie apart (parts of one row a token side by side)."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError(name + " must be a GPU tensor")
+    if t.dtype != (torch.float32 if desc.dtype == PE_F32 else torch.bfloat16):
+        raise ValueError("%s must be of the cache's dtype, got %s" % (name, t.dtype))
+    if tuple(t.shape) != (tokens, heads, desc.head_dim):
+        raise ValueError("%s must be [%d, %d, %d], got %s" % (name, tokens, heads, desc.head_dim, tuple(t.shape)))
+    dense = heads * desc.head_dim
+    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != desc.head_dim)):
+        raise ValueError(name + ": a token's heads must be dense")
+    return t.data_ptr(), (t.stride(0) if tokens > 1 else dense)
+
+
+def pe_rotate(desc, rope, transpose, positions, q, k, v, q_out, k_out, slots=None, k_pool=None, v_pool=None):
+    """q, k, v, q_out, k_out: [T, heads, D] with dense heads, tokens any stride apart."""
+    T = int(positions.numel())
+    qp, qs = _token_rows(q, "q", T, desc.num_q_heads, desc)
+    kp, ks = _token_rows(k, "k", T, desc.num_kv_heads, desc)
+    vp, vs = _token_rows(v if slots is not None else None, "v", T, desc.num_kv_heads, desc)
+    qo, qos = _token_rows(q_out, "q_out", T, desc.num_q_heads, desc)
+    ko, kos = _token_rows(k_out, "k_out", T, desc.num_kv_heads, desc)
+    check(lib().pe_rotate(ctypes.byref(desc), ctypes.byref(rope), 1 if transpose else 0, T, _addr(positions, "positions", torch.int32),
+                          qp, qs, kp, ks, vp, vs, qo, qos, ko, kos, _addr_opt(slots, "slots", torch.int64),
+                          _addr_opt(k_pool, "k_pool"), _addr_opt(v_pool, "v_pool"), _stream()), "pe_rotate")
+
+
+def make_quant_cache(desc, k, v, scales, k_tail, v_tail):
+    """The descriptor of an 8-bit cache in these tensors (k, v: one byte an element, uint8 or float8_e4m3fn).  It holds them."""
+    shared = desc.layout == PE_LAYOUT_SHARED
+    heads = (desc.num_kv_heads,) if shared else ()
+    pool = (desc.num_phys_blocks, desc.block_size) + heads + (desc.head_dim,)
+    tail = (desc.num_seqs, desc.num_kv_heads, desc.block_size, desc.head_dim)
+    wants = (("k", k, pool, None), ("v", v, pool, None), ("scales", scales, (desc.num_phys_blocks,) + heads + (2,), torch.float32),
+             ("k_tail", k_tail, tail, torch.float32 if desc.dtype == PE_F32 else torch.bfloat16),
+             ("v_tail", v_tail, tail, torch.float32 if desc.dtype == PE_F32 else torch.bfloat16))
+    addresses = []
+    for name, t, shape, dtype in wants:
+        addresses.append(_addr(t, name, dtype))
+        if dtype is None and t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise ValueError("%s must be uint8 or float8_e4m3fn, got %s" % (name, t.dtype))
+        if tuple(t.shape) != shape:
+            raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
+    cache = pe_quant_cache(*addresses)
+    cache.tensors = (k, v, scales, k_tail, v_tail)
+    return cache
+
+
+def pe_quant_pages(desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out=None):
+    check(lib().pe_quant_pages(ctypes.byref(desc), ctypes.byref(cache), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                               _addr(src_table, "src_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                               _addr(block_table, "block_table", torch.int32), _addr_opt(scores_out, "scores_out", torch.float32),
+                               _stream()), "pe_quant_pages")
+
+
+def pe_quant_append(desc, cache, rope, positions, q, q_out, new_k, new_v, block_table, seq_lens, seq_lens_out, freed_phys, spare,
+                    spare_used, scores=None):
+    """rope None: positions, q and q_out are not looked at."""
+    turned = rope is not None
+    check(lib().pe_quant_append(ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(rope) if turned else None,
+                                _addr(positions, "positions", torch.int32) if turned else None, _addr(q, "q") if turned else None,
+                                _addr(q_out, "q_out") if turned else None, _addr(new_k, "new_k"), _addr(new_v, "new_v"),
+                                _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(freed_phys, "freed_phys", torch.int32),
+                                _addr(spare, "spare", torch.int32), _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]),
+                                _addr_opt(scores, "scores", torch.float32), _stream()), "pe_quant_append")
+
+
+def pe_quant_decode(desc, cache, q, block_table, seq_lens, softmax_scale, out, workspace=None):
+    wp, wn = _ws(workspace)
+    check(lib().pe_quant_decode(ctypes.byref(desc), ctypes.byref(cache), _addr(q, "q"), _addr(block_table, "block_table", torch.int32),
+                                _addr(seq_lens, "seq_lens", torch.int32), float(softmax_scale), _addr(out, "out"), wp, wn, _stream()),
+          "pe_quant_decode")

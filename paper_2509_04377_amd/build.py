@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "libpe.so")
 HOST_LIB = os.path.join(HERE, "_pe_host.so")
 SOURCES = ["pe_api.hip", "score_blocks.hip", "evict_blocks.hip", "paged_decode.hip", "paged_decode_bf16.hip",
            "prefill_prune.hip", "pe_api_rows.hip", "paged_rows.hip", "tree_wide.hip", "append_path.hip", "pe_api_pages.hip",
-           "select_pages.hip"]
+           "select_pages.hip", "pe_api_tokens.hip", "plan_tokens.hip", "rotate.hip", "pe_api_quant.hip", "quant_pages.hip",
+           "quant_decode.hip"]
 # Packed fp32 VALU ops are switched off for all device code.  The leading kernel arguments (up to 14 dwords) are preloaded
 # into scalar registers instead of being loaded by every wave.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

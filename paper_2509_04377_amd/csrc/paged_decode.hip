@@ -593,6 +593,15 @@ size_t decode_partials_bytes(int num_seqs, int num_q_heads, int head_dim, int sp
   return (size_t)num_seqs * num_q_heads * splits * (head_dim + 2) * sizeof(float);
 }
 
+hipError_t launch_decode_merge(const DecodeArgs& a, hipStream_t stream) {
+  const bool d64 = a.head_dim == 64;
+  if (a.is_bf16)
+    d64 ? launch_reduce<bf16_t, 64>(a, stream) : launch_reduce<bf16_t, 128>(a, stream);
+  else
+    d64 ? launch_reduce<float, 64>(a, stream) : launch_reduce<float, 128>(a, stream);
+  return hipGetLastError();
+}
+
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t stream) {
   if (a.head_dim != 64 && a.head_dim != 128) return hipErrorInvalidValue;
   const bool d64 = a.head_dim == 64;
@@ -604,11 +613,7 @@ hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t stream) {
   else
     e = launch_paged_decode_bf16(a, stream);
   if (e != hipSuccess || a.splits == 1 || a.counted || a.tagged) return e;
-  if (a.is_bf16)
-    d64 ? launch_reduce<bf16_t, 64>(a, stream) : launch_reduce<bf16_t, 128>(a, stream);
-  else
-    d64 ? launch_reduce<float, 64>(a, stream) : launch_reduce<float, 128>(a, stream);
-  return hipGetLastError();
+  return launch_decode_merge(a, stream);
 }
 
 }  // namespace pe

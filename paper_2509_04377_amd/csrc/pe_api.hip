@@ -8,6 +8,7 @@
 
 #include "pe_check.h"
 #include "pe_launch.h"
+#include "pe_quant.h"
 #include "pe_select.h"
 #include "pe_rows.h"
 
@@ -202,16 +203,6 @@ bool splits_tagged(const pe_cache_desc* d, const pe::DecodeArgs& a) {
   return splits_counted(d, a) && (a.splits < 8 || (a.splits == 8 && a.waves == 4 && row_bytes(d) / 8 < (256 << 10)));
 }
 
-// A launch's own tag: a counter from the time of the first call on, mixed as in SplitMix64 (Steele, Lea and Flood, 2014: its increment, shifts and
-// multipliers).  No two of a process are the same (the mixing is one to one), and what lies in memory is none by chance.
-uint64_t launch_tag() {
-  static std::atomic<uint64_t> calls{(uint64_t)std::chrono::system_clock::now().time_since_epoch().count()};
-  uint64_t x = calls.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b97f4a7c15ull;
-  x = (x ^ x >> 30) * 0xbf58476d1ce4e5b9ull;
-  x = (x ^ x >> 27) * 0x94d049bb133111ebull;
-  return x ^ x >> 31;
-}
-
 // For a call of the attention alone: tags its launch where that pays and the output can hold tags before it is written, that is, nothing
 // that is read lies there.
 void tag_attention(const pe_cache_desc* d, pe::DecodeArgs* a) {
@@ -223,9 +214,25 @@ void tag_attention(const pe_cache_desc* d, pe::DecodeArgs* a) {
 
 }  // namespace
 
+namespace pe {
+namespace host {
+
+// A launch's own tag: a counter from the time of the first call on, mixed as in SplitMix64 (Steele, Lea and Flood, 2014: its increment, shifts and
+// multipliers).  No two of a process are the same (the mixing is one to one), and what lies in memory is none by chance.
+uint64_t launch_tag() {
+  static std::atomic<uint64_t> calls{(uint64_t)std::chrono::system_clock::now().time_since_epoch().count()};
+  uint64_t x = calls.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b97f4a7c15ull;
+  x = (x ^ x >> 30) * 0xbf58476d1ce4e5b9ull;
+  x = (x ^ x >> 27) * 0x94d049bb133111ebull;
+  return x ^ x >> 31;
+}
+
+}  // namespace host
+}  // namespace pe
+
 extern "C" {
 
-int pe_version(void) { return 400; }  // 0.4.0: trees of drafts, selected pages, page weights
+int pe_version(void) { return 500; }  // 0.5.0: plans of tokens, rotary positions, caches in 8 bits
 
 const char* pe_status_string(int status) {
   switch (status) {
@@ -257,6 +264,8 @@ size_t pe_workspace_bytes(int op, const pe_cache_desc* desc, int64_t total_token
       return pe::weights_workspace_bytes(desc);
     case PE_OP_SELECT_PAGES:
       return pe::select_workspace_bytes(desc);
+    case PE_OP_QUANT_DECODE:
+      return pe::quant_workspace_bytes(desc);
     default:
       return 0;
   }

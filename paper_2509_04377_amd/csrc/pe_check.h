@@ -62,6 +62,8 @@ inline int compute_units() {
   return n;
 }
 
+uint64_t launch_tag();  // of a launch whose splits are merged by the last to arrive (pe_api.hip)
+
 // A row of workgroups has fewer than 2^32 threads.
 inline bool one_launch(int64_t workgroups, int threads) { return workgroups <= ((1LL << 32) - 1) / threads; }
 
@@ -69,6 +71,12 @@ inline int check_workspace(const void* ws, size_t have, size_t need) {
   if (need == 0) return PE_OK;
   if (ws == nullptr || have < need || !aligned(ws, 256)) return PE_ERR_WORKSPACE;
   return PE_OK;
+}
+
+// A structure that pe_rope_init has filled, for heads of this size.
+inline bool rope_ok(const pe_rope* r, int head_dim) {
+  return r != nullptr && r->filled == 1 && r->rotary_dim >= 2 && r->rotary_dim <= head_dim && r->rotary_dim % 2 == 0 &&
+         (r->pairs == PE_ROPE_HALF || r->pairs == PE_ROPE_INTERLEAVED);
 }
 
 inline bool finite(float x) { return x == x && x - x == 0.f; }

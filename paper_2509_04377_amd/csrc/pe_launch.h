@@ -98,6 +98,7 @@ struct DecodeArgs {
 };
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t stream);
 hipError_t launch_paged_decode_bf16(const DecodeArgs& a, hipStream_t stream);  // the attention kernel alone (no merge)
+hipError_t launch_decode_merge(const DecodeArgs& a, hipStream_t stream);       // the merge of its splits alone
 size_t decode_partials_bytes(int num_seqs, int num_q_heads, int head_dim, int splits);
 // The most splits of a row that are counted or tagged, and with so many query heads a KV head; up to here they are added in one order on
 // every way.

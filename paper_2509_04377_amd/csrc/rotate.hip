@@ -1,0 +1,252 @@
+// Rotary positions of queries and keys, and the turned keys' and the values' way into the pages (pe_rotate).
+//
+// Bound by memory: every element is read and written once (stored keys written twice), the angles cost some thirty instructions for
+// each pair of a token, whatever the number of heads.  A workgroup takes some tokens: first its threads put the cosines and
+// sines of their pairs into LDS, then they walk over (token, head, part), 16 bytes of each half of a pair at a time (neighbouring
+// pairs: 16 bytes), two or four of them on their way before the first is used.
+//
+// Where rows are not 16-byte aligned, or a half is no multiple of 16 bytes, threads walk over single pairs instead.
+#include "pe_rope_device.h"
+#include "pe_tokens.h"
+
+namespace pe {
+namespace {
+
+constexpr int kThreads = kRotateThreads;
+constexpr int kMostPairs = 64;
+
+// Elements of 16 bytes as fp32, and back.
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(const uint4& r, float (&x)[4]) {
+    x[0] = __uint_as_float(r.x), x[1] = __uint_as_float(r.y), x[2] = __uint_as_float(r.z), x[3] = __uint_as_float(r.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+template <>
+struct Vec<bf16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4& r, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = vec_elem<bf16_t>(r, e);
+  }
+  static __device__ __forceinline__ uint32_t two(float a, float b) { return (uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16; }
+  static __device__ __forceinline__ uint4 put(const float (&x)[8]) {
+    return make_uint4(two(x[0], x[1]), two(x[2], x[3]), two(x[4], x[5]), two(x[6], x[7]));
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ float load_one(const void* p, int64_t i) {
+  if constexpr (sizeof(T) == 4)
+    return static_cast<const float*>(p)[i];
+  else
+    return __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[i] << 16);
+}
+template <typename T>
+__device__ __forceinline__ void store_one(void* p, int64_t i, float x) {
+  if constexpr (sizeof(T) == 4)
+    static_cast<float*>(p)[i] = x;
+  else
+    static_cast<uint16_t*>(p)[i] = f32_to_bf16(x);
+}
+
+// Where head h of the batch's queries, keys and values (numbered in this order) is read and written.
+struct Head {
+  const void* from;
+  void* to;       // null: not kept
+  int64_t in, out;  // element of the head's first
+  int kv;         // its number among the keys or values, or -1
+  bool value;
+};
+__device__ __forceinline__ Head head_of(const RotateArgs& a, int64_t t, int h) {
+  if (h < a.num_q_heads) return Head{a.q, a.q_out, t * a.q_stride + (int64_t)h * a.head_dim, t * a.q_out_stride + (int64_t)h * a.head_dim, -1, false};
+  h -= a.num_q_heads;
+  if (h < a.num_kv_heads) return Head{a.k, a.k_out, t * a.k_stride + (int64_t)h * a.head_dim, t * a.k_out_stride + (int64_t)h * a.head_dim, h, false};
+  h -= a.num_kv_heads;
+  return Head{a.v, nullptr, t * a.v_stride + (int64_t)h * a.head_dim, 0, h, true};
+}
+// The head's first element in the pools, or -1.
+__device__ __forceinline__ int64_t pool_at(const RotateArgs& a, int64_t t, const Head& head) {
+  if (a.slots == nullptr || head.kv < 0) return -1;
+  const int64_t slot = a.shared ? a.slots[t] : a.slots[t * a.num_kv_heads + head.kv];
+  if (slot < 0 || slot >= a.pool_tokens) return -1;
+  return (a.shared ? slot * a.num_kv_heads + head.kv : slot) * a.head_dim;
+}
+
+struct Rope {
+  int pairs;  // R / 2
+  float magnitude;
+  uint64_t turns[kMostPairs];
+};
+
+// Cosines and sines of `count` tokens' pairs, times the magnitude.
+__device__ __forceinline__ void fill_turns(Turn* sm, const Rope& rope, const int32_t* positions, int64_t t0, int count, bool transpose) {
+  for (int i = (int)threadIdx.x; i < count * kMostPairs; i += kThreads) {
+    const int t = i / kMostPairs, p = i % kMostPairs;
+    if (p >= rope.pairs) continue;
+    Turn x = turn_of(rope.turns[p], positions[t0 + t]);
+    x.c *= rope.magnitude;
+    x.s *= transpose ? -rope.magnitude : rope.magnitude;
+    sm[t * kMostPairs + p] = x;
+  }
+  __syncthreads();
+}
+
+// Single pairs (i, i + R/2) or (2i, 2i + 1), and what is behind them two elements at a time.
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotate_pairs_kernel(const RotateArgs a, const Rope rope, int heads) {
+  __shared__ Turn sm[kMostPairs];
+  const int64_t t = blockIdx.x;
+  fill_turns(sm, rope, a.positions, t, 1, a.transpose);
+  const int half = a.head_dim / 2;
+  for (int i = (int)threadIdx.x; i < heads * half; i += kThreads) {
+    const int h = i / half, p = i % half;
+    const Head head = head_of(a, t, h);
+    const int64_t pool = pool_at(a, t, head);
+    if (head.value && pool < 0) continue;
+    const bool turned = p < rope.pairs;
+    const int ea = !turned || INTERLEAVED ? 2 * p : p, eb = !turned || INTERLEAVED ? 2 * p + 1 : p + rope.pairs;
+    float x = load_one<T>(head.from, head.in + ea), y = load_one<T>(head.from, head.in + eb);
+    if (turned && !head.value) {
+      const Turn w = sm[p];
+      const float x0 = x;
+      x = x0 * w.c - y * w.s;
+      y = y * w.c + x0 * w.s;
+    }
+    // (value heads go by 2p, 2p + 1 or by halves alike: each element is one thread's)
+    if (head.to != nullptr) store_one<T>(head.to, head.out + ea, x), store_one<T>(head.to, head.out + eb, y);
+    if (pool >= 0) {
+      void* to = head.value ? a.v_pool : a.k_pool;
+      store_one<T>(to, pool + ea, x), store_one<T>(to, pool + eb, y);
+    }
+  }
+}
+
+// 16 bytes at a time.  A head has `units` of work: of each half 16 bytes (INTERLEAVED: 16 bytes) turned, then 16 bytes copied.
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, const Rope rope, int heads, int tokens_each, int log2_units,
+                                                          uint32_t inv_heads) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ Turn turns[];
+  const int64_t t0 = (int64_t)blockIdx.x * tokens_each;
+  const int count = a.tokens - t0 < tokens_each ? (int)(a.tokens - t0) : tokens_each;
+  fill_turns(turns, rope, a.positions, t0, count, a.transpose);
+  const int nturned = INTERLEAVED ? 2 * rope.pairs / N : rope.pairs / N;  // units that turn
+  const int nvec = a.head_dim / N;
+  const int u = (int)threadIdx.x & ((1 << log2_units) - 1);
+  const int all = count * heads;
+  for (int i = (int)threadIdx.x >> log2_units; i < all; i += kThreads >> log2_units) {
+    const int t = (int)((uint64_t)(uint32_t)i * inv_heads >> 32), h = i - t * heads;
+    const Head head = head_of(a, t0 + t, h);
+    const int64_t pool = pool_at(a, t0 + t, head);
+    void* const pages = head.value ? a.v_pool : a.k_pool;
+    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(head.from) + head.in);
+    uint4* to = head.to == nullptr ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(head.to) + head.out);
+    uint4* page = pool < 0 ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(pages) + pool);
+    if (head.value) {
+      if (page != nullptr)
+        for (int j = u; j < nvec; j += 1 << log2_units) page[j] = from[j];
+    } else if (u < nturned) {
+      const Turn* w = turns + t * kMostPairs;
+      if constexpr (INTERLEAVED) {
+        float x[N];
+        Vec<T>::get(from[u], x);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+          const Turn r = w[u * (N / 2) + e];
+          const float p = x[2 * e], q = x[2 * e + 1];
+          x[2 * e] = p * r.c - q * r.s;
+          x[2 * e + 1] = q * r.c + p * r.s;
+        }
+        const uint4 o = Vec<T>::put(x);
+        if (to != nullptr) to[u] = o;
+        if (page != nullptr) page[u] = o;
+      } else {
+        float x[N], y[N];
+        Vec<T>::get(from[u], x);
+        Vec<T>::get(from[u + nturned], y);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const Turn r = w[u * N + e];
+          const float p = x[e], q = y[e];
+          x[e] = p * r.c - q * r.s;
+          y[e] = q * r.c + p * r.s;
+        }
+        const uint4 o = Vec<T>::put(x), o2 = Vec<T>::put(y);
+        if (to != nullptr) to[u] = o, to[u + nturned] = o2;
+        if (page != nullptr) page[u] = o, page[u + nturned] = o2;
+      }
+    } else {
+      const int j = u + (INTERLEAVED ? 0 : nturned);
+      if (j < nvec) {
+        const uint4 r = from[j];
+        if (to != nullptr) to[j] = r;
+        if (page != nullptr) page[j] = r;
+      }
+    }
+  }
+}
+
+template <typename T>
+bool by_vectors(const RotateArgs& a, const pe_rope& rope) {
+  constexpr int N = Vec<T>::N;
+  const auto fits = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % N == 0; };
+  return rope.rotary_dim % (rope.pairs == PE_ROPE_INTERLEAVED ? N : 2 * N) == 0 && fits(a.q, a.q_stride) && fits(a.k, a.k_stride) &&
+         fits(a.v, a.v_stride) && fits(a.q_out, a.q_out_stride) && fits(a.k_out, a.k_out_stride) && fits(a.k_pool, 0) && fits(a.v_pool, 0);
+}
+
+template <typename T, bool INTERLEAVED>
+hipError_t launch(const RotateArgs& a, const pe_rope& rope, hipStream_t stream) {
+  Rope r;
+  r.pairs = rope.rotary_dim / 2;
+  r.magnitude = rope.magnitude;
+  for (int i = 0; i < kMostPairs; ++i) r.turns[i] = rope.turns[i];
+  const int heads = a.num_q_heads + a.num_kv_heads * (a.slots != nullptr ? 2 : 1);
+  if (!by_vectors<T>(a, rope)) {
+    hipLaunchKernelGGL((rotate_pairs_kernel<T, INTERLEAVED>), dim3((unsigned)a.tokens), dim3(kThreads), 0, stream, a, r, heads);
+    return hipGetLastError();
+  }
+  constexpr int N = Vec<T>::N;
+  const int units = a.head_dim / N - (INTERLEAVED ? 0 : r.pairs / N);
+  int log2_units = 0;
+  while ((1 << log2_units) < units) ++log2_units;
+  const int each = 1;
+  const int64_t groups = (a.tokens + each - 1) / each;
+  const uint32_t inv_heads = (uint32_t)((1ull << 32) / (uint32_t)heads + 1);
+  hipLaunchKernelGGL((rotate_kernel<T, INTERLEAVED>), dim3((unsigned)groups), dim3(kThreads), each * kMostPairs * sizeof(Turn), stream, a, r, heads,
+                     each, log2_units, inv_heads);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs& all, const pe_rope& rope, hipStream_t stream) {
+  const bool inter = rope.pairs == PE_ROPE_INTERLEAVED;
+  const int64_t bytes = all.is_bf16 ? 2 : 4, most = ((1LL << 32) - 1) / kThreads;  // a launch has fewer than 2^32 threads
+  const auto behind = [&](const void* p, int64_t elements) {
+    return p == nullptr ? static_cast<const char*>(nullptr) : static_cast<const char*>(p) + elements * bytes;
+  };
+  for (int64_t t = 0; t < all.tokens; t += most) {
+    RotateArgs a = all;
+    a.tokens = all.tokens - t < most ? all.tokens - t : most;
+    a.positions = all.positions + t;
+    a.q = behind(all.q, t * all.q_stride);
+    a.k = behind(all.k, t * all.k_stride);
+    a.v = behind(all.v, t * all.v_stride);
+    a.q_out = const_cast<char*>(behind(all.q_out, t * all.q_out_stride));
+    a.k_out = const_cast<char*>(behind(all.k_out, t * all.k_out_stride));
+    if (a.slots != nullptr) a.slots = all.slots + t * (all.shared ? 1 : all.num_kv_heads);
+    const hipError_t e = a.is_bf16 ? (inter ? launch<bf16_t, true>(a, rope, stream) : launch<bf16_t, false>(a, rope, stream))
+                                   : (inter ? launch<float, true>(a, rope, stream) : launch<float, false>(a, rope, stream));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace pe
