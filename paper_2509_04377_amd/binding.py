@@ -91,10 +91,12 @@ def _load_host():
     if os.path.exists(HOST_PATH):
         try:
             from . import _pe_host
-            if (_pe_host.bind_descriptor(pe_cache_desc) == _layout(pe_cache_desc) and
-                    _pe_host.bind_evict_opts(pe_evict_opts) == _layout(pe_evict_opts)):
+            binds = ((_pe_host.bind_descriptor, pe_cache_desc), (_pe_host.bind_evict_opts, pe_evict_opts), (_pe_host.bind_rope, pe_rope),
+                     (_pe_host.bind_quant_cache, pe_quant_cache))
+            others = [of.__name__ for bind, of in binds if bind(of) != _layout(of)]
+            if not others:
                 return _pe_host
-            why = "has another pe_cache_desc or pe_evict_opts"
+            why = "has another " + " and ".join(others)
         except (ImportError, AttributeError) as e:
             why = "does not load: %s" % e
     warnings.warn("_pe_host.so %s (%s): arguments are checked in Python, some 3 us more a call; build as for libpe.so" % (why, HOST_PATH),
@@ -180,7 +182,8 @@ def lib():
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
-                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages"):
+                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens", "rotate",
+                     "quant_pages", "quant_append", "quant_decode"):
             setattr(L, "addr_" + name, ctypes.cast(getattr(L, "pe_" + name), vp).value)
         _lib = L
     return _lib
@@ -503,15 +506,20 @@ def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, soft
 
 def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used, block_table, spare,
                    seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out):
-    check(lib().pe_plan_tokens(ctypes.byref(desc), _addr(seq_lens, "seq_lens", torch.int32), _addr(new_lens, "new_lens", torch.int32),
-                               _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
-                               _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
-                               _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
-                               _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
-                               _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
-                               _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
-                               _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
-                               _stream()), "pe_plan_tokens")
+    L = lib()
+    status = _host.plan_tokens(L.addr_plan_tokens, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages, free_used,
+                               block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out)
+    if status is None:
+        status = L.pe_plan_tokens(ctypes.byref(desc), _addr(seq_lens, "seq_lens", torch.int32), _addr(new_lens, "new_lens", torch.int32),
+                                  _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
+                                  _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
+                                  _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
+                                  _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
+                                  _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
+                                  _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
+                                  _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
+                                  _stream())
+    check(status, "pe_plan_tokens")
 
 
 def make_rope(rotary_dim, base, interleaved=False, scaling=PE_ROPE_PLAIN, factor=1.0, low=1.0, high=4.0, original=8192.0, magnitude=1.0):
@@ -540,15 +548,19 @@ def _token_rows(t, name, tokens, heads, desc):
 
 def pe_rotate(desc, rope, transpose, positions, q, k, v, q_out, k_out, slots=None, k_pool=None, v_pool=None):
     """q, k, v, q_out, k_out: [T, heads, D] with dense heads, tokens any stride apart."""
-    T = int(positions.numel())
-    qp, qs = _token_rows(q, "q", T, desc.num_q_heads, desc)
-    kp, ks = _token_rows(k, "k", T, desc.num_kv_heads, desc)
-    vp, vs = _token_rows(v if slots is not None else None, "v", T, desc.num_kv_heads, desc)
-    qo, qos = _token_rows(q_out, "q_out", T, desc.num_q_heads, desc)
-    ko, kos = _token_rows(k_out, "k_out", T, desc.num_kv_heads, desc)
-    check(lib().pe_rotate(ctypes.byref(desc), ctypes.byref(rope), 1 if transpose else 0, T, _addr(positions, "positions", torch.int32),
-                          qp, qs, kp, ks, vp, vs, qo, qos, ko, kos, _addr_opt(slots, "slots", torch.int64),
-                          _addr_opt(k_pool, "k_pool"), _addr_opt(v_pool, "v_pool"), _stream()), "pe_rotate")
+    L = lib()
+    status = _host.rotate(L.addr_rotate, desc, rope, transpose, positions, q, k, v, q_out, k_out, slots, k_pool, v_pool)
+    if status is None:
+        T = int(positions.numel())
+        qp, qs = _token_rows(q, "q", T, desc.num_q_heads, desc)
+        kp, ks = _token_rows(k, "k", T, desc.num_kv_heads, desc)
+        vp, vs = _token_rows(v if slots is not None else None, "v", T, desc.num_kv_heads, desc)
+        qo, qos = _token_rows(q_out, "q_out", T, desc.num_q_heads, desc)
+        ko, kos = _token_rows(k_out, "k_out", T, desc.num_kv_heads, desc)
+        status = L.pe_rotate(ctypes.byref(desc), ctypes.byref(rope), 1 if transpose else 0, T, _addr(positions, "positions", torch.int32),
+                             qp, qs, kp, ks, vp, vs, qo, qos, ko, kos, _addr_opt(slots, "slots", torch.int64),
+                             _addr_opt(k_pool, "k_pool"), _addr_opt(v_pool, "v_pool"), _stream())
+    check(status, "pe_rotate")
 
 
 def make_quant_cache(desc, k, v, scales, k_tail, v_tail):
@@ -573,27 +585,41 @@ def make_quant_cache(desc, k, v, scales, k_tail, v_tail):
 
 
 def pe_quant_pages(desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out=None):
-    check(lib().pe_quant_pages(ctypes.byref(desc), ctypes.byref(cache), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                               _addr(src_table, "src_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                               _addr(block_table, "block_table", torch.int32), _addr_opt(scores_out, "scores_out", torch.float32),
-                               _stream()), "pe_quant_pages")
+    L = lib()
+    status = _host.quant_pages(L.addr_quant_pages, desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out)
+    if status is None:
+        status = L.pe_quant_pages(ctypes.byref(desc), ctypes.byref(cache), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                  _addr(src_table, "src_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                  _addr(block_table, "block_table", torch.int32), _addr_opt(scores_out, "scores_out", torch.float32),
+                                  _stream())
+    check(status, "pe_quant_pages")
 
 
 def pe_quant_append(desc, cache, rope, positions, q, q_out, new_k, new_v, block_table, seq_lens, seq_lens_out, freed_phys, spare,
                     spare_used, scores=None):
     """rope None: positions, q and q_out are not looked at."""
+    L = lib()
     turned = rope is not None
-    check(lib().pe_quant_append(ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(rope) if turned else None,
-                                _addr(positions, "positions", torch.int32) if turned else None, _addr(q, "q") if turned else None,
-                                _addr(q_out, "q_out") if turned else None, _addr(new_k, "new_k"), _addr(new_v, "new_v"),
-                                _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                                _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(freed_phys, "freed_phys", torch.int32),
-                                _addr(spare, "spare", torch.int32), _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]),
-                                _addr_opt(scores, "scores", torch.float32), _stream()), "pe_quant_append")
+    if not turned:
+        positions = q = q_out = None
+    status = _host.quant_append(L.addr_quant_append, desc, cache, rope, positions, q, q_out, new_k, new_v, block_table, seq_lens, seq_lens_out,
+                                freed_phys, spare, spare_used, spare, scores)
+    if status is None:
+        status = L.pe_quant_append(ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(rope) if turned else None,
+                                   _addr(positions, "positions", torch.int32) if turned else None, _addr(q, "q") if turned else None,
+                                   _addr(q_out, "q_out") if turned else None, _addr(new_k, "new_k"), _addr(new_v, "new_v"),
+                                   _addr(block_table, "block_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                   _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(freed_phys, "freed_phys", torch.int32),
+                                   _addr(spare, "spare", torch.int32), _addr(spare_used, "spare_used", torch.int32), int(spare.shape[-1]),
+                                   _addr_opt(scores, "scores", torch.float32), _stream())
+    check(status, "pe_quant_append")
 
 
 def pe_quant_decode(desc, cache, q, block_table, seq_lens, softmax_scale, out, workspace=None):
-    wp, wn = _ws(workspace)
-    check(lib().pe_quant_decode(ctypes.byref(desc), ctypes.byref(cache), _addr(q, "q"), _addr(block_table, "block_table", torch.int32),
-                                _addr(seq_lens, "seq_lens", torch.int32), float(softmax_scale), _addr(out, "out"), wp, wn, _stream()),
-          "pe_quant_decode")
+    L = lib()
+    status = _host.quant_decode(L.addr_quant_decode, desc, cache, q, block_table, seq_lens, softmax_scale, out, workspace)
+    if status is None:
+        wp, wn = _ws(workspace)
+        status = L.pe_quant_decode(ctypes.byref(desc), ctypes.byref(cache), _addr(q, "q"), _addr(block_table, "block_table", torch.int32),
+                                   _addr(seq_lens, "seq_lens", torch.int32), float(softmax_scale), _addr(out, "out"), wp, wn, _stream())
+    check(status, "pe_quant_decode")

@@ -58,6 +58,23 @@ struct Words {  // 64-bit integers
   std::tuple<Address> c;
   bool get(PyObject* o) { return address_of(o, true, at::kLong, &std::get<0>(c)); }
 };
+struct WordsOrNone {
+  std::tuple<Address> c;
+  bool get(PyObject* o) { return o == Py_None || address_of(o, true, at::kLong, &std::get<0>(c)); }
+};
+struct TensorOrNone {
+  std::tuple<Address> c;
+  bool get(PyObject* o) { return o == Py_None || address_of(o, false, at::kInt, &std::get<0>(c)); }
+};
+struct Numel {  // how many elements a tensor has
+  std::tuple<int32_t> c;
+  bool get(PyObject* o) {
+    if (!THPVariable_Check(o)) return false;
+    const int64_t n = THPVariable_Unpack(o).numel();
+    std::get<0>(c) = (int32_t)n;
+    return std::get<0>(c) == n;
+  }
+};
 struct SecondDim {  // the size of a tensor's second dimension
   std::tuple<int32_t> c;
   bool get(PyObject* o) {
@@ -65,6 +82,18 @@ struct SecondDim {  // the size of a tensor's second dimension
     const at::Tensor& t = THPVariable_Unpack(o);
     if (t.dim() < 2) return false;
     std::get<0>(c) = (int32_t)t.size(1);
+    return true;
+  }
+};
+struct LastDimOrNone {  // the size of a tensor's last dimension, 0 without one
+  std::tuple<int32_t> c;
+  bool get(PyObject* o) {
+    std::get<0>(c) = 0;
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.dim() < 1) return false;
+    std::get<0>(c) = (int32_t)t.size(-1);
     return true;
   }
 };
@@ -115,7 +144,7 @@ struct Workspace {
 };
 
 // binding.py's ctypes structures (see bind_descriptor); nullptr: not named yet.
-PyTypeObject *descriptor_type = nullptr, *evict_opts_type = nullptr;
+PyTypeObject *descriptor_type = nullptr, *evict_opts_type = nullptr, *rope_type = nullptr, *quant_cache_type = nullptr;
 
 // A structure: an object of that type and of no other, read through the buffer protocol.
 template <typename T>
@@ -139,6 +168,26 @@ struct EvictOpts {
   pe_evict_opts opts;
   std::tuple<const pe_evict_opts*> c{&opts};
   bool get(PyObject* o) { return structure(o, evict_opts_type, &opts); }
+};
+
+struct Rope {
+  pe_rope rope;
+  std::tuple<const pe_rope*> c{&rope};
+  bool get(PyObject* o) { return structure(o, rope_type, &rope); }
+};
+struct RopeOrNone {
+  pe_rope rope;
+  std::tuple<const pe_rope*> c{nullptr};
+  bool get(PyObject* o) {
+    if (o == Py_None) return true;
+    std::get<0>(c) = &rope;
+    return structure(o, rope_type, &rope);
+  }
+};
+struct QuantCache {
+  pe_quant_cache cache;
+  std::tuple<const pe_quant_cache*> c{&cache};
+  bool get(PyObject* o) { return structure(o, quant_cache_type, &cache); }
 };
 
 template <typename... Args, size_t... I>
@@ -171,6 +220,63 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
   } catch (const std::exception&) {  // e.g. a tensor without storage
+    Py_RETURN_NONE;
+  }
+}
+
+// [tokens, heads, D] with dense heads, tokens any stride apart; None: no address.
+struct TokenRows {
+  void* p = nullptr;
+  int64_t stride = 0;
+  bool get(PyObject* o, int64_t tokens, int heads, const pe_cache_desc& d) {
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.dim() != 3) return false;
+    if (t.scalar_type() != (d.dtype == PE_F32 ? at::kFloat : at::kBFloat16)) return false;
+    if (t.size(0) != tokens || t.size(1) != heads || t.size(2) != d.head_dim) return false;
+    if (t.stride(2) != 1 || (heads > 1 && t.stride(1) != d.head_dim)) return false;
+    p = t.data_ptr();
+    stride = tokens > 1 ? t.stride(0) : (int64_t)heads * d.head_dim;
+    return true;
+  }
+};
+
+// args: address of pe_rotate, descriptor, rope, transpose, positions, q, k, v, q_out, k_out, slots, k_pool, v_pool
+PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 13) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return nullptr;
+  }
+  const auto fn = reinterpret_cast<decltype(&pe_rotate)>(PyLong_AsVoidPtr(args[0]));
+  if (fn == nullptr) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no function");
+    return nullptr;
+  }
+  try {
+    Desc desc;
+    Rope rope;
+    Ints positions;
+    WordsOrNone slots;
+    TensorOrNone k_pool, v_pool;
+    TokenRows q, k, v, q_out, k_out;
+    if (!desc.get(args[1]) || !rope.get(args[2]) || !PyBool_Check(args[3]) || !positions.get(args[4]) || !slots.get(args[10]) ||
+        !k_pool.get(args[11]) || !v_pool.get(args[12]))
+      Py_RETURN_NONE;
+    const pe_cache_desc& d = desc.d;
+    const int64_t T = THPVariable_Unpack(args[4]).numel();
+    if (!q.get(args[5], T, d.num_q_heads, d) || !k.get(args[6], T, d.num_kv_heads, d) ||
+        (args[10] != Py_None && !v.get(args[7], T, d.num_kv_heads, d)) || !q_out.get(args[8], T, d.num_q_heads, d) ||
+        !k_out.get(args[9], T, d.num_kv_heads, d))
+      Py_RETURN_NONE;
+    const auto stream = c10::hip::getCurrentHIPStream().stream();
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn(&d, &rope.rope, args[3] == Py_True ? 1 : 0, T, std::get<0>(positions.c), q.p, q.stride, k.p, k.stride, v.p, v.stride, q_out.p,
+                q_out.stride, k_out.p, k_out.stride, std::get<0>(slots.c), std::get<0>(k_pool.c), std::get<0>(v_pool.c), (void*)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+  } catch (const std::exception&) {
     Py_RETURN_NONE;
   }
 }
@@ -218,9 +324,43 @@ PyObject* bind_evict_opts(PyObject*, PyObject* type) {
   return layout;
 }
 
+// And of the rotary frequencies and the 8-bit cache.
+PyObject* bind_rope(PyObject*, PyObject* type) {
+  if (!PyType_Check(type)) {
+    PyErr_SetString(PyExc_TypeError, "the type of the frequencies");
+    return nullptr;
+  }
+#define PE_FIELD(f) #f, (Py_ssize_t)offsetof(pe_rope, f), (Py_ssize_t)sizeof(pe_rope::f)
+  PyObject* layout = Py_BuildValue("(n(snn)(snn)(snn)(snn)(snn))", (Py_ssize_t)sizeof(pe_rope), PE_FIELD(rotary_dim), PE_FIELD(pairs),
+                                   PE_FIELD(magnitude), PE_FIELD(filled), PE_FIELD(turns));
+#undef PE_FIELD
+  if (layout == nullptr) return nullptr;
+  Py_INCREF(type);
+  Py_XDECREF((PyObject*)rope_type);
+  rope_type = reinterpret_cast<PyTypeObject*>(type);
+  return layout;
+}
+PyObject* bind_quant_cache(PyObject*, PyObject* type) {
+  if (!PyType_Check(type)) {
+    PyErr_SetString(PyExc_TypeError, "the type of the cache");
+    return nullptr;
+  }
+#define PE_FIELD(f) #f, (Py_ssize_t)offsetof(pe_quant_cache, f), (Py_ssize_t)sizeof(pe_quant_cache::f)
+  PyObject* layout = Py_BuildValue("(n(snn)(snn)(snn)(snn)(snn))", (Py_ssize_t)sizeof(pe_quant_cache), PE_FIELD(k), PE_FIELD(v),
+                                   PE_FIELD(scales), PE_FIELD(k_tail), PE_FIELD(v_tail));
+#undef PE_FIELD
+  if (layout == nullptr) return nullptr;
+  Py_INCREF(type);
+  Py_XDECREF((PyObject*)quant_cache_type);
+  quant_cache_type = reinterpret_cast<PyTypeObject*>(type);
+  return layout;
+}
+
 PyMethodDef methods[] = {
     {"bind_descriptor", bind_descriptor, METH_O, nullptr},
     {"bind_evict_opts", bind_evict_opts, METH_O, nullptr},
+    {"bind_rope", bind_rope, METH_O, nullptr},
+    {"bind_quant_cache", bind_quant_cache, METH_O, nullptr},
     // q, k_pool, v_pool, block_table, seq_lens, softmax_scale, out, workspace
     method<call<decltype(&pe_paged_decode), Tensor, Tensor, Tensor, Ints, Ints, Float, Tensor, Workspace>>("paged_decode"),
     // new_k, new_v, q, k_pool, v_pool, block_table, seq_lens, seq_lens_out, freed_phys, spare, spare_used, spare, softmax_scale,
@@ -258,6 +398,18 @@ PyMethodDef methods[] = {
     method<call<decltype(&pe_page_bounds), Tensor, Ints, Ints, Number<int32_t>, Tensor>>("page_bounds"),
     // q, bounds, block_table, seq_lens, num_pages, block_table_out, seq_lens_out, page_idx_out, workspace
     method<call<decltype(&pe_select_pages), Tensor, Tensor, Ints, Ints, Number<int32_t>, Ints, Ints, IntsOrNone, Workspace>>("select_pages"),
+    // seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages, free_used, block_table, spare, spare,
+    // seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out
+    method<call<decltype(&pe_plan_tokens), Ints, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Ints, Numel, Ints, Ints, IntsOrNone,
+                LastDimOrNone, Ints, Ints, IntsOrNone, IntsOrNone, WordsOrNone>>("plan_tokens"),
+    method<rotate>("rotate"),
+    // cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out
+    method<call<decltype(&pe_quant_pages), QuantCache, Tensor, Tensor, Ints, Ints, Ints, FloatsOrNone>>("quant_pages"),
+    // cache, rope, positions, q, q_out, new_k, new_v, block_table, seq_lens, seq_lens_out, freed_phys, spare, spare_used, spare, scores
+    method<call<decltype(&pe_quant_append), QuantCache, RopeOrNone, IntsOrNone, TensorOrNone, TensorOrNone, Tensor, Tensor, Ints, Ints, Ints,
+                Ints, Ints, Ints, LastDim, FloatsOrNone>>("quant_append"),
+    // cache, q, block_table, seq_lens, softmax_scale, out, workspace
+    method<call<decltype(&pe_quant_decode), QuantCache, Tensor, Ints, Ints, Float, Tensor, Workspace>>("quant_decode"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pe_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
