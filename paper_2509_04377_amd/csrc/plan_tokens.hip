@@ -3,10 +3,11 @@
 // With n_s tokens that sequence s brings and p_s pages that each of its rows is to get, everything follows from two exclusive prefix sums
 // over the sequences, of n_s and of rows * p_s: token t belongs to the sequence whose sum brackets t, and so does dealt page p.  The sums
 // are short (a batch of sequences) and what hangs on them is long (a 64-bit slot for each token and row), so every workgroup makes all
-// sums by itself, kPlanThreads sequences at a time, and writes its own share of pages and slots in between: one launch, no workgroup waits
-// for another, nothing is ordered by an atomic.  Shares are pieces of kPlanThreads tokens or pages, dealt round robin, that a workgroup cuts with
-// the sequences it has just summed.  The table is written where it has no entry yet and read where it has one, so that the order
-// of workgroups does not matter.
+// sums by itself, kThreads sequences at a time, and writes its own share of slots and pages in between: one launch, no workgroup waits
+// for another, nothing is ordered by an atomic.  Shares are pieces of kThreads tokens or pages, cut out of the sequences that have just been
+// summed.  The table is written where it has no entry yet and read where it has one, so that the order of workgroups does not matter.
+//
+// Bound: for a step of a batch by the chain of a launch (lengths, sums, the page, the slot), for a batch of prompts by its stores.
 #include "pe_device.h"
 #include "pe_tokens.h"
 
@@ -20,14 +21,9 @@ struct Sums {
   int64_t tokens, pages;
 };
 
-// Inclusive sums over the lanes of a wave of numbers of up to 63 bits.
-__device__ __forceinline__ int64_t wave_inclusive(int64_t v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int64_t o = __shfl_up(v, d);
-    if (lane_id() >= d) v += o;
-  }
-  return v;
+// Inclusive sums over the lanes of a wave of numbers of up to 31 bits: in two parts, which 32 bits hold.
+__device__ __forceinline__ int64_t wave_inclusive(uint32_t v) {
+  return (int64_t)wave_prefix_sum_u32(v & 0xffffffu) + ((int64_t)wave_prefix_sum_u32(v >> 24) << 24);
 }
 
 // First i in [0, n) with end[i] > x (end ascending; the last one is).
@@ -40,17 +36,21 @@ __device__ __forceinline__ int bracket(const int64_t* end, int n, int64_t x) {
   return lo;
 }
 
-// The first of this workgroup's pieces that reaches number x or lies behind it (what is dealt has fewer than 2^31 numbers; a sum
-// may be larger, no piece is taken there).
-__device__ __forceinline__ uint32_t first_piece(int64_t x) {
-  const uint32_t p = (uint32_t)((x < 0x7fffffffLL ? x : 0x7fffffffLL) / kThreads), turn = p % gridDim.x;
-  return p + (blockIdx.x >= turn ? blockIdx.x - turn : blockIdx.x + gridDim.x - turn);
-}
+struct Seqs {  // of the sequences that have just been summed
+  int64_t token_end[kThreads], page_end[kThreads];
+  int32_t have[kThreads], per_row[kThreads], len[kThreads], first[kThreads];
+  int8_t served[kThreads];  // 0: left as it was; 1: pages are there, its slots are not known; 2: and they are
+};
+struct Tokens {  // of a piece
+  int32_t seq[kThreads];  // -1: no slot
+  int32_t page[kThreads];  // in its row
+  int16_t slot[kThreads];
+};
 
-__global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a) {
-  __shared__ int64_t token_end[kThreads], page_end[kThreads];
-  __shared__ int32_t have_of[kThreads], per_row_of[kThreads], len_of[kThreads], first_of[kThreads];
-  __shared__ int8_t served_of[kThreads];  // 0: left as it was; 1: pages are there, its slots are not known; 2: and they are
+__global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a, const uint32_t token_pieces, const uint32_t pieces,
+                                                               const uint32_t inv_rows) {
+  __shared__ Seqs q;
+  __shared__ Tokens tok;
   __shared__ Sums wave_sums[kWaves];
   __shared__ int64_t dealt_of[kWaves];
 
@@ -60,17 +60,17 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a)
   const int64_t used = given < 0 ? 0 : given > a.num_free ? a.num_free : given;
   const int64_t left = a.num_free - used;
   Sums before{0, 0};
-  int64_t dealt = 0;  // (thread 0's, in the end the launch's)
+  int64_t dealt = 0;
 
   for (int s0 = 0; s0 < a.num_seqs; s0 += kThreads) {
     const int s = s0 + me, count = a.num_seqs - s0 < kThreads ? a.num_seqs - s0 : kThreads;
-    int64_t n = 0, need = 0;
-    int len = 0, have = 0, per_row = 0;
+    int n = 0, len = 0, have = 0, per_row = 0, first = 0;
     int64_t after = 0, kept = 0;
     bool fits = false;
     if (s < a.num_seqs) {
       len = a.seq_lens[s];
       n = a.new_lens[s];
+      first = a.first_positions != nullptr ? a.first_positions[s] : len;
       n = n < 0 ? 0 : n;
       const int64_t holds = len < 0 ? 0 : len;
       have = (int)((holds + B - 1) >> log2_block);
@@ -79,84 +79,104 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a)
       const int64_t pages = (kept + B - 1) >> log2_block;
       fits = len >= 0 && pages <= a.max_blocks && kept <= 0x7fffffffLL;
       if (fits) per_row = (int)(pages - have) + (holds == 0 && n > 0 ? a.n_spare : 0);
-      need = (int64_t)per_row * rows;
     }
-    const int64_t t_in = wave_inclusive(n), p_in = wave_inclusive(need);
-    __syncthreads();  // (those before may still be read)
+    const int need = per_row * rows;  // (the host keeps it under 2^31)
+    const int64_t t_in = wave_inclusive((uint32_t)n), p_in = wave_inclusive((uint32_t)need);
+    if (s0 > 0) __syncthreads();  // (what is written below may still be read)
     if (lane == kWave - 1) wave_sums[wave] = Sums{t_in, p_in};
     __syncthreads();
     Sums off = before;
-    for (int w = 0; w < wave; ++w) off.tokens += wave_sums[w].tokens, off.pages += wave_sums[w].pages;
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w)
+      if (w < wave) off.tokens += wave_sums[w].tokens, off.pages += wave_sums[w].pages;
     const int64_t t_end = off.tokens + t_in, p_end = off.pages + p_in;
     const bool served = fits && (need == 0 || p_end <= left);
-    token_end[me] = t_end;
-    page_end[me] = p_end;
-    have_of[me] = have;
-    per_row_of[me] = per_row;
-    len_of[me] = len;
-    served_of[me] = served ? (kept == after ? 2 : 1) : 0;
-    if (s < a.num_seqs) first_of[me] = a.first_positions != nullptr ? a.first_positions[s] : len;
-    int64_t mine = served && p_end <= left ? p_end : 0;  // the sums ascend: the last that the list holds has the most
+    q.token_end[me] = t_end;
+    q.page_end[me] = p_end;
+    q.have[me] = have;
+    q.per_row[me] = per_row;
+    q.len[me] = len;
+    q.served[me] = served ? (kept == after ? 2 : 1) : 0;
+    q.first[me] = first;
+    if (blockIdx.x == 0) {
+      // the sums ascend: the last that the list holds has the most
+      int64_t mine = served && p_end <= left ? p_end : 0;
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int64_t o = __shfl_xor(mine, d);
-      mine = o > mine ? o : mine;
-    }
-    if (lane == 0) dealt_of[wave] = mine;
-    if (blockIdx.x == 0 && s < a.num_seqs) {
-      a.seq_lens_out[s] = served ? (int32_t)kept : len;
-      if (a.cu_out != nullptr) {
-        if (s == 0) a.cu_out[0] = 0;
-        a.cu_out[s + 1] = (int32_t)(t_end < 0x7fffffffLL ? t_end : 0x7fffffffLL);
+      for (int d = 1; d < kWave; d *= 2) {
+        const int64_t o = __shfl_xor(mine, d);
+        mine = o > mine ? o : mine;
       }
-    }
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) dealt = dealt_of[w] > dealt ? dealt_of[w] : dealt;
-
-    // pages [before.pages, last) of the deal, those of this workgroup's pieces
-    const int64_t p_last = page_end[count - 1] < left ? page_end[count - 1] : left;
-    for (uint32_t piece = first_piece(before.pages); (int64_t)piece * kThreads < p_last; piece += gridDim.x) {
-      const int64_t p = (int64_t)piece * kThreads + me;
-      if (p < before.pages || p >= p_last) continue;
-      const int i = bracket(page_end, count, p);
-      if (!served_of[i]) continue;
-      const int per = per_row_of[i];
-      const uint32_t in = (uint32_t)(p - (i > 0 ? page_end[i - 1] : before.pages));  // (the host keeps a sequence's under 2^31)
-      const int h = (int)(in / (uint32_t)per), j = (int)(in - (uint32_t)h * (uint32_t)per);
-      const bool begins = len_of[i] == 0 && a.n_spare > 0;  // (only one that brings tokens has pages here)
-      const int of_table = begins ? per - a.n_spare : per;
-      const int64_t row = (int64_t)(s0 + i) * rows + h;
-      const int32_t page = a.free_pages[used + p];
-      if (j < of_table)
-        a.block_table[row * a.max_blocks + have_of[i] + j] = page;
-      else
-        a.spare[row * a.n_spare + (j - of_table)] = page;
-    }
-
-    // tokens [before.tokens, last)
-    if (a.positions_out != nullptr || a.slots_out != nullptr) {
-      const int64_t t_last = token_end[count - 1] < a.total_tokens ? token_end[count - 1] : a.total_tokens;
-      for (uint32_t piece = first_piece(before.tokens); (int64_t)piece * kThreads < t_last; piece += gridDim.x) {
-        const int64_t t = (int64_t)piece * kThreads + me;
-        if (t < before.tokens || t >= t_last) continue;
-        const int i = bracket(token_end, count, t);
-        const int64_t nth = t - (i > 0 ? token_end[i - 1] : before.tokens);
-        if (a.positions_out != nullptr) a.positions_out[t] = (int32_t)((uint32_t)first_of[i] + (uint32_t)nth);
-        if (a.slots_out == nullptr) continue;
-        const int64_t at = len_of[i] + nth;
-        const int j = (int)(at >> log2_block), slot = (int)at & (B - 1);
-        const int64_t start = used + (i > 0 ? page_end[i - 1] : before.pages);
-        for (int h = 0; h < rows; ++h) {
-          int32_t page = -1;
-          if (served_of[i] == 2)
-            page = j < have_of[i] ? a.block_table[((int64_t)(s0 + i) * rows + h) * a.max_blocks + j]
-                                  : a.free_pages[start + (int64_t)h * per_row_of[i] + (j - have_of[i])];
-          a.slots_out[t * rows + h] = page < 0 ? -1 : (int64_t)page * B + slot;
+      if (lane == 0) dealt_of[wave] = mine;
+      if (s < a.num_seqs) {
+        a.seq_lens_out[s] = served ? (int32_t)kept : len;
+        if (a.cu_out != nullptr) {
+          if (s == 0) a.cu_out[0] = 0;
+          a.cu_out[s + 1] = (int32_t)(t_end < 0x7fffffffLL ? t_end : 0x7fffffffLL);
         }
       }
     }
     __syncthreads();
-    before = Sums{token_end[count - 1], page_end[count - 1]};
+    if (blockIdx.x == 0) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) dealt = dealt_of[w] > dealt ? dealt_of[w] : dealt;
+    }
+    const int64_t t_last = q.token_end[count - 1] < a.total_tokens ? q.token_end[count - 1] : a.total_tokens;
+    const int64_t p_last = q.page_end[count - 1] < left ? q.page_end[count - 1] : left;
+
+    for (uint32_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+      if (piece < token_pieces) {
+        const int64_t t0 = (int64_t)piece * kThreads;
+        if (t0 >= t_last || t0 + kThreads <= before.tokens) continue;
+        const int64_t t = t0 + me;
+        int seq = -1;
+        if (t >= before.tokens && t < t_last) {
+          const int i = bracket(q.token_end, count, t);
+          const int64_t nth = t - (i > 0 ? q.token_end[i - 1] : before.tokens);
+          if (a.positions_out != nullptr) a.positions_out[t] = (int32_t)((uint32_t)q.first[i] + (uint32_t)nth);
+          const int64_t at = q.len[i] + nth;
+          seq = q.served[i] == 2 ? i : -1;
+          tok.page[me] = (int)(at >> log2_block);
+          tok.slot[me] = (int16_t)(at & (B - 1));
+        }
+        if (a.slots_out == nullptr) continue;
+        tok.seq[me] = seq;
+        __syncthreads();
+        // a thread for each (token, row), rows side by side as they are stored
+        const int begin = (int)(before.tokens > t0 ? before.tokens - t0 : 0), end = (int)(t_last - t0 < kThreads ? t_last - t0 : kThreads);
+#pragma unroll 4
+        for (int idx = begin * rows + me; idx < end * rows; idx += kThreads) {
+          const int k = inv_rows == ~0u ? idx / rows : inv_rows != 0u ? (int)((uint64_t)(uint32_t)idx * inv_rows >> 32) : idx, h = idx - k * rows;
+          const int i = tok.seq[k];
+          int32_t page = -1;
+          if (i >= 0) {
+            const int j = tok.page[k], more = j - q.have[i];
+            const int64_t start = used + (i > 0 ? q.page_end[i - 1] : before.pages);
+            const int32_t* from = more < 0 ? a.block_table + (((int64_t)(s0 + i) * rows + h) * a.max_blocks + j)
+                                           : a.free_pages + (start + (int64_t)h * q.per_row[i] + more);
+            page = *from;
+          }
+          a.slots_out[t0 * rows + idx] = page < 0 ? -1 : ((int64_t)page << log2_block) + tok.slot[k];
+        }
+        __syncthreads();
+      } else {
+        const int64_t p = (int64_t)(piece - token_pieces) * kThreads + me;
+        if (p < before.pages || p >= p_last) continue;
+        const int i = bracket(q.page_end, count, p);
+        if (!q.served[i]) continue;
+        const int per = q.per_row[i];
+        const uint32_t in = (uint32_t)(p - (i > 0 ? q.page_end[i - 1] : before.pages));
+        const int32_t page = a.free_pages[used + p];
+        const int h = (int)(in / (uint32_t)per), j = (int)(in - (uint32_t)h * (uint32_t)per);
+        const bool begins = q.len[i] == 0 && a.n_spare > 0;  // (only one that brings tokens has pages here)
+        const int of_table = begins ? per - a.n_spare : per;
+        const int64_t row = (int64_t)(s0 + i) * rows + h;
+        if (j < of_table)
+          a.block_table[row * a.max_blocks + q.have[i] + j] = page;
+        else
+          a.spare[row * a.n_spare + (j - of_table)] = page;
+      }
+    }
+    before = Sums{q.token_end[count - 1], q.page_end[count - 1]};
   }
 
   if (blockIdx.x == 0 && me == 0) *a.free_used_out = (int32_t)(used + dealt);
@@ -171,13 +191,16 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a)
 }  // namespace
 
 hipError_t launch_plan_tokens(const PlanArgs& a, int compute_units, hipStream_t stream) {
-  // a workgroup for a piece of tokens or of pages (as many as a table could take), two a compute unit at most
-  const int64_t pages = (int64_t)a.num_seqs * a.rows_per_seq * (a.max_blocks + (int64_t)a.n_spare);
-  const int64_t most = pages < a.num_free ? pages : a.num_free, work = most > a.total_tokens ? most : a.total_tokens;
-  int64_t groups = (work + kThreads - 1) / kThreads;
-  if (groups > 2LL * compute_units) groups = 2LL * compute_units;
-  if (groups < 1) groups = 1;
-  hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+  const int64_t room = (int64_t)a.num_seqs * a.rows_per_seq * (a.max_blocks + (int64_t)a.n_spare);
+  const int64_t pages = room < a.num_free ? room : a.num_free;
+  const bool tokens = a.positions_out != nullptr || a.slots_out != nullptr;
+  const uint32_t token_pieces = tokens ? (uint32_t)((a.total_tokens + kThreads - 1) / kThreads) : 0u;
+  const uint32_t pieces = token_pieces + (uint32_t)((pages + kThreads - 1) / kThreads);
+  // a workgroup a piece, as many as the compute units hold at once
+  const uint32_t most = 8u * (uint32_t)compute_units, groups = pieces < most ? pieces : most;
+  // idx / rows is the upper half of idx * inv_rows as long as idx * rows < 2^32 (idx < kThreads * rows); ~0: divided
+  const uint32_t rows = (uint32_t)a.rows_per_seq, inv_rows = rows == 1 ? 0u : rows < 4096 ? (uint32_t)((1ull << 32) / rows + 1) : ~0u;
+  hipLaunchKernelGGL(plan_tokens_kernel, dim3(groups < 1 ? 1 : groups), dim3(kThreads), 0, stream, a, token_pieces, pieces, inv_rows);
   return hipGetLastError();
 }
 

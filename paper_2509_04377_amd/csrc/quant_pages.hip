@@ -67,78 +67,59 @@ struct Page {
   static constexpr int kTokens = kLoads * TPL;                             // of a wave
   static_assert(kWaves * kLoads == kAll, "whole waves");
 };
-constexpr int kMostWaves = 8;
-
-// What the waves of a workgroup leave for one another.
-template <int B, int PAGES>
-struct Shared {
-  float most[kMostWaves][2];
-  double ratio[PAGES][B];
-};
-
-// A page in registers: k[i], v[i] hold the lane's 16 bytes of token (wave in page) * kTokens + i * TPL + lane / LPR.  All waves of the workgroup
-// call this together (`real`: the wave has a page).  to: the page's number in the cache; part: the head's first byte in the page; row_bytes:
-// bytes between a head's consecutive tokens.
-template <typename T, int D, int B, int PAGES>
-__device__ __forceinline__ void round_page(const uint4 (&k)[Page<T, D, B>::kLoads], const uint4 (&v)[Page<T, D, B>::kLoads], bool real, int slot,
-                                           int part_wave, Shared<B, PAGES>& sm, const pe_quant_cache& cache, int64_t page_byte, int row_bytes,
-                                           int64_t scale_at, float* score) {
+// What a wave does with its part of a page: k[i], v[i] hold the lane's 16 bytes of token (part) * kTokens + i * TPL + lane / LPR.
+template <typename T, int D, int B>
+struct Part {
   using P = Page<T, D, B>;
-  constexpr int N = Elem<T>::kPerVec;
-  const int lane = lane_id();
-  float mk = 0.f, mv = 0.f;
+  static constexpr int kLoads = P::kLoads;
+
+  static __device__ __forceinline__ void most(const uint4 (&k)[kLoads], const uint4 (&v)[kLoads], float& mk, float& mv) {
+    mk = mv = 0.f;
 #pragma unroll
-  for (int i = 0; i < P::kLoads; ++i) {
-    mk = fmaxf(mk, vec_most<T>(k[i]));
-    mv = fmaxf(mv, vec_most<T>(v[i]));
-  }
-  mk = wave_max(mk);
-  mv = wave_max(mv);
-  if constexpr (P::kWaves > 1) {
-    const int wave = slot * P::kWaves + part_wave;
-    if (lane == 0) sm.most[wave][0] = mk, sm.most[wave][1] = mv;
-  }
-  if (score != nullptr) {
-    double part[2 * P::kLoads];
-#pragma unroll
-    for (int i = 0; i < P::kLoads; ++i) {
-      part[i] = sumsq_vec<T>(k[i], 0.0);
-      part[P::kLoads + i] = sumsq_vec<T>(v[i], 0.0);
+    for (int i = 0; i < kLoads; ++i) {
+      mk = fmaxf(mk, vec_most<T>(k[i]));
+      mv = fmaxf(mv, vec_most<T>(v[i]));
     }
-    const double ratio = token_ratio_from_partials<P::kLoads, P::LPR>(part, lane);
-    // every lane holds one of its token rows' ratios: load bit_reverse((lane >> 1) & (kLoads - 1))
-    const int i = bit_reverse<ilog2(P::kLoads)>((lane >> 1) & (P::kLoads - 1));
-    const int in_row = lane % P::LPR;
-    if (in_row < 2 * P::kLoads && (in_row & 1) == 0) sm.ratio[slot][part_wave * P::kTokens + i * P::TPL + lane / P::LPR] = ratio;
+    mk = wave_max(mk);
+    mv = wave_max(mv);
   }
-  __syncthreads();
-  if constexpr (P::kWaves > 1) {
+
+  // The tokens' norm ratios, to[token of the page].
+  static __device__ __forceinline__ void ratios(const uint4 (&k)[kLoads], const uint4 (&v)[kLoads], int part, double* to) {
+    const int lane = lane_id();
+    double sums[2 * kLoads];
 #pragma unroll
-    for (int w = 0; w < P::kWaves; ++w) {
-      mk = fmaxf(mk, sm.most[slot * P::kWaves + w][0]);
-      mv = fmaxf(mv, sm.most[slot * P::kWaves + w][1]);
+    for (int i = 0; i < kLoads; ++i) {
+      sums[i] = sumsq_vec<T>(k[i], 0.0);
+      sums[kLoads + i] = sumsq_vec<T>(v[i], 0.0);
+    }
+    const double ratio = token_ratio_from_partials<kLoads, P::LPR>(sums, lane);
+    // every lane holds one of its token rows' ratios: that of load bit_reverse((lane >> 1) & (kLoads - 1))
+    const int i = bit_reverse<ilog2(kLoads)>((lane >> 1) & (kLoads - 1)), in_row = lane % P::LPR;
+    if (in_row < 2 * kLoads && (in_row & 1) == 0) to[part * P::kTokens + i * P::TPL + lane / P::LPR] = ratio;
+  }
+
+  // page_byte: of the head's first element in the pools; row_bytes: between its consecutive tokens.
+  static __device__ __forceinline__ void store(const uint4 (&k)[kLoads], const uint4 (&v)[kLoads], int part, const pe_quant_cache& cache,
+                                               int64_t page_byte, int row_bytes, float inv_k, float inv_v) {
+    const int lane = lane_id();
+    const int64_t lane_byte = page_byte + (int64_t)(part * P::kTokens + lane / P::LPR) * row_bytes + lane % P::LPR * Elem<T>::kPerVec;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int64_t at = lane_byte + (int64_t)i * P::TPL * row_bytes;
+      store_e4m3<T>(static_cast<char*>(cache.k) + at, k[i], inv_k);
+      store_e4m3<T>(static_cast<char*>(cache.v) + at, v[i], inv_v);
     }
   }
-  if (!real) return;
-  const int ek = scale_exponent(mk), ev = scale_exponent(mv);
-  const float ik = exp2i(-ek), iv = exp2i(-ev);
-  const int64_t lane_byte = page_byte + (int64_t)(part_wave * P::kTokens + lane / P::LPR) * row_bytes + lane % P::LPR * N;
-#pragma unroll
-  for (int i = 0; i < P::kLoads; ++i) {
-    const int64_t at = lane_byte + (int64_t)i * P::TPL * row_bytes;
-    store_e4m3<T>(static_cast<char*>(cache.k) + at, k[i], ik);
-    store_e4m3<T>(static_cast<char*>(cache.v) + at, v[i], iv);
-  }
-  if (part_wave == 0 && lane == 0) {
-    *reinterpret_cast<float2*>(cache.scales + scale_at) = make_float2(exp2i(ek), exp2i(ev));
-    if (score != nullptr) {
-      double sum = 0.0;
+
+  // The mean of a page's ratios, in slot order, rounded once.
+  static __device__ __forceinline__ float score(const double* ratio) {
+    double sum = 0.0;
 #pragma unroll 16
-      for (int t = 0; t < B; ++t) sum += sm.ratio[slot][t];
-      *score = (float)(sum / (double)B);
-    }
+    for (int t = 0; t < B; ++t) sum += ratio[t];
+    return (float)(sum / (double)B);
   }
-}
+};
 
 // Workgroups of four waves (eight where a page takes them); page j of a row is its slot (j % PAGES)'s in workgroup j / PAGES.
 template <typename T, int D, int B>
@@ -152,8 +133,9 @@ template <typename T, int D, int B>
 __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_pages_kernel(const QuantPagesArgs a, int groups_per_row) {
   using P = Page<T, D, B>;
   constexpr int kPages = Groups<T, D, B>::kPages;
-  constexpr int N = Elem<T>::kPerVec;
-  __shared__ Shared<B, kPages> sm;
+  using PT = Part<T, D, B>;
+  __shared__ float most_of[Groups<T, D, B>::kWaves][2];
+  __shared__ double ratio[kPages][B];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int slot = wave / P::kWaves, part_wave = wave % P::kWaves;
   const int row = (int)(blockIdx.x / (unsigned)groups_per_row), s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
@@ -178,9 +160,26 @@ __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_pages
     for (int i = 0; i < P::kLoads; ++i) k[i] = load_vec_stream(kp, real ? lane_vec + (int64_t)i * P::TPL * heads * P::LPR : 0);
 #pragma unroll
     for (int i = 0; i < P::kLoads; ++i) v[i] = load_vec_stream(vp, real ? lane_vec + (int64_t)i * P::TPL * heads * P::LPR : 0);
-    // (one barrier inside, which all waves of the workgroup reach: here, or in the other branch)
-    round_page<T, D, B, kPages>(k, v, real, slot, part_wave, sm, a.cache, ((int64_t)to * B * heads + head_row) * D, heads * D,
-                                ((int64_t)to * heads + head_row) * 2, a.scores != nullptr ? a.scores + (int64_t)row * a.max_blocks + j : nullptr);
+    float mk, mv;
+    PT::most(k, v, mk, mv);
+    if (P::kWaves > 1 && lane == 0) most_of[wave][0] = mk, most_of[wave][1] = mv;
+    if (a.scores != nullptr) PT::ratios(k, v, part_wave, ratio[slot]);
+    __syncthreads();  // (as in the other branch: every wave of the workgroup reaches one)
+    if constexpr (P::kWaves > 1) {
+#pragma unroll
+      for (int w = 0; w < P::kWaves; ++w) {
+        mk = fmaxf(mk, most_of[slot * P::kWaves + w][0]);
+        mv = fmaxf(mv, most_of[slot * P::kWaves + w][1]);
+      }
+    }
+    if (real) {
+      const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+      PT::store(k, v, part_wave, a.cache, ((int64_t)to * B * heads + head_row) * D, heads * D, exp2i(-ek), exp2i(-ev));
+      if (part_wave == 0 && lane == 0) {
+        *reinterpret_cast<float2*>(a.cache.scales + ((int64_t)to * heads + head_row) * 2) = make_float2(exp2i(ek), exp2i(ev));
+        if (a.scores != nullptr) a.scores[(int64_t)row * a.max_blocks + j] = PT::score(ratio[slot]);
+      }
+    }
     if (!real && a.scores != nullptr && part_wave == 0 && lane == 0) a.scores[(int64_t)row * a.max_blocks + j] = __builtin_inff();
   } else {
     __syncthreads();
@@ -230,52 +229,73 @@ __device__ __forceinline__ T as(float x) {
     return T{f32_to_bf16(x)};
 }
 
-// One workgroup a row: thread i turns pair i % (D/2) of one of the row's query heads, or of the key, and takes its part of the value.  The
-// new token meets the rest of its page, where it fills it, in LDS.
+// One wave a row, four rows a workgroup.  Lane l turns pair l % (D/2) of the row's key and query heads and takes its part of the value; the
+// new token's rows meet in LDS, from where they go to the tail, and where they fill the page join the rest of it.  A page larger than
+// a wave's registers is read twice (out of the second-level cache): once in every B steps.
+constexpr int kAppendWaves = 4;
+
 template <typename T, int D, int B>
-__global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_append_kernel(const QuantAppendArgs a, const AppendRope rope) {
+__global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(const QuantAppendArgs a, const AppendRope rope) {
   using P = Page<T, D, B>;
-  constexpr int kThreads = Groups<T, D, B>::kWaves * kWave, kPairs = D / 2;
-  __shared__ Shared<B, 1> sm;
-  __shared__ __attribute__((aligned(16))) T now[2][D];
-  const int me = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(me / kWave);
-  const int row = (int)blockIdx.x, s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
+  using PT = Part<T, D, B>;
+  constexpr int kPairs = D / 2, kAtOnce = kWave / kPairs;  // heads that a wave takes at once
+  __shared__ __attribute__((aligned(16))) T sm_now[kAppendWaves][2][D];
+  __shared__ double sm_ratio[kAppendWaves][B];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int row = (int)blockIdx.x * kAppendWaves + wave;
+  if (row >= a.num_seqs * a.num_kv_heads) return;
+  const int s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
+  T(*now)[D] = sm_now[wave];
   const int len = a.seq_lens[s];
-  const int slot = len & (B - 1), jb = len / B;
-  const bool runs = len >= 0 && jb < a.max_blocks;
-  if (hk == 0 && me == 0) a.seq_lens_out[s] = runs ? len + 1 : len;
+  const int64_t table_row = a.shared ? s : row;
   const int G = a.num_q_heads / a.num_kv_heads;
-  const T* new_k = static_cast<const T*>(a.new_k) + (int64_t)row * D;
-  const T* new_v = static_cast<const T*>(a.new_v) + (int64_t)row * D;
-  const int p = me & (kPairs - 1);
+  const int p = lane & (kPairs - 1);
   const bool turned = p < rope.pairs;
   const int ea = turned && !rope.interleaved ? p : 2 * p, eb = turned && !rope.interleaved ? p + rope.pairs : 2 * p + 1;
+  // the row's key, its value, then its queries (where they are turned)
+  const int heads = 2 + (rope.pairs > 0 ? G : 0);
+  constexpr int kSteps = (2 + 8 + kAtOnce - 1) / kAtOnce;
+  float x[kSteps], y[kSteps];
+  const int64_t q0 = ((int64_t)s * a.num_q_heads + (int64_t)hk * G) * D;
+  const auto base_of = [&](int h) -> const T* {
+    return h == 0 ? static_cast<const T*>(a.new_k) + (int64_t)row * D : h == 1 ? static_cast<const T*>(a.new_v) + (int64_t)row * D
+                                                                              : static_cast<const T*>(a.q) + q0 + (int64_t)(h - 2) * D;
+  };
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int h = i * kAtOnce + lane / kPairs;
+    if (h < heads) {
+      const T* from = base_of(h);
+      x[i] = get(from, ea), y[i] = get(from, eb);
+    }
+  }
   Turn w{1.f, 0.f};
   if (turned) {
     w = turn_of(rope.turns[p], a.positions[s]);
     w.c *= rope.magnitude;
     w.s *= rope.magnitude;
   }
-  // heads of the row: its key, its value, then its queries (where they are turned)
-  const int heads = 2 + (rope.pairs > 0 ? G : 0);
-  for (int h = me / kPairs; h < heads; h += kThreads / kPairs) {
-    const int64_t qh = ((int64_t)s * a.num_q_heads + hk * G + (h - 2)) * D;
-    const T* from = h == 0 ? new_k : h == 1 ? new_v : static_cast<const T*>(a.q) + qh;
-    const float x = get(from, ea), y = get(from, eb);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int h = i * kAtOnce + lane / kPairs;
+    if (h >= heads) continue;
     const bool turn = turned && h != 1;
-    const T u = as<T>(turn ? x * w.c - y * w.s : x), v = as<T>(turn ? y * w.c + x * w.s : y);
+    const T u = as<T>(turn ? x[i] * w.c - y[i] * w.s : x[i]), v = as<T>(turn ? y[i] * w.c + x[i] * w.s : y[i]);
     if (h < 2) {
       now[h][ea] = u, now[h][eb] = v;
     } else {
-      T* to = static_cast<T*>(a.q_out) + qh;
+      T* to = static_cast<T*>(a.q_out) + q0 + (int64_t)(h - 2) * D;
       to[ea] = u, to[eb] = v;
     }
   }
-  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's accesses to LDS are carried out in order)
+
+  const int slot = len & (B - 1), jb = len / B;
+  const bool runs = len >= 0 && jb < a.max_blocks;
+  if (hk == 0 && lane == 0) a.seq_lens_out[s] = runs ? len + 1 : len;
   if (!runs) return;
-  const int64_t table_row = a.shared ? s : row;
   int32_t* entry = a.block_table + table_row * a.max_blocks + jb;
-  if (slot == 0 && me == 0 && (!a.shared || hk == 0)) {
+  if (slot == 0 && lane == 0 && (!a.shared || hk == 0)) {
     int page = a.freed_phys[table_row];
     if (page >= 0) {
       a.freed_phys[table_row] = -1;
@@ -288,36 +308,52 @@ __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_appen
   }
   uint4* kt = static_cast<uint4*>(a.cache.k_tail) + (int64_t)row * B * P::LPR;
   uint4* vt = static_cast<uint4*>(a.cache.v_tail) + (int64_t)row * B * P::LPR;
-  if (me < 2 * P::LPR) {
-    const int kv = me / P::LPR, u = me % P::LPR;
+  if (lane < 2 * P::LPR) {
+    const int kv = lane / P::LPR, u = lane % P::LPR;
     (kv ? vt : kt)[slot * P::LPR + u] = reinterpret_cast<const uint4*>(now[kv])[u];
   }
   if (slot != B - 1) return;
   // the page is full: its other tokens from the tail, the last one from LDS
   const int page = *entry;
-  const bool real = page >= 0 && wave < P::kWaves;
-  uint4 k[P::kLoads], v[P::kLoads];
-#pragma unroll
-  for (int i = 0; i < P::kLoads; ++i) {
-    const int t = (real ? wave * P::kTokens : 0) + i * P::TPL + lane / P::LPR, u = lane % P::LPR;
-    const bool last = t == B - 1;
-    k[i] = last ? reinterpret_cast<const uint4*>(now[0])[u] : kt[t * P::LPR + u];
-    v[i] = last ? reinterpret_cast<const uint4*>(now[1])[u] : vt[t * P::LPR + u];
-  }
+  if (page < 0) return;  // spare list exhausted (precondition violated): the page is dropped
   const int rows = a.shared ? a.num_kv_heads : 1, head_row = a.shared ? hk : 0;
-  // (waves beyond those that hold the page take part in the barrier alone)
-  if (wave >= P::kWaves) {
-    __syncthreads();
-    return;
+  uint4 k[P::kLoads], v[P::kLoads];
+  const auto load = [&](int part) {
+#pragma unroll
+    for (int i = 0; i < P::kLoads; ++i) {
+      const int t = part * P::kTokens + i * P::TPL + lane / P::LPR, u = lane % P::LPR;
+      const bool last = t == B - 1;
+      k[i] = last ? reinterpret_cast<const uint4*>(now[0])[u] : kt[t * P::LPR + u];
+      v[i] = last ? reinterpret_cast<const uint4*>(now[1])[u] : vt[t * P::LPR + u];
+    }
+  };
+  float most_k = 0.f, most_v = 0.f;
+#pragma unroll 1
+  for (int part = 0; part < P::kWaves; ++part) {
+    load(part);
+    float mk, mv;
+    PT::most(k, v, mk, mv);
+    most_k = fmaxf(most_k, mk);
+    most_v = fmaxf(most_v, mv);
+    if (a.scores != nullptr) PT::ratios(k, v, part, sm_ratio[wave]);
   }
-  round_page<T, D, B, 1>(k, v, real, 0, wave, sm, a.cache, ((int64_t)page * B * rows + head_row) * D, rows * D,
-                         ((int64_t)page * rows + head_row) * 2, a.scores != nullptr ? a.scores + (int64_t)row * a.max_blocks + jb : nullptr);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int ek = scale_exponent(most_k), ev = scale_exponent(most_v);
+#pragma unroll 1
+  for (int part = 0; part < P::kWaves; ++part) {
+    if (P::kWaves > 1) load(part);
+    PT::store(k, v, part, a.cache, ((int64_t)page * B * rows + head_row) * D, rows * D, exp2i(-ek), exp2i(-ev));
+  }
+  if (lane == 0) {
+    *reinterpret_cast<float2*>(a.cache.scales + ((int64_t)page * rows + head_row) * 2) = make_float2(exp2i(ek), exp2i(ev));
+    if (a.scores != nullptr) a.scores[(int64_t)row * a.max_blocks + jb] = PT::score(sm_ratio[wave]);
+  }
 }
 
 template <typename T, int D, int B>
 hipError_t launch_append(const QuantAppendArgs& a, const AppendRope& rope, hipStream_t stream) {
-  hipLaunchKernelGGL((quant_append_kernel<T, D, B>), dim3((unsigned)(a.num_seqs * a.num_kv_heads)), dim3(Groups<T, D, B>::kWaves * kWave), 0,
-                     stream, a, rope);
+  const unsigned groups = (unsigned)((a.num_seqs * a.num_kv_heads + kAppendWaves - 1) / kAppendWaves);
+  hipLaunchKernelGGL((quant_append_kernel<T, D, B>), dim3(groups), dim3(kAppendWaves * kWave), 0, stream, a, rope);
   return hipGetLastError();
 }
 

@@ -118,6 +118,11 @@ def test_many_tokens():
     _run([0, 3, 0], [5000, 20001, 7777], 5, 16, extra_blocks=3)
 
 
+@pytest.mark.parametrize("Hk", [1, 7, 8, 63, 4095, 4096, 5003])
+def test_many_heads(Hk):
+    _run([0, 3, 16], [20, 1, 17], Hk, 16)
+
+
 def test_missing_pages_give_no_slot():
     """A row of a sequence that goes on without its page."""
     lens, new, B, width = _i32([20]), _i32([3]), 16, 3
