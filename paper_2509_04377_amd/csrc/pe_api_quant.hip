@@ -122,9 +122,11 @@ int pe_quant_decode(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
   a.is_bf16 = bf16;
   a.shared = desc->layout == PE_LAYOUT_SHARED;
   const int64_t groups = (int64_t)desc->num_seqs * desc->num_kv_heads * splits;
-  a.waves = groups <= compute_units() ? 8 : 4;
+  a.waves = pe::quant_waves(desc, splits);
+  a.depth = pe::quant_depth(desc, splits, a.waves);
+  // the splits are merged by the last of a row to arrive where that pays (pe_decode_common.h), and where the output can hold tags before it is written
   const int heads = desc->num_q_heads / desc->num_kv_heads;
-  if (splits > 1 && splits <= pe::most_arrivals(heads) && heads * desc->head_dim <= 128 * a.waves && groups <= 2LL * compute_units() &&
+  if (splits > 1 && splits <= pe::most_arrivals(heads) && (heads > 4 ? 8 : 4) * desc->head_dim <= 128 * a.waves && groups <= 2LL * compute_units() &&
       aligned(out, 8) && out != q) {
     a.tagged = true;
     a.tag = launch_tag();

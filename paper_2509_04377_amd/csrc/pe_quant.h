@@ -59,14 +59,41 @@ struct QuantDecodeArgs {
   bool tagged = false;  // splits merged by the last of a row to arrive
   uint64_t tag = 0;
 };
-// Splits of a row: as many as leave no compute unit two workgroups, none shorter than 256 tokens of the table row.
+// Splits of a row.  The host sees the length of a table row, not of the sequences, so a count has to pay on full rows and on rows of unequal
+// length (37 tokens to all; four query heads a KV head, us, best count / others; measured on an MI355X, fp32 the same order):
+//   - up to half as many rows as compute units: as many as leave no compute unit two workgroups, of 128 tokens or more (64 rows of D = 128 x
+//     1024 in four 6.7, x 4096 in four 12.5; eight rows x 4096 in 32 6.7, in sixteen 7.1), two only of 512 or more (128 rows x 1024 in two 8.5, x 512
+//     whole 6.4 / 6.8); rows of 32 KiB of K whole (eight of D = 64 x 512 whole 4.7 / 4.8, of D = 128 x 512 in four 5.3 / 5.9 whole);
+//   - more, of 2048 tokens or more: three up to five eighths of the compute units (D = 128, 160 rows x 2048 in three 15.3, whole 16.1, ragged 11.6 / 13),
+//     four up to three quarters (192 rows x 2048 full in four 18.1, whole 17.1, ragged 12.7 / 15), else whole (224 rows 18.9, in three 20.9, ragged
+//     15.4 / 14.3); shorter ones whole (160 rows x 1024 9.8, in three 10.2, ragged 8.8 / 8.7);
+//   - a few more rows than compute units, of 2048 or more, four (264 rows of D = 64 x 2048 14.4, whole 16.7; of D = 128 x 4096 48.4 / 58; not 384 rows
+//     x 2048 of D = 64: whole 17.4, in two 18.4).
 inline int quant_splits(const pe_cache_desc* d) {
   if (d->decode_splits > 0) return d->decode_splits;
   const int64_t rows = (int64_t)d->num_seqs * d->num_kv_heads, tokens = (int64_t)d->max_blocks * d->block_size;
-  int64_t splits = host::compute_units() / rows;
-  if (splits > tokens / 256) splits = tokens / 256;
+  const int64_t cus = host::compute_units(), fit = cus / rows;
+  if (tokens * d->head_dim <= 32768) return 1;
+  if (fit < 2) {
+    if (tokens < 2048) return 1;
+    if (rows > cus) return rows * 10 <= cus * 13 ? 4 : 1;
+    return rows * 8 <= cus * 5 ? 3 : rows * 4 <= cus * 3 ? 4 : 1;
+  }
+  int64_t splits = tokens / (fit == 2 ? 512 : 128);
+  if (splits > fit) splits = fit;
   return splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
 }
+
+// The workgroup: eight waves, four where split rows make more workgroups than compute units (192 rows of D = 128 x 2048, ragged, in four 12.7, with eight
+// waves 14.6), and tiles in flight a wave: one (256 rows of D = 128 x 2048 21.4, two 21.5; 64 x 1024 in four 6.75 / 6.9), two for D = 64 in long
+// pieces, whose wave-loads are half as long (256 rows x 2048 12.3, one 13.6; 64 rows x 4096 in four 9.0 / 9.4; pieces of 256 5.5, two 6.3).
+inline int quant_waves(const pe_cache_desc* d, int splits) {
+  return splits > 1 && (int64_t)d->num_seqs * d->num_kv_heads * splits > host::compute_units() ? 4 : 8;
+}
+inline int quant_depth(const pe_cache_desc* d, int splits, int waves) {
+  return d->head_dim == 64 && waves == 8 && (int64_t)d->max_blocks * d->block_size / splits >= 1024 ? 2 : 1;
+}
+
 inline size_t quant_workspace_bytes(const pe_cache_desc* d) {
   return decode_partials_bytes(d->num_seqs, d->num_q_heads, d->head_dim, quant_splits(d));
 }
