@@ -41,16 +41,17 @@ struct Seqs {  // of the sequences that have just been summed
   int32_t have[kThreads], per_row[kThreads], len[kThreads], first[kThreads];
   int8_t served[kThreads];  // 0: left as it was; 1: pages are there, its slots are not known; 2: and they are
 };
-struct Tokens {  // of a piece
-  int32_t seq[kThreads];  // -1: no slot
-  int32_t page[kThreads];  // in its row
-  int16_t slot[kThreads];
+struct __attribute__((aligned(16))) Token {  // of a piece: where the pages of its rows stand, `step` entries apart
+  int64_t at;
+  int32_t step;
+  int32_t slot;  // in its page; kInTable: the pages are in the table, not among the free ones; negative: no slot
 };
+constexpr int kInTable = 1 << 16;
 
 __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a, const uint32_t token_pieces, const uint32_t pieces,
                                                                const uint32_t inv_rows) {
   __shared__ Seqs q;
-  __shared__ Tokens tok;
+  __shared__ Token tok[kThreads];
   __shared__ Sums wave_sums[kWaves];
   __shared__ int64_t dealt_of[kWaves];
 
@@ -128,34 +129,35 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a,
         const int64_t t0 = (int64_t)piece * kThreads;
         if (t0 >= t_last || t0 + kThreads <= before.tokens) continue;
         const int64_t t = t0 + me;
-        int seq = -1;
+        Token mine{0, 0, -1};
         if (t >= before.tokens && t < t_last) {
           const int i = bracket(q.token_end, count, t);
           const int64_t nth = t - (i > 0 ? q.token_end[i - 1] : before.tokens);
           if (a.positions_out != nullptr) a.positions_out[t] = (int32_t)((uint32_t)q.first[i] + (uint32_t)nth);
           const int64_t at = q.len[i] + nth;
-          seq = q.served[i] == 2 ? i : -1;
-          tok.page[me] = (int)(at >> log2_block);
-          tok.slot[me] = (int16_t)(at & (B - 1));
+          if (q.served[i] == 2) {
+            const int j = (int)(at >> log2_block), more = j - q.have[i], slot = (int)at & (B - 1);
+            if (more < 0)
+              mine = Token{(int64_t)(s0 + i) * rows * a.max_blocks + j, a.max_blocks, slot | kInTable};
+            else
+              mine = Token{used + (i > 0 ? q.page_end[i - 1] : before.pages) + more, q.per_row[i], slot};
+          }
         }
         if (a.slots_out == nullptr) continue;
-        tok.seq[me] = seq;
+        tok[me] = mine;
         __syncthreads();
         // a thread for each (token, row), rows side by side as they are stored
         const int begin = (int)(before.tokens > t0 ? before.tokens - t0 : 0), end = (int)(t_last - t0 < kThreads ? t_last - t0 : kThreads);
 #pragma unroll 4
         for (int idx = begin * rows + me; idx < end * rows; idx += kThreads) {
           const int k = inv_rows == ~0u ? idx / rows : inv_rows != 0u ? (int)((uint64_t)(uint32_t)idx * inv_rows >> 32) : idx, h = idx - k * rows;
-          const int i = tok.seq[k];
-          int32_t page = -1;
-          if (i >= 0) {
-            const int j = tok.page[k], more = j - q.have[i];
-            const int64_t start = used + (i > 0 ? q.page_end[i - 1] : before.pages);
-            const int32_t* from = more < 0 ? a.block_table + (((int64_t)(s0 + i) * rows + h) * a.max_blocks + j)
-                                           : a.free_pages + (start + (int64_t)h * q.per_row[i] + more);
-            page = *from;
+          const Token of = tok[k];
+          int64_t slot = -1;
+          if (of.slot >= 0) {
+            const int32_t page = ((of.slot & kInTable) ? a.block_table : a.free_pages)[of.at + (int64_t)h * of.step];
+            if (page >= 0) slot = ((int64_t)page << log2_block) + (of.slot & (kInTable - 1));
           }
-          a.slots_out[t0 * rows + idx] = page < 0 ? -1 : ((int64_t)page << log2_block) + tok.slot[k];
+          a.slots_out[t0 * rows + idx] = slot;
         }
         __syncthreads();
       } else {
