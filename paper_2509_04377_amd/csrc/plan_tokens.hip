@@ -48,8 +48,11 @@ struct __attribute__((aligned(16))) Token {  // of a piece: where the pages of i
 };
 constexpr int kInTable = 1 << 16;
 
-__global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a, const uint32_t token_pieces, const uint32_t pieces,
-                                                               const uint32_t inv_rows) {
+// (The leading arguments are what a workgroup waits for first: they come in registers, the others with a load.)
+__global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* free_used, const int32_t* seq_lens, const int32_t* new_lens,
+                                                               const int32_t* first_positions, const int num_seqs, const int num_free,
+                                                               const uint32_t token_pieces, const uint32_t pieces, const uint32_t inv_rows,
+                                                               const PlanArgs a) {
   __shared__ Seqs q;
   __shared__ Token tok[kThreads];
   __shared__ Sums wave_sums[kWaves];
@@ -57,21 +60,21 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a,
 
   const int me = (int)threadIdx.x, wave = me / kWave, lane = lane_id();
   const int B = a.block_size, log2_block = __builtin_ctz((unsigned)B), rows = a.rows_per_seq;
-  const int64_t given = *a.free_used;
-  const int64_t used = given < 0 ? 0 : given > a.num_free ? a.num_free : given;
-  const int64_t left = a.num_free - used;
+  const int64_t given = *free_used;
+  const int64_t used = given < 0 ? 0 : given > num_free ? num_free : given;
+  const int64_t left = num_free - used;
   Sums before{0, 0};
   int64_t dealt = 0;
 
-  for (int s0 = 0; s0 < a.num_seqs; s0 += kThreads) {
-    const int s = s0 + me, count = a.num_seqs - s0 < kThreads ? a.num_seqs - s0 : kThreads;
+  for (int s0 = 0; s0 < num_seqs; s0 += kThreads) {
+    const int s = s0 + me, count = num_seqs - s0 < kThreads ? num_seqs - s0 : kThreads;
     int n = 0, len = 0, have = 0, per_row = 0, first = 0;
     int64_t after = 0, kept = 0;
     bool fits = false;
-    if (s < a.num_seqs) {
-      len = a.seq_lens[s];
-      n = a.new_lens[s];
-      first = a.first_positions != nullptr ? a.first_positions[s] : len;
+    if (s < num_seqs) {
+      len = seq_lens[s];
+      n = new_lens[s];
+      first = first_positions != nullptr ? first_positions[s] : len;
       n = n < 0 ? 0 : n;
       const int64_t holds = len < 0 ? 0 : len;
       have = (int)((holds + B - 1) >> log2_block);
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a,
         mine = o > mine ? o : mine;
       }
       if (lane == 0) dealt_of[wave] = mine;
-      if (s < a.num_seqs) {
+      if (s < num_seqs) {
         a.seq_lens_out[s] = served ? (int32_t)kept : len;
         if (a.cu_out != nullptr) {
           if (s == 0) a.cu_out[0] = 0;
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const PlanArgs a,
         __syncthreads();
         // a thread for each (token, row), rows side by side as they are stored
         const int begin = (int)(before.tokens > t0 ? before.tokens - t0 : 0), end = (int)(t_last - t0 < kThreads ? t_last - t0 : kThreads);
-#pragma unroll 4
+#pragma unroll 8
         for (int idx = begin * rows + me; idx < end * rows; idx += kThreads) {
           const int k = inv_rows == ~0u ? idx / rows : inv_rows != 0u ? (int)((uint64_t)(uint32_t)idx * inv_rows >> 32) : idx, h = idx - k * rows;
           const Token of = tok[k];
@@ -202,7 +205,8 @@ hipError_t launch_plan_tokens(const PlanArgs& a, int compute_units, hipStream_t 
   const uint32_t most = 8u * (uint32_t)compute_units, groups = pieces < most ? pieces : most;
   // idx / rows is the upper half of idx * inv_rows as long as idx * rows < 2^32 (idx < kThreads * rows); ~0: divided
   const uint32_t rows = (uint32_t)a.rows_per_seq, inv_rows = rows == 1 ? 0u : rows < 4096 ? (uint32_t)((1ull << 32) / rows + 1) : ~0u;
-  hipLaunchKernelGGL(plan_tokens_kernel, dim3(groups < 1 ? 1 : groups), dim3(kThreads), 0, stream, a, token_pieces, pieces, inv_rows);
+  hipLaunchKernelGGL(plan_tokens_kernel, dim3(groups < 1 ? 1 : groups), dim3(kThreads), 0, stream, a.free_used, a.seq_lens,
+                     a.new_lens, a.first_positions, a.num_seqs, a.num_free, token_pieces, pieces, inv_rows, a);
   return hipGetLastError();
 }
 

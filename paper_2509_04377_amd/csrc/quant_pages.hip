@@ -56,21 +56,20 @@ __device__ __forceinline__ float wave_max(float v) {
 
 constexpr int smaller(int a, int b) { return a < b ? a : b; }
 
-// How a page of one head lies in the lanes of kWaves waves.
-template <typename T, int D, int B>
+// How a page of one head lies in the lanes of kWaves waves (or of one that takes it in so many parts), MOST wave-loads of K each at most.
+template <typename T, int D, int B, int MOST = 8>
 struct Page {
   using G = RowGeom<T, D>;
   static constexpr int LPR = G::kLanesPerRow, TPL = G::kTokensPerLoad;
   static constexpr int kAll = B / TPL;                                     // wave-loads of K
-  static constexpr int kLoads = smaller(kAll, smaller(8, LPR / 2));        // of a wave
+  static constexpr int kLoads = smaller(kAll, smaller(MOST, LPR / 2));     // of a wave
   static constexpr int kWaves = kAll / kLoads;                             // that share a page
   static constexpr int kTokens = kLoads * TPL;                             // of a wave
   static_assert(kWaves * kLoads == kAll, "whole waves");
 };
 // What a wave does with its part of a page: k[i], v[i] hold the lane's 16 bytes of token (part) * kTokens + i * TPL + lane / LPR.
-template <typename T, int D, int B>
+template <typename T, int D, int B, typename P>
 struct Part {
-  using P = Page<T, D, B>;
   static constexpr int kLoads = P::kLoads;
 
   static __device__ __forceinline__ void most(const uint4 (&k)[kLoads], const uint4 (&v)[kLoads], float& mk, float& mv) {
@@ -133,7 +132,7 @@ template <typename T, int D, int B>
 __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_pages_kernel(const QuantPagesArgs a, int groups_per_row) {
   using P = Page<T, D, B>;
   constexpr int kPages = Groups<T, D, B>::kPages;
-  using PT = Part<T, D, B>;
+  using PT = Part<T, D, B, P>;
   __shared__ float most_of[Groups<T, D, B>::kWaves][2];
   __shared__ double ratio[kPages][B];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -214,31 +213,50 @@ struct AppendRope {
   uint64_t turns[64];
 };
 
-template <typename T>
-__device__ __forceinline__ float get(const T* p, int64_t i) {
-  if constexpr (sizeof(T) == 4)
-    return reinterpret_cast<const float*>(p)[i];
-  else
-    return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << 16);
+// N neighbouring elements as fp32, and back (to nearest, ties to even).
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+template <int N>
+__device__ __forceinline__ void get(const float* p, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = p[i];
 }
-template <typename T>
-__device__ __forceinline__ T as(float x) {
-  if constexpr (sizeof(T) == 4)
-    return x;
+template <int N>
+__device__ __forceinline__ void get(const bf16_t* p, float (&x)[N]) {
+  if constexpr (N == 2) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+    x[0] = bf16_lo_to_f32(w), x[1] = bf16_hi_to_f32(w);
+  } else {
+    x[0] = __uint_as_float((uint32_t)p->bits << 16);
+  }
+}
+template <int N>
+__device__ __forceinline__ void put(float* p, const float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = x[i];
+}
+template <int N>
+__device__ __forceinline__ void put(bf16_t* p, const float (&x)[N]) {
+  const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[0], x[N - 1]}), bf16x2_t));
+  if constexpr (N == 2)
+    *reinterpret_cast<uint32_t*>(p) = w;
   else
-    return T{f32_to_bf16(x)};
+    p->bits = (uint16_t)w;
 }
 
-// One wave a row, four rows a workgroup.  Lane l turns pair l % (D/2) of the row's key and query heads and takes its part of the value; the
-// new token's rows meet in LDS, from where they go to the tail, and where they fill the page join the rest of it.  A page larger than
-// a wave's registers is read twice (out of the second-level cache): once in every B steps.
+// One wave a row, four rows a workgroup.  A lane turns N pairs (two, where their number is even) of some of the row's heads, and takes its
+// part of the value; the new token's rows meet in LDS, from where they go to the tail, and where they fill the page join the rest of it.  A
+// page is taken two wave-loads at a time, and read twice (out of the cache) where it has more: it fills once in B steps, and with few
+// registers all rows of a large batch are on their way at once.
+//
+// Bound: for a layer's rows by the chain of a launch (3.2 us); for many rows by the instructions of the conversions and of the addresses.
 constexpr int kAppendWaves = 4;
 
-template <typename T, int D, int B>
+template <typename T, int D, int B, int N>
 __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(const QuantAppendArgs a, const AppendRope rope) {
-  using P = Page<T, D, B>;
-  using PT = Part<T, D, B>;
-  constexpr int kPairs = D / 2, kAtOnce = kWave / kPairs;  // heads that a wave takes at once
+  using P = Page<T, D, B, 2>;
+  using PT = Part<T, D, B, P>;
+  constexpr int kUnits = D / (2 * N), kAtOnce = kWave / kUnits;  // lanes of a head, heads that a wave takes at once
   __shared__ __attribute__((aligned(16))) T sm_now[kAppendWaves][2][D];
   __shared__ double sm_ratio[kAppendWaves][B];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -249,13 +267,14 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
   const int len = a.seq_lens[s];
   const int64_t table_row = a.shared ? s : row;
   const int G = a.num_q_heads / a.num_kv_heads;
-  const int p = lane & (kPairs - 1);
-  const bool turned = p < rope.pairs;
-  const int ea = turned && !rope.interleaved ? p : 2 * p, eb = turned && !rope.interleaved ? p + rope.pairs : 2 * p + 1;
+  // this lane's elements of a head: N from ea on and N from eb on
+  const int p = N * (lane & (kUnits - 1));
+  const bool turned = p < rope.pairs, apart = turned && !rope.interleaved;
+  const int ea = apart ? p : 2 * p, eb = apart ? p + rope.pairs : 2 * p + N;
   // the row's key, its value, then its queries (where they are turned)
   const int heads = 2 + (rope.pairs > 0 ? G : 0);
   constexpr int kSteps = (2 + 8 + kAtOnce - 1) / kAtOnce;
-  float x[kSteps], y[kSteps];
+  float x[kSteps][N], y[kSteps][N];
   const int64_t q0 = ((int64_t)s * a.num_q_heads + (int64_t)hk * G) * D;
   const auto base_of = [&](int h) -> const T* {
     return h == 0 ? static_cast<const T*>(a.new_k) + (int64_t)row * D : h == 1 ? static_cast<const T*>(a.new_v) + (int64_t)row * D
@@ -263,30 +282,44 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
   };
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int h = i * kAtOnce + lane / kPairs;
+    const int h = i * kAtOnce + lane / kUnits;
     if (h < heads) {
       const T* from = base_of(h);
-      x[i] = get(from, ea), y[i] = get(from, eb);
+      get(from + ea, x[i]);
+      get(from + eb, y[i]);
     }
   }
-  Turn w{1.f, 0.f};
+  Turn w[N];
   if (turned) {
-    w = turn_of(rope.turns[p], a.positions[s]);
-    w.c *= rope.magnitude;
-    w.s *= rope.magnitude;
+    const int position = a.positions[s];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      w[n] = turn_of(rope.turns[p + n], position);
+      w[n].c *= rope.magnitude;
+      w[n].s *= rope.magnitude;
+    }
   }
+  const auto turn = [](const Turn& t, float& u, float& v) {
+    const float u0 = u;
+    u = u0 * t.c - v * t.s;
+    v = v * t.c + u0 * t.s;
+  };
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int h = i * kAtOnce + lane / kPairs;
+    const int h = i * kAtOnce + lane / kUnits;
     if (h >= heads) continue;
-    const bool turn = turned && h != 1;
-    const T u = as<T>(turn ? x[i] * w.c - y[i] * w.s : x[i]), v = as<T>(turn ? y[i] * w.c + x[i] * w.s : y[i]);
-    if (h < 2) {
-      now[h][ea] = u, now[h][eb] = v;
-    } else {
-      T* to = static_cast<T*>(a.q_out) + q0 + (int64_t)(h - 2) * D;
-      to[ea] = u, to[eb] = v;
+    if (turned && h != 1) {
+      if (N == 1 || apart) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) turn(w[n], x[i][n], y[i][n]);
+      } else {
+        turn(w[0], x[i][0], x[i][N - 1]);
+        turn(w[N - 1], y[i][0], y[i][N - 1]);
+      }
     }
+    T* to = h < 2 ? now[h] : static_cast<T*>(a.q_out) + q0 + (int64_t)(h - 2) * D;
+    put(to + ea, x[i]);
+    put(to + eb, y[i]);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's accesses to LDS are carried out in order)
 
@@ -353,7 +386,8 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
 template <typename T, int D, int B>
 hipError_t launch_append(const QuantAppendArgs& a, const AppendRope& rope, hipStream_t stream) {
   const unsigned groups = (unsigned)((a.num_seqs * a.num_kv_heads + kAppendWaves - 1) / kAppendWaves);
-  hipLaunchKernelGGL((quant_append_kernel<T, D, B>), dim3(groups), dim3(kAppendWaves * kWave), 0, stream, a, rope);
+  const auto kernel = rope.pairs % 2 == 0 ? quant_append_kernel<T, D, B, 2> : quant_append_kernel<T, D, B, 1>;
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(kAppendWaves * kWave), 0, stream, a, rope);
   return hipGetLastError();
 }
 

@@ -35,7 +35,11 @@ struct Vec<bf16_t> {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = vec_elem<bf16_t>(r, e);
   }
-  static __device__ __forceinline__ uint32_t two(float a, float b) { return (uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16; }
+  static __device__ __forceinline__ uint32_t two(float a, float b) {  // to nearest, ties to even
+    typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+  }
   static __device__ __forceinline__ uint4 put(const float (&x)[8]) {
     return make_uint4(two(x[0], x[1]), two(x[2], x[3]), two(x[4], x[5]), two(x[6], x[7]));
   }
@@ -128,7 +132,8 @@ __global__ __launch_bounds__(kThreads) void rotate_pairs_kernel(const RotateArgs
   }
 }
 
-// 16 bytes at a time.  A head has `units` of work: of each half 16 bytes (INTERLEAVED: 16 bytes) turned, then 16 bytes copied.
+// 16 bytes at a time.  A head has `units` of work: of each half 16 bytes (INTERLEAVED: 16 bytes) turned, then 16 bytes copied; of a value
+// head twice 16 bytes copied.  The first unit's elements are asked for in front of the angles, the next one's in front of the stores.
 template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, const Rope rope, int heads, int tokens_each, int log2_units,
                                                           uint32_t inv_heads) {
@@ -136,60 +141,88 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, co
   extern __shared__ Turn turns[];
   const int64_t t0 = (int64_t)blockIdx.x * tokens_each;
   const int count = a.tokens - t0 < tokens_each ? (int)(a.tokens - t0) : tokens_each;
-  fill_turns(turns, rope, a.positions, t0, count, a.transpose);
   const int nturned = INTERLEAVED ? 2 * rope.pairs / N : rope.pairs / N;  // units that turn
   const int nvec = a.head_dim / N;
-  const int u = (int)threadIdx.x & ((1 << log2_units) - 1);
+  const int units = 1 << log2_units, u = (int)threadIdx.x & (units - 1);
   const int all = count * heads;
-  for (int i = (int)threadIdx.x >> log2_units; i < all; i += kThreads >> log2_units) {
-    const int t = (int)((uint64_t)(uint32_t)i * inv_heads >> 32), h = i - t * heads;
+
+  struct Unit {
+    uint4* to;
+    uint4* page;
+    int token, first, second;  // its vectors of a head; second -1: one alone
+    bool turned;
+    uint4 x, y;
+  };
+  const auto load = [&](int i) {
+    Unit w{};
+    w.first = w.second = -1;
+    if (i >= all) return w;
+    const int t = inv_heads != 0u ? (int)((uint64_t)(uint32_t)i * inv_heads >> 32) : 0, h = i - t * heads;
     const Head head = head_of(a, t0 + t, h);
     const int64_t pool = pool_at(a, t0 + t, head);
-    void* const pages = head.value ? a.v_pool : a.k_pool;
-    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(head.from) + head.in);
-    uint4* to = head.to == nullptr ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(head.to) + head.out);
-    uint4* page = pool < 0 ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(pages) + pool);
+    w.token = t;
+    w.to = head.to == nullptr ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(head.to) + head.out);
+    w.page = pool < 0 ? nullptr : reinterpret_cast<uint4*>(static_cast<T*>(head.value ? a.v_pool : a.k_pool) + pool);
     if (head.value) {
-      if (page != nullptr)
-        for (int j = u; j < nvec; j += 1 << log2_units) page[j] = from[j];
+      if (w.page == nullptr) return w;
+      if (u < nvec) w.first = u;
+      if (u + units < nvec) w.second = u + units;
     } else if (u < nturned) {
-      const Turn* w = turns + t * kMostPairs;
+      w.turned = true;
+      w.first = u;
+      if (!INTERLEAVED) w.second = u + nturned;
+    } else if (u + (INTERLEAVED ? 0 : nturned) < nvec) {
+      w.first = u + (INTERLEAVED ? 0 : nturned);
+    }
+    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(head.from) + head.in);
+    if (w.first >= 0) w.x = from[w.first];
+    if (w.second >= 0) w.y = from[w.second];
+    return w;
+  };
+  const auto finish = [&](Unit& w) {
+    if (w.turned) {
+      const Turn* r = turns + w.token * kMostPairs;
+      float x[N], y[N];
+      Vec<T>::get(w.x, x);
       if constexpr (INTERLEAVED) {
-        float x[N];
-        Vec<T>::get(from[u], x);
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) {
-          const Turn r = w[u * (N / 2) + e];
+          const Turn v = r[u * (N / 2) + e];
           const float p = x[2 * e], q = x[2 * e + 1];
-          x[2 * e] = p * r.c - q * r.s;
-          x[2 * e + 1] = q * r.c + p * r.s;
+          x[2 * e] = p * v.c - q * v.s;
+          x[2 * e + 1] = q * v.c + p * v.s;
         }
-        const uint4 o = Vec<T>::put(x);
-        if (to != nullptr) to[u] = o;
-        if (page != nullptr) page[u] = o;
       } else {
-        float x[N], y[N];
-        Vec<T>::get(from[u], x);
-        Vec<T>::get(from[u + nturned], y);
+        Vec<T>::get(w.y, y);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const Turn r = w[u * N + e];
+          const Turn v = r[u * N + e];
           const float p = x[e], q = y[e];
-          x[e] = p * r.c - q * r.s;
-          y[e] = q * r.c + p * r.s;
+          x[e] = p * v.c - q * v.s;
+          y[e] = q * v.c + p * v.s;
         }
-        const uint4 o = Vec<T>::put(x), o2 = Vec<T>::put(y);
-        if (to != nullptr) to[u] = o, to[u + nturned] = o2;
-        if (page != nullptr) page[u] = o, page[u + nturned] = o2;
+        w.y = Vec<T>::put(y);
       }
-    } else {
-      const int j = u + (INTERLEAVED ? 0 : nturned);
-      if (j < nvec) {
-        const uint4 r = from[j];
-        if (to != nullptr) to[j] = r;
-        if (page != nullptr) page[j] = r;
-      }
+      w.x = Vec<T>::put(x);
     }
+    if (w.first >= 0) {
+      if (w.to != nullptr) w.to[w.first] = w.x;
+      if (w.page != nullptr) w.page[w.first] = w.x;
+    }
+    if (w.second >= 0) {
+      if (w.to != nullptr) w.to[w.second] = w.y;
+      if (w.page != nullptr) w.page[w.second] = w.y;
+    }
+  };
+
+  const int step = kThreads >> log2_units;
+  int i = (int)threadIdx.x >> log2_units;
+  Unit now = load(i);
+  fill_turns(turns, rope, a.positions, t0, count, a.transpose);
+  for (; i < all; i += step) {
+    Unit next = load(i + step);
+    finish(now);
+    now = next;
   }
 }
 
@@ -214,11 +247,11 @@ hipError_t launch(const RotateArgs& a, const pe_rope& rope, hipStream_t stream) 
   }
   constexpr int N = Vec<T>::N;
   const int units = a.head_dim / N - (INTERLEAVED ? 0 : r.pairs / N);
-  int log2_units = 0;
+  int log2_units = 0;  // (of a value head: half of its vectors at least)
   while ((1 << log2_units) < units) ++log2_units;
   const int each = 1;
   const int64_t groups = (a.tokens + each - 1) / each;
-  const uint32_t inv_heads = (uint32_t)((1ull << 32) / (uint32_t)heads + 1);
+  const uint32_t inv_heads = each == 1 ? 0u : (uint32_t)((1ull << 32) / (uint32_t)heads + 1);
   hipLaunchKernelGGL((rotate_kernel<T, INTERLEAVED>), dim3((unsigned)groups), dim3(kThreads), each * kMostPairs * sizeof(Turn), stream, a, r, heads,
                      each, log2_units, inv_heads);
   return hipGetLastError();
