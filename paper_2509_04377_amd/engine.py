@@ -12,6 +12,9 @@ dimension").  Scoring, eviction and the prefill prune see the folded table in ON
 attention are launched per layer, in layer order, because in a model layer l+1's query depends on layer l's
 output.
 
+What goes into a cache: admit() plans the pages, slots and positions of prompts from their lengths on the device, rotate() turns queries and
+keys and stores them by that plan.  QuantCache and LayeredQuantCache are the same drivers over pages in 8 bits.
+
 Beside the paper's step there are three more: a verification of drafted tokens (tree_decode, then accept_path, which scores and
 evicts between the accepted tokens where single steps would have), attention over the pages with the highest bounds
 (select_pages) and eviction by the attention that pages got (evict_by_attention).
@@ -22,6 +25,7 @@ from typing import List, Optional
 import torch
 
 from . import binding as pe
+from .synth import PageLayout
 
 
 class HostOnly:
@@ -59,7 +63,63 @@ def evicts_within(n, tokens, block_size: int, budget: int) -> bool:
 
 
 @dataclass
-class PagedCache:
+class FreePages:
+    """The pages that no sequence has yet, on the device: pages[used:] are free.  One list serves all caches of a pool."""
+    pages: torch.Tensor        # int32
+    used: torch.Tensor         # [1] int32
+    used_alt: torch.Tensor     # the second counter (swapped after each plan)
+
+    @staticmethod
+    def of(pages):
+        one = dict(dtype=torch.int32, device=pages.device)
+        return FreePages(pages, torch.zeros(1, **one), torch.zeros(1, **one))
+
+
+@dataclass
+class Plan:
+    """What admit() leaves for a batch of packed tokens."""
+    cu_seqlens: torch.Tensor   # [S + 1] int32
+    positions: torch.Tensor    # [T] int32
+    slots: torch.Tensor        # [T, Hk] int64 (shared: [T])
+
+
+def empty_layout(num_seqs, num_kv_heads, max_blocks, n_spare, num_phys_blocks, device="cuda", shared=False):
+    """Tables without a page, for a cache whose pages admit() deals out."""
+    rows = 1 if shared else num_kv_heads
+    i32 = dict(dtype=torch.int32, device=device)
+    return PageLayout(torch.full((num_seqs, rows, max_blocks), -1, **i32), torch.full((num_seqs, rows, n_spare), -1, **i32), max_blocks, n_spare,
+                      num_phys_blocks)
+
+
+class Admits:
+    """Plans of tokens and rotations, for a cache with desc, block_table, seq_lens, spare and budget."""
+
+    def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, plan=None, whole=False):
+        """Pages for the tokens that every sequence brings (new_lens [S] int32 on the device, packed total_tokens of them or fewer), up to
+        the budget, and for sequences that begin their spare pages too.  Sequences that do not get their pages stay as they were.  whole: the
+        tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
+        lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
+        set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
+        dev = self.block_table.device
+        if plan is None:
+            rows = self.block_table.shape[1:-1]   # (shared: none)
+            plan = Plan(torch.empty(self.desc.num_seqs + 1, dtype=torch.int32, device=dev), torch.empty(total_tokens, dtype=torch.int32, device=dev),
+                        torch.empty((total_tokens,) + tuple(rows), dtype=torch.int64, device=dev))
+        if self.seq_lens_alt is None:
+            self.seq_lens_alt = torch.empty_like(self.seq_lens)
+        _launch(pe.pe_plan_tokens, self.desc, self.seq_lens, new_lens, first_positions, int(total_tokens), 0 if whole else self.budget, free.pages, free.used,
+                self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots)
+        self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
+        free.used, free.used_alt = free.used_alt, free.used
+        return plan
+
+    def rotate(self, rope, positions, q, k, q_out, k_out, transpose=False):
+        """Rotary positions of q [T, Hq, D] and k [T, Hk, D]; in place or apart, tokens any stride apart."""
+        _launch(pe.pe_rotate, self.desc, rope, transpose, positions, q, k, None, q_out, k_out)
+
+
+@dataclass
+class PagedCache(Admits):
     """Device-side state of one paged KV cache (one layer, or several layers folded into num_seqs).
 
     Owns nothing but tensors; every operation is a C-ABI call."""
@@ -127,6 +187,10 @@ class PagedCache:
             workspace = pe.alloc_workspace(pe.PE_OP_PREFILL_PRUNE, self.desc, total, device=k_in.device)
         _launch(pe.pe_prefill_prune, self.desc, k_in, v_in, cu_seqlens, total, max_seqlen, self.budget, self.k_pool, self.v_pool,
                          self.block_table, self.seq_lens, kept_idx_out, workspace)
+
+    def rotate_store(self, rope, plan: Plan, q, k, v, q_out, k_out=None):
+        """rotate(), and the turned keys and the values into the pages that admit() planned for them (prompts that are kept whole)."""
+        _launch(pe.pe_rotate, self.desc, rope, False, plan.positions, q, k, v, q_out, k_out, plan.slots, self.k_pool, self.v_pool)
 
     def set_host_lens(self, prompt_lens):
         """Tell the host mirror what the prune was given: cached length = min(L, C)."""
@@ -518,6 +582,148 @@ class LayeredCache:
         one = pe.alloc_workspace(pe.PE_OP_DECODE_WEIGHTS, self.per_layer[0].desc, device=self.device)
         for c in self.per_layer:
             c.attention = Attention(float(decay), one)
+
+
+@dataclass
+class QuantCache(Admits):
+    """A paged cache in 8 bits (one layer, or several folded into num_seqs): full pages in e4m3 with scales, the newest, unfinished
+    one in the activations' type.  Its scores are made when a page is rounded, so that an eviction reads no page."""
+    desc: pe.pe_cache_desc
+    cache: pe.pe_quant_cache   # of the five tensors that follow
+    k: torch.Tensor            # [P, B, D] float8_e4m3fn (shared: [P, B, Hk, D])
+    v: torch.Tensor
+    scales: torch.Tensor       # [P, 2] (shared: [P, Hk, 2])
+    k_tail: torch.Tensor       # [S, Hk, B, D]
+    v_tail: torch.Tensor
+    block_table: torch.Tensor  # and the rest as in PagedCache
+    seq_lens: torch.Tensor
+    seq_lens_alt: torch.Tensor
+    spare: torch.Tensor
+    spare_used: torch.Tensor
+    freed_phys: torch.Tensor
+    evicted_logical: torch.Tensor
+    scores: torch.Tensor
+    budget: int
+    workspace: torch.Tensor
+    host_lens: list
+    rope: pe.pe_rope = None         # turns keys and queries on their way (positions: see decode_step)
+    positions: torch.Tensor = None  # [S] int32, of the new token of every sequence: the caller's, changed in place from step to step
+    turned: torch.Tensor = None     # [S, Hq, D]: the queries, turned
+    evict_opts: pe.pe_evict_opts = None
+    cached_scores = fused_evict = False   # (what GraphedStepper asks a cache about: not here)
+    selection = attention = host_scored = None
+
+    @staticmethod
+    def create(dtype, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device="cuda", shared=False, rope=None,
+               decode_splits=0):
+        """As PagedCache.create.  Pages from `layout`, or from admit() behind empty_layout()."""
+        desc = pe.make_desc(dtype, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout.max_blocks, layout.num_phys_blocks,
+                            pe.PE_LAYOUT_SHARED if shared else pe.PE_LAYOUT_PER_HEAD, decode_splits=decode_splits)
+        table, spare = layout.block_table, layout.spare
+        heads, per_row = (), (num_seqs, num_kv_heads)
+        if shared:
+            assert table.shape[1] == 1, "a shared cache takes a layout with one row per sequence"
+            table, spare = table[:, 0], spare[:, 0]
+            heads, per_row = (num_kv_heads,), (num_seqs,)
+        P, on = layout.num_phys_blocks, dict(device=device)
+        k, v = (torch.zeros((P, block_size) + heads + (head_dim,), dtype=torch.uint8, **on).view(torch.float8_e4m3fn) for _ in range(2))
+        scales = torch.ones((P,) + heads + (2,), dtype=torch.float32, **on)
+        k_tail, v_tail = (torch.zeros((num_seqs, num_kv_heads, block_size, head_dim), dtype=dtype, **on) for _ in range(2))
+        i32 = dict(dtype=torch.int32, device=device)
+        return QuantCache(desc, pe.make_quant_cache(desc, k, v, scales, k_tail, v_tail), k, v, scales, k_tail, v_tail,
+                          table.to(device).contiguous(), torch.zeros(num_seqs, **i32), torch.zeros(num_seqs, **i32), spare.to(device).contiguous(),
+                          torch.zeros(per_row, **i32), torch.full(per_row, -1, **i32), torch.full(per_row, -1, **i32),
+                          torch.full((num_seqs, num_kv_heads, layout.max_blocks), float("inf"), dtype=torch.float32, **on), int(budget),
+                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, rope,
+                          torch.zeros(num_seqs, **i32) if rope is not None else None,
+                          torch.empty((num_seqs, num_q_heads, head_dim), dtype=dtype, **on) if rope is not None else None)
+
+    def take(self, paged: PagedCache):
+        """The tokens of an unrounded cache of the same shape (behind its prefill_prune, say) become this one's: its full pages are rounded
+        into the pages of this table, which has as many, and scored; the rest goes to the tail."""
+        _launch(pe.pe_quant_pages, self.desc, self.cache, paged.k_pool, paged.v_pool, paged.block_table, paged.seq_lens, self.block_table, self.scores)
+        if not HostOnly.active:
+            self.seq_lens.copy_(paged.seq_lens)
+        self.host_lens = list(paged.host_lens)
+
+    def triggers(self) -> List[bool]:
+        return triggers(self.host_lens, self.desc.block_size, self.budget)
+
+    def score_and_evict(self):
+        """The pages' scores are there: only the decision is left (pe_evict_blocks_cached, or evict_opts' variant of it)."""
+        if self.evict_opts is None:
+            _launch(pe.pe_evict_blocks_cached, self.desc, self.scores, self.block_table, self.seq_lens, self.budget, self.evicted_logical,
+                    self.freed_phys)
+        else:
+            o = self.evict_opts
+            _launch(pe.pe_evict_blocks_ex, self.desc, pe.pe_evict_opts(o.policy, o.protect_first, o.protect_last, o.share_heads, 1), self.scores,
+                    self.block_table, self.seq_lens, self.budget, self.evicted_logical, self.freed_phys)
+        self.host_lens = [n - self.desc.block_size if t else n for n, t in zip(self.host_lens, self.triggers())]
+
+    def append_and_attend(self, new_k, new_v, q, out, softmax_scale=None):
+        if softmax_scale is None:
+            softmax_scale = float(self.desc.head_dim) ** -0.5
+        _launch(pe.pe_quant_append, self.desc, self.cache, self.rope, self.positions, q, self.turned, new_k, new_v, self.block_table, self.seq_lens,
+                self.seq_lens_alt, self.freed_phys, self.spare, self.spare_used, self.scores)
+        self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
+        _launch(pe.pe_quant_decode, self.desc, self.cache, q if self.rope is None else self.turned, self.block_table, self.seq_lens, softmax_scale,
+                out, self.workspace)
+
+    def decode_step(self, new_k, new_v, q, out, softmax_scale=None):
+        """One decode iteration (Alg. 3) over the 8-bit cache: evict where a page has filled at budget, append, attend.  With a rope, new_k and q come
+        unturned, and `positions` hold the tokens' positions (which an eviction does not change)."""
+        if any(self.triggers()):
+            self.score_and_evict()
+        self.append_and_attend(new_k, new_v, q, out, softmax_scale)
+        self.host_lens = [n + 1 for n in self.host_lens]
+
+    def rows(self, first, end):
+        """The same cache's sequences first .. end - 1, as a cache (views of the same pages; host_lens is a copy)."""
+        d, sl = self.desc, slice(first, end)
+        desc = pe.pe_cache_desc(**{**{name: getattr(d, name) for name, _ in d._fields_}, "num_seqs": end - first})
+        names = ("k_tail", "v_tail", "block_table", "seq_lens", "seq_lens_alt", "spare", "spare_used", "freed_phys", "evicted_logical", "scores",
+                 "host_lens", "positions", "turned")
+        views = {name: None if getattr(self, name) is None else getattr(self, name)[sl] for name in names}
+        return replace(self, desc=desc, cache=pe.make_quant_cache(desc, self.k, self.v, self.scales, views["k_tail"], views["v_tail"]), **views,
+                       workspace=pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=self.k.device))
+
+
+class LayeredQuantCache:
+    """The multi-layer driver over an 8-bit cache: evictions of all layers in one launch, then append and attention layer by layer.  With a
+    rope, `positions` [S] serve every layer.  GraphedStepper replays its steps."""
+
+    def __init__(self, dtype, layers, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device="cuda", shared=False,
+                 rope=None):
+        self.layers, self.S, self.B, self.budget = layers, num_seqs, block_size, int(budget)
+        assert layout.block_table.shape[0] == layers * num_seqs
+        f = self.folded = QuantCache.create(dtype, layers * num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device, shared,
+                                            rope)
+        self.per_layer = [f.rows(l * num_seqs, (l + 1) * num_seqs) for l in range(layers)]
+        self.positions = None if rope is None else self.per_layer[0].positions
+        for c in self.per_layer:   # one layer at a time, on one stream
+            c.workspace, c.positions, c.turned = self.per_layer[0].workspace, self.positions, self.per_layer[0].turned
+        self.host_lens = [0] * num_seqs   # the same in every layer
+        self.fused = False
+
+    def take_layer(self, layer, paged: PagedCache):
+        self.per_layer[layer].take(paged)
+        self.host_lens = list(self.per_layer[layer].host_lens)
+
+    def _triggers(self):
+        return triggers(self.host_lens, self.B, self.budget)
+
+    def decode_step(self, new_k, new_v, q, out, softmax_scale: Optional[float] = None):
+        """new_k, new_v [layers, S, Hk, D]; q, out [layers, S, Hq, D].  One decode iteration of all layers."""
+        trig, f = self._triggers(), self.folded
+        f.host_lens = self.host_lens * self.layers
+        if any(trig):
+            f.score_and_evict()
+            self.host_lens = f.host_lens[:self.S]
+        for l, c in enumerate(self.per_layer):
+            c.append_and_attend(new_k[l], new_v[l], q[l], out[l], softmax_scale)
+        f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens   # (each layer has swapped its part)
+        self.host_lens = [n + 1 for n in self.host_lens]
+        return any(trig)
 
 
 class GraphedStepper:
