@@ -485,7 +485,7 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
  *
  * pe_rotate turns the queries and keys of num_tokens tokens (0: nothing to do) and, where slots are given, stores the turned keys and the
  * values into the pages: token t of KV head h goes to slot slots[t][h] of the pools, counted in tokens (page * B + slot, as (8) gives
- * them); slots outside 0 .. P*B - 1 are left out.  Of desc only dtype, heads, head_dim, block_size, num_phys_blocks and layout matter.
+ * them); slots outside 0 .. P*B - 1 are left out, the others are distinct.  Of desc only dtype, heads, head_dim, block_size, num_phys_blocks and layout matter.
  *     q: [num_tokens][Hq][D], k, v: [num_tokens][Hk][D], each token's heads dense, consecutive tokens q_stride, k_stride, v_stride
  *     elements apart (a projection's output may hold all three side by side).  positions: [num_tokens] int32, any value.
  *     q, q_out both NULL: no queries; k NULL: no keys (then k_out, slots too).  q_out, k_out: strides of their own; in place
@@ -526,7 +526,8 @@ int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose,
  * them; its pages' number is not looked at) rounded into the pages block_table[..][j] of `cache`, and the tokens behind them copied to
  * the tail's first slots (others are left).  src_table, block_table: [S][Hk][max_blocks], may be the same.  scores_out: NULL, or
  * [S][Hk][max_blocks] as pe_score_blocks gives them: the scores of the pages before their rounding (fp32: within one step of an
- * fp32 number, as sums may be taken in another order), +INF behind them.  Entries of -1 are passed over.
+ * fp32 number, as sums may be taken in another order), +INF behind them.  Entries of -1 are passed over.  The pools of `cache` and k_pool, v_pool must
+ * not overlap.
  *
  * pe_quant_append: a decode step's new token of every sequence, as pe_append_kv but that it goes to slot seq_lens[s] % B of the row's tail; where
  * that fills the page, the page is rounded into page seq_lens[s] / B of the row and, with scores not NULL, its score is written to
@@ -534,8 +535,7 @@ int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose,
  * it; a sequence with seq_lens[s] >= max_blocks*B (or < 0) is left untouched, with its length.
  * rope not NULL: the new key, and q into q_out (may be q; both [S][Hq][D]), are turned on the way as by (9), positions: [S].  rope NULL: keys
  * as they come; positions, q, q_out are not looked at.
- * new_k, new_v: [S][Hk][D], 16-byte aligned, as q and q_out.  At most 65536 KV heads, and S * Hk < 2^23 (else
- * PE_ERR_UNSUPPORTED).
+ * new_k, new_v: [S][Hk][D], 16-byte aligned, as q and q_out.  S * Hk < 2^23 (else PE_ERR_UNSUPPORTED).
  */
 typedef struct pe_quant_cache {
   void* k;
@@ -553,13 +553,15 @@ int pe_quant_append(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
 
 /*
  * (11) Paged decode attention over a cache in 8 bits: pe_paged_decode's sum over the seq_lens[s] tokens of row (s, hk), the full pages by
- *      block_table with their scales and the last seq_lens[s] % B tokens from the tail.  fp32 accumulation; queries, numbers and softmax
- *      weights enter the products with all of their bits; output rounded to desc->dtype.  seq_lens[s] == 0 gives zeros.  (Behind an eviction
- *      that comes before the next append no page is unfinished: lengths are multiples of B then.)
+ *      block_table with their scales and the last seq_lens[s] % B tokens from the tail.  fp32 accumulation; queries and keys enter the products
+ *      with all of their bits, softmax weights too where desc->dtype is fp32, to within 2^-17 of themselves where it is bfloat16; output rounded to
+ *      desc->dtype.  seq_lens[s] == 0 gives zeros.  (Behind an eviction that comes before the next append no page is unfinished: lengths are
+ *      multiples of B then.)  A length that the table row does not hold is cut there.
  *      q, the tokens attended to and the scales of their pages are finite; what lies behind a row's end may be anything.
  *      `out` may be q itself and must not otherwise overlap what is read; it is the library's until the call's launches are through, as in
  *      pe_paged_decode.
- *      desc->decode_splits is the number of splits of a row (0: the library's choice), the other decode_* fields are not looked at.
+ *      desc->decode_splits is the number of splits of a row (0: the library's choice, from the shape; another number adds in another order),
+ *      the other decode_* fields are not looked at.  At most 65536 KV heads, in all calls of a cache in 8 bits.
  *      workspace: pe_workspace_bytes(PE_OP_QUANT_DECODE, desc, 0).
  *      shared: block_table [S][max_blocks].
  */

@@ -27,7 +27,7 @@ int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const
   if (st != PE_OK) return st;
   if (!k_pool || !v_pool || !src_table || !seq_lens || !block_table) return PE_ERR_INVALID_ARG;
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(scores_out, 4)) return PE_ERR_INVALID_ARG;
-  if (!pe::quant_pages_launches(desc)) return PE_ERR_UNSUPPORTED;
+  if (desc->num_kv_heads > 65536 || !pe::quant_pages_launches(desc)) return PE_ERR_UNSUPPORTED;
   pe::QuantPagesArgs a;
   a.cache = *cache;
   a.k_pool = k_pool;
@@ -101,6 +101,7 @@ int pe_quant_decode(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
   const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * (bf16 ? 2 : 4);
   const size_t tail = (size_t)desc->num_seqs * desc->num_kv_heads * desc->block_size * desc->head_dim * (bf16 ? 2 : 4);
   if ((out != q && overlap(out, o, q, o)) || overlap(out, o, cache->k_tail, tail) || overlap(out, o, cache->v_tail, tail)) return PE_ERR_INVALID_ARG;
+  if (desc->num_kv_heads > 65536) return PE_ERR_UNSUPPORTED;
   const int splits = pe::quant_splits(desc);
   const int ws = check_workspace(workspace, workspace_bytes, pe::decode_partials_bytes(desc->num_seqs, desc->num_q_heads, desc->head_dim, splits));
   if (ws != PE_OK) return ws;

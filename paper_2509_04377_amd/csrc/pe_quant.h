@@ -62,7 +62,8 @@ struct QuantDecodeArgs {
 // Splits of a row.  The host sees the length of a table row, not of the sequences, so a count has to pay on full rows and on rows of unequal
 // length (37 tokens to all; four query heads a KV head, us, best count / others; measured on an MI355X, fp32 the same order):
 //   - up to half as many rows as compute units: as many as leave no compute unit two workgroups, of 128 tokens or more (64 rows of D = 128 x
-//     1024 in four 6.7, x 4096 in four 12.5; eight rows x 4096 in 32 6.7, in sixteen 7.1), two only of 512 or more (128 rows x 1024 in two 8.5, x 512
+//     1024 in four 6.7, x 4096 in four 12.5; eight rows x 4096 in 32 6.7, in sixteen 7.1), but not a few more than those that need no merge launch
+//     (two rows of D = 64 x 1649 in thirteen 5.8, in twelve 5.3), two only of 512 or more (128 rows x 1024 in two 8.5, x 512
 //     whole 6.4 / 6.8); rows of 32 KiB of K whole (eight of D = 64 x 512 whole 4.7 / 4.8, of D = 128 x 512 in four 5.3 / 5.9 whole);
 //   - more, of 2048 tokens or more: three up to five eighths of the compute units (D = 128, 160 rows x 2048 in three 15.3, whole 16.1, ragged 11.6 / 13),
 //     four up to three quarters (192 rows x 2048 full in four 18.1, whole 17.1, ragged 12.7 / 15), else whole (224 rows 18.9, in three 20.9, ragged
@@ -81,6 +82,8 @@ inline int quant_splits(const pe_cache_desc* d) {
   }
   int64_t splits = tokens / (fit == 2 ? 512 : 128);
   if (splits > fit) splits = fit;
+  const int most = most_arrivals(d->num_q_heads / d->num_kv_heads);
+  if (splits > most && splits <= most + 4) splits = most;
   return splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
 }
 

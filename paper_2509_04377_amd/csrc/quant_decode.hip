@@ -276,8 +276,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
   const int k_off = k_tok * row_bytes + (SHARED ? hk * D : 0) + k_elem;
   const int v_off = g * row_bytes + (SHARED ? hk * D : 0) + EV * m;
 
-  const int most = max_blocks << log2_block;  // (a longer length is a caller error: the table row is the end)
-  const int len = len_raw < 0 ? 0 : len_raw < most || most <= 0 ? len_raw : most;
+  // (a length that the table does not hold is a caller error: the table row is the end)
+  const int len = len_raw < 0 ? 0 : (len_raw >> log2_block) < max_blocks ? len_raw : max_blocks << log2_block;
   const int full = len >> log2_block << log2_block;  // tokens in 8 bits
   const int ntiles = full >> ilog2(kTile), tail_tiles = (len - full + kTile - 1) >> ilog2(kTile);
   const int tail0 = stride - 1 - first;

@@ -56,13 +56,13 @@ __device__ __forceinline__ float wave_max(float v) {
 
 constexpr int smaller(int a, int b) { return a < b ? a : b; }
 
-// How a page of one head lies in the lanes of kWaves waves (or of one that takes it in so many parts), MOST wave-loads of K each at most.
-template <typename T, int D, int B, int MOST = 8>
+// How a page of one head lies in the lanes of kWaves waves.
+template <typename T, int D, int B>
 struct Page {
   using G = RowGeom<T, D>;
   static constexpr int LPR = G::kLanesPerRow, TPL = G::kTokensPerLoad;
   static constexpr int kAll = B / TPL;                                     // wave-loads of K
-  static constexpr int kLoads = smaller(kAll, smaller(MOST, LPR / 2));     // of a wave
+  static constexpr int kLoads = smaller(kAll, smaller(8, LPR / 2));        // of a wave
   static constexpr int kWaves = kAll / kLoads;                             // that share a page
   static constexpr int kTokens = kLoads * TPL;                             // of a wave
   static_assert(kWaves * kLoads == kAll, "whole waves");
@@ -244,31 +244,48 @@ __device__ __forceinline__ void put(bf16_t* p, const float (&x)[N]) {
     p->bits = (uint16_t)w;
 }
 
-// One wave a row, four rows a workgroup.  A lane turns N pairs (two, where their number is even) of some of the row's heads, and takes its
-// part of the value; the new token's rows meet in LDS, from where they go to the tail, and where they fill the page join the rest of it.  A
-// page is taken two wave-loads at a time, and read twice (out of the cache) where it has more: it fills once in B steps, and with few
-// registers all rows of a large batch are on their way at once.
+// As many waves a row as hold a page (up to eight wave-loads of K and of V each); rows of one wave are four to a workgroup.  A lane turns N
+// pairs (two, where their number is even) of some of the row's heads, and takes its part of the value; the new token's rows meet in LDS, from
+// where they go to the tail, and where they fill the page join the rest of it, which is asked for as soon as the length is there.
 //
-// Bound: for a layer's rows by the chain of a launch (3.2 us); for many rows by the instructions of the conversions and of the addresses.
-constexpr int kAppendWaves = 4;
+// Bound: by the chain of a launch (64 rows 3.1 us; 174 rows of D = 128 that all fill, bfloat16, B = 16, 5.6, fp32, B = 128, 9.8); for many rows
+// by instructions (8192 rows of D = 128, none filling, 7.4, a sixteenth 10.5, all 23.7).  Pages taken in smaller parts one after the other, each
+// waiting for memory, leave more registers and take 6.8, 34 and 29.4 us where all fill.
+template <typename T, int D, int B>
+struct RowWaves {
+  using P = Page<T, D, B>;
+  static constexpr int kWaves = P::kWaves;                  // of a row
+  static constexpr int kRows = kWaves == 1 ? 4 : 1;         // of a workgroup
+  static constexpr int kThreads = kWaves * kRows * kWave;
+};
 
 template <typename T, int D, int B, int N>
-__global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(const QuantAppendArgs a, const AppendRope rope) {
-  using P = Page<T, D, B, 2>;
+__global__ __launch_bounds__((RowWaves<T, D, B>::kThreads)) void quant_append_kernel(const QuantAppendArgs a, const AppendRope rope) {
+  using P = Page<T, D, B>;
   using PT = Part<T, D, B, P>;
-  constexpr int kUnits = D / (2 * N), kAtOnce = kWave / kUnits;  // lanes of a head, heads that a wave takes at once
-  __shared__ __attribute__((aligned(16))) T sm_now[kAppendWaves][2][D];
-  __shared__ double sm_ratio[kAppendWaves][B];
+  using RW = RowWaves<T, D, B>;
+  constexpr int kUnits = D / (2 * N), kAtOnce = RW::kWaves * kWave / kUnits;  // lanes of a head, heads that a row's waves take at once
+  __shared__ __attribute__((aligned(16))) T sm_now[RW::kRows][2][D];
+  __shared__ double sm_ratio[RW::kRows][B];
+  __shared__ float2 sm_most[RW::kWaves];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const int row = (int)blockIdx.x * kAppendWaves + wave;
-  if (row >= a.num_seqs * a.num_kv_heads) return;
+  const int part = RW::kWaves == 1 ? 0 : wave, slot_of_row = RW::kWaves == 1 ? wave : 0;
+  const int me = part * kWave + lane;  // in the row
+  const int row = (int)blockIdx.x * RW::kRows + slot_of_row;
+  if (row >= a.num_seqs * a.num_kv_heads) return;  // (of a row of several waves all or none)
   const int s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
-  T(*now)[D] = sm_now[wave];
+  T(*now)[D] = sm_now[slot_of_row];
+  const auto row_sync = [] {
+    if constexpr (RW::kWaves == 1)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's accesses to LDS are carried out in order)
+    else
+      __syncthreads();
+  };
   const int len = a.seq_lens[s];
   const int64_t table_row = a.shared ? s : row;
   const int G = a.num_q_heads / a.num_kv_heads;
   // this lane's elements of a head: N from ea on and N from eb on
-  const int p = N * (lane & (kUnits - 1));
+  const int p = N * (me & (kUnits - 1));
   const bool turned = p < rope.pairs, apart = turned && !rope.interleaved;
   const int ea = apart ? p : 2 * p, eb = apart ? p + rope.pairs : 2 * p + N;
   // the row's key, its value, then its queries (where they are turned)
@@ -282,7 +299,7 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
   };
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int h = i * kAtOnce + lane / kUnits;
+    const int h = i * kAtOnce + me / kUnits;
     if (h < heads) {
       const T* from = base_of(h);
       get(from + ea, x[i]);
@@ -299,6 +316,23 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
       w[n].s *= rope.magnitude;
     }
   }
+  const int slot = len & (B - 1), jb = len / B;
+  const bool runs = len >= 0 && jb < a.max_blocks, fills = runs && slot == B - 1;
+  int32_t* entry = a.block_table + table_row * a.max_blocks + jb;
+  uint4* kt = static_cast<uint4*>(a.cache.k_tail) + (int64_t)row * B * P::LPR;
+  uint4* vt = static_cast<uint4*>(a.cache.v_tail) + (int64_t)row * B * P::LPR;
+  // a page that fills: its tokens so far (the place of the last one holds something older)
+  int page = -1;
+  uint4 k[P::kLoads], v[P::kLoads];
+  if (fills) {
+    page = *entry;
+#pragma unroll
+    for (int i = 0; i < P::kLoads; ++i) {
+      const int at = (part * P::kTokens + i * P::TPL) * P::LPR + lane;
+      k[i] = kt[at];
+      v[i] = vt[at];
+    }
+  }
   const auto turn = [](const Turn& t, float& u, float& v) {
     const float u0 = u;
     u = u0 * t.c - v * t.s;
@@ -306,7 +340,7 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
   };
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int h = i * kAtOnce + lane / kUnits;
+    const int h = i * kAtOnce + me / kUnits;
     if (h >= heads) continue;
     if (turned && h != 1) {
       if (N == 1 || apart) {
@@ -321,73 +355,55 @@ __global__ __launch_bounds__(kAppendWaves * kWave) void quant_append_kernel(cons
     put(to + ea, x[i]);
     put(to + eb, y[i]);
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's accesses to LDS are carried out in order)
+  row_sync();
 
-  const int slot = len & (B - 1), jb = len / B;
-  const bool runs = len >= 0 && jb < a.max_blocks;
-  if (hk == 0 && lane == 0) a.seq_lens_out[s] = runs ? len + 1 : len;
+  if (hk == 0 && me == 0) a.seq_lens_out[s] = runs ? len + 1 : len;
   if (!runs) return;
-  int32_t* entry = a.block_table + table_row * a.max_blocks + jb;
-  if (slot == 0 && lane == 0 && (!a.shared || hk == 0)) {
-    int page = a.freed_phys[table_row];
-    if (page >= 0) {
+  if (slot == 0 && me == 0 && (!a.shared || hk == 0)) {
+    int link = a.freed_phys[table_row];
+    if (link >= 0) {
       a.freed_phys[table_row] = -1;
     } else {
       const int used = a.spare_used[table_row];
-      page = used >= 0 && used < a.n_spare ? a.spare[table_row * a.n_spare + used] : -1;
+      link = used >= 0 && used < a.n_spare ? a.spare[table_row * a.n_spare + used] : -1;
       a.spare_used[table_row] = used + 1;
     }
-    *entry = page;
+    *entry = link;
   }
-  uint4* kt = static_cast<uint4*>(a.cache.k_tail) + (int64_t)row * B * P::LPR;
-  uint4* vt = static_cast<uint4*>(a.cache.v_tail) + (int64_t)row * B * P::LPR;
-  if (lane < 2 * P::LPR) {
+  if (part == 0 && lane < 2 * P::LPR) {
     const int kv = lane / P::LPR, u = lane % P::LPR;
     (kv ? vt : kt)[slot * P::LPR + u] = reinterpret_cast<const uint4*>(now[kv])[u];
   }
-  if (slot != B - 1) return;
-  // the page is full: its other tokens from the tail, the last one from LDS
-  const int page = *entry;
+  if (!fills) return;
+  if (part * P::kTokens + (P::kLoads - 1) * P::TPL + lane / P::LPR == B - 1) {  // the new token, the last of the page
+    k[P::kLoads - 1] = reinterpret_cast<const uint4*>(now[0])[lane % P::LPR];
+    v[P::kLoads - 1] = reinterpret_cast<const uint4*>(now[1])[lane % P::LPR];
+  }
+  float mk, mv;
+  PT::most(k, v, mk, mv);
+  if (a.scores != nullptr) PT::ratios(k, v, part, sm_ratio[slot_of_row]);
+  if (RW::kWaves > 1 && lane == 0) sm_most[part] = make_float2(mk, mv);
+  row_sync();
+  if constexpr (RW::kWaves > 1) {
+#pragma unroll
+    for (int i = 0; i < RW::kWaves; ++i) mk = fmaxf(mk, sm_most[i].x), mv = fmaxf(mv, sm_most[i].y);
+  }
   if (page < 0) return;  // spare list exhausted (precondition violated): the page is dropped
   const int rows = a.shared ? a.num_kv_heads : 1, head_row = a.shared ? hk : 0;
-  uint4 k[P::kLoads], v[P::kLoads];
-  const auto load = [&](int part) {
-#pragma unroll
-    for (int i = 0; i < P::kLoads; ++i) {
-      const int t = part * P::kTokens + i * P::TPL + lane / P::LPR, u = lane % P::LPR;
-      const bool last = t == B - 1;
-      k[i] = last ? reinterpret_cast<const uint4*>(now[0])[u] : kt[t * P::LPR + u];
-      v[i] = last ? reinterpret_cast<const uint4*>(now[1])[u] : vt[t * P::LPR + u];
-    }
-  };
-  float most_k = 0.f, most_v = 0.f;
-#pragma unroll 1
-  for (int part = 0; part < P::kWaves; ++part) {
-    load(part);
-    float mk, mv;
-    PT::most(k, v, mk, mv);
-    most_k = fmaxf(most_k, mk);
-    most_v = fmaxf(most_v, mv);
-    if (a.scores != nullptr) PT::ratios(k, v, part, sm_ratio[wave]);
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  const int ek = scale_exponent(most_k), ev = scale_exponent(most_v);
-#pragma unroll 1
-  for (int part = 0; part < P::kWaves; ++part) {
-    if (P::kWaves > 1) load(part);
-    PT::store(k, v, part, a.cache, ((int64_t)page * B * rows + head_row) * D, rows * D, exp2i(-ek), exp2i(-ev));
-  }
-  if (lane == 0) {
+  const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+  PT::store(k, v, part, a.cache, ((int64_t)page * B * rows + head_row) * D, rows * D, exp2i(-ek), exp2i(-ev));
+  if (me == 0) {
     *reinterpret_cast<float2*>(a.cache.scales + ((int64_t)page * rows + head_row) * 2) = make_float2(exp2i(ek), exp2i(ev));
-    if (a.scores != nullptr) a.scores[(int64_t)row * a.max_blocks + jb] = PT::score(sm_ratio[wave]);
+    if (a.scores != nullptr) a.scores[(int64_t)row * a.max_blocks + jb] = PT::score(sm_ratio[slot_of_row]);
   }
 }
 
 template <typename T, int D, int B>
 hipError_t launch_append(const QuantAppendArgs& a, const AppendRope& rope, hipStream_t stream) {
-  const unsigned groups = (unsigned)((a.num_seqs * a.num_kv_heads + kAppendWaves - 1) / kAppendWaves);
+  using RW = RowWaves<T, D, B>;
+  const unsigned groups = (unsigned)((a.num_seqs * a.num_kv_heads + RW::kRows - 1) / RW::kRows);
   const auto kernel = rope.pairs % 2 == 0 ? quant_append_kernel<T, D, B, 2> : quant_append_kernel<T, D, B, 1>;
-  hipLaunchKernelGGL(kernel, dim3(groups), dim3(kAppendWaves * kWave), 0, stream, a, rope);
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(RW::kThreads), 0, stream, a, rope);
   return hipGetLastError();
 }
 

@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, co
     Unit w{};
     w.first = w.second = -1;
     if (i >= all) return w;
-    const int t = inv_heads != 0u ? (int)((uint64_t)(uint32_t)i * inv_heads >> 32) : 0, h = i - t * heads;
+    const int t = tokens_each == 1 ? 0 : heads == 1 ? i : (int)((uint64_t)(uint32_t)i * inv_heads >> 32), h = i - t * heads;
     const Head head = head_of(a, t0 + t, h);
     const int64_t pool = pool_at(a, t0 + t, head);
     w.token = t;
@@ -234,6 +234,16 @@ bool by_vectors(const RotateArgs& a, const pe_rope& rope) {
          fits(a.v, a.v_stride) && fits(a.q_out, a.q_out_stride) && fits(a.k_out, a.k_out_stride) && fits(a.k_pool, 0) && fits(a.v_pool, 0);
 }
 
+// Tokens of a workgroup: one where it has 5 KiB or more to turn (workgroups that are soon through stream best: 32004 tokens of 32 + 8 heads of D =
+// 128 in one | two | four tokens 152 | 163 | 169 us, of D = 64 87 | 95 | 103), as many as that takes of few heads where tokens are many (67000 of 2 + 1
+// heads of D = 128 71 | 41 | 30, eight 27; fp32 106 | 81 | 69; 32004 of 8 + 2 39 | 34 | 34; not 500 of these: 4.2 | 4.3 | 5.7).
+constexpr int kMostTokens = 8;
+int tokens_each(int64_t tokens, int token_bytes) {
+  int each = 1;
+  while (each < kMostTokens && each * token_bytes < 5 << 10 && tokens >= each * 2048) each *= 2;
+  return each;
+}
+
 template <typename T, bool INTERLEAVED>
 hipError_t launch(const RotateArgs& a, const pe_rope& rope, hipStream_t stream) {
   Rope r;
@@ -249,9 +259,10 @@ hipError_t launch(const RotateArgs& a, const pe_rope& rope, hipStream_t stream) 
   const int units = a.head_dim / N - (INTERLEAVED ? 0 : r.pairs / N);
   int log2_units = 0;  // (of a value head: half of its vectors at least)
   while ((1 << log2_units) < units) ++log2_units;
-  const int each = 1;
+  const int each = tokens_each(a.tokens, heads * a.head_dim * (int)sizeof(T));
   const int64_t groups = (a.tokens + each - 1) / each;
-  const uint32_t inv_heads = each == 1 ? 0u : (uint32_t)((1ull << 32) / (uint32_t)heads + 1);
+  // i / heads is the upper half of i * inv_heads (several tokens: few heads)
+  const uint32_t inv_heads = (uint32_t)((1ull << 32) / (uint32_t)heads + 1);
   hipLaunchKernelGGL((rotate_kernel<T, INTERLEAVED>), dim3((unsigned)groups), dim3(kThreads), each * kMostPairs * sizeof(Turn), stream, a, r, heads,
                      each, log2_units, inv_heads);
   return hipGetLastError();

@@ -61,7 +61,7 @@ def attend(q, k, v, dtype, scale=None):
     """q [n, D], k, v [t, D] in float64 -> (out, bound).  Half steps of 2^-24:
       - a logit's D products, of eight term products each at most (fp32 queries and keys), summed in any order, with the scales of the
         page and of the softmax: 8 D + 4 relative to sum |q_d k_d| scale, and what is left out of fp32 terms 2^-29; a weight twice that
-        relative to itself, and exp2 and the scaling by V's scale 2^-22;
+        relative to itself, and exp2 and the scaling by V's scale 2^-22; bfloat16: what the weight's second term of 8 bits leaves of it, 2^-17;
       - a sum over t tokens of up to nine term products: 9 t + 4, above and below the division."""
     scale = q.shape[1] ** -0.5 if scale is None else scale
     if k.shape[0] == 0:
@@ -71,5 +71,5 @@ def attend(q, k, v, dtype, scale=None):
     x = q @ k.T * scale
     mag = q.abs() @ k.abs().T * abs(scale)
     w = torch.softmax(x, 1)
-    off = 2 * ((terms * q.shape[1] + 4) * 2.0 ** -24 + 2.0 ** -29) * mag.amax(1, keepdim=True) + 2.0 ** -21 + 2 * (3 * terms * k.shape[0] + 4) * 2.0 ** -24
+    off = 2 * ((terms * q.shape[1] + 4) * 2.0 ** -24 + 2.0 ** -29) * mag.amax(1, keepdim=True) + 2.0 ** -21 + (2.0 ** -17 if terms == 1 else 0) + 2 * (3 * terms * k.shape[0] + 4) * 2.0 ** -24
     return w @ v, off * (w @ v.abs())

@@ -61,13 +61,26 @@ def test_heads(Hk, G):
         assert_close(got, y, bound, got.dtype)
 
 
-@pytest.mark.parametrize("T", [1, 2, 63, 300, 2049])
-def test_tokens(T):
-    desc, rope, pos, q, k, want = _case(T, T, 2, 3, 64, 64, "f32")
+def test_very_many_heads():
+    desc, rope, pos, q, k, want = _case(1, 2, 30000, 2, 64, 64, "bf16")
     out = [torch.empty_like(x, device=DEV) for x in (q, k)]
     pe.pe_rotate(desc, rope, False, pos, q.to(DEV), k.to(DEV), None, *out)
     for got, (y, bound) in zip(out, want):
         assert_close(got, y, bound, got.dtype)
+
+
+@pytest.mark.parametrize("Hk,G,D,dt", [(2, 3, 64, "f32"), (1, 1, 64, "bf16"), (1, 2, 128, "bf16"), (2, 4, 128, "bf16")])
+@pytest.mark.parametrize("T", [1, 2, 63, 300, 2049, 4097, 8195, 16385])
+def test_tokens(T, Hk, G, D, dt):
+    """One token a workgroup, and up to eight."""
+    desc, rope, pos, q, k, want = _case(T, T, Hk, G, D, D, dt)
+    out = [torch.empty_like(x, device=DEV) for x in (q, k)]
+    pe.pe_rotate(desc, rope, False, pos, q.to(DEV), k.to(DEV), None, *out)
+    for got, (y, bound) in zip(out, want):
+        assert_close(got, y, bound, got.dtype)
+    ko = torch.empty_like(k, device=DEV)   # one kind of heads alone
+    pe.pe_rotate(desc, rope, False, pos, None, k.to(DEV), None, None, ko)
+    assert torch.equal(ko, out[1])
 
 
 def test_far_and_negative_positions():

@@ -113,6 +113,31 @@ def test_decode():
     assert pe.pe_workspace_bytes(pe.PE_OP_QUANT_DECODE, _desc(decode_splits=1)) == 0
 
 
+def test_too_many_heads():
+    for call in CALLS:
+        assert call(_desc(num_kv_heads=65537, num_q_heads=65537, num_seqs=1, max_blocks=2)) == pe.PE_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(num_seqs=1, max_blocks=16), 1), (dict(num_seqs=1, max_blocks=17), 2), (dict(num_seqs=1, head_dim=64, max_blocks=32), 1),
+    (dict(num_seqs=1, head_dim=64, max_blocks=33), 4), (dict(num_seqs=1, max_blocks=96), 12), (dict(num_seqs=1, max_blocks=104), 12),
+    (dict(num_seqs=1, max_blocks=128), 12), (dict(num_seqs=1, max_blocks=136), 17), (dict(num_seqs=1, num_q_heads=64, max_blocks=96), 8),
+    (dict(num_seqs=1, num_q_heads=64, max_blocks=104), 13), (dict(num_seqs=1, max_blocks=4096), 32),
+    (dict(num_seqs=1, num_kv_heads=1, num_q_heads=4, max_blocks=4096), 64), (dict(num_seqs=8, max_blocks=64), 4), (dict(num_seqs=10, max_blocks=64), 3),
+    (dict(num_seqs=11, max_blocks=63), 1), (dict(num_seqs=16, max_blocks=64), 2), (dict(num_seqs=17, max_blocks=127), 1),
+    (dict(num_seqs=17, max_blocks=128), 3), (dict(num_seqs=20, max_blocks=128), 3), (dict(num_seqs=21, max_blocks=128), 4),
+    (dict(num_seqs=24, max_blocks=128), 4), (dict(num_seqs=25, max_blocks=128), 1), (dict(num_seqs=32, max_blocks=4096), 1),
+    (dict(num_seqs=33, max_blocks=128), 4), (dict(num_seqs=33, max_blocks=127), 1), (dict(num_seqs=41, max_blocks=128), 4),
+    (dict(num_seqs=42, max_blocks=128), 1)])
+@pytest.mark.parametrize("dtype", [pe.PE_BF16, pe.PE_F32])
+def test_split_rule(kw, want, dtype):
+    """At the edges, on a device of 256 compute units (what the library assumes without one)."""
+    if torch.cuda.is_available() and torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("a device with another number of compute units")
+    d = _desc(**dict(dict(decode_splits=0, dtype=dtype), **kw))
+    assert pe.pe_workspace_bytes(pe.PE_OP_QUANT_DECODE, d) == (0 if want == 1 else want * d.num_seqs * d.num_q_heads * (d.head_dim + 2) * 4)
+
+
 def test_tensors_are_checked_before_the_call():
     x, i = torch.zeros((1, 8, 64)), torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError, match="must be a GPU tensor"):
