@@ -465,7 +465,18 @@ class Attention:
     started: bool = False      # the scores hold weights
 
 
-class LayeredCache:
+class LayeredAdmits:
+    """admit() for a driver of several layers."""
+
+    def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, whole=False):
+        """The caches' admit() in every layer, one after the other out of one list of pages: a plan for each."""
+        plans = [c.admit(new_lens, total_tokens, free, first_positions, whole=whole) for c in self.per_layer]
+        f = self.folded   # (each layer has swapped its part of the lengths)
+        f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens
+        return plans
+
+
+class LayeredCache(LayeredAdmits):
     def __init__(self, dtype, layers, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget,
                  device="cuda", shared=False, decode_opts=None):
         self.layers, self.S = layers, num_seqs
@@ -688,7 +699,7 @@ class QuantCache(Admits):
                        workspace=pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=self.k.device))
 
 
-class LayeredQuantCache:
+class LayeredQuantCache(LayeredAdmits):
     """The multi-layer driver over an 8-bit cache: evictions of all layers in one launch, then append and attention layer by layer.  With a
     rope, `positions` [S] serve every layer.  GraphedStepper replays its steps."""
 

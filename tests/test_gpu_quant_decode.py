@@ -114,6 +114,56 @@ def test_many_rows_and_long_ones():
     _run(14, [4000, 1], 2, 8, 64, 16, "f32", shared=True)
 
 
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_long_pieces(D, dt, G):
+    """Rows whole: two tiles in flight for D = 64, odd and even numbers of them, waves without any."""
+    _run(G, [1024, 1040, 1153, 1300, 2000, 2 * 8 * 16 * 5, 17], 1, G, D, 16, dt, splits=1)
+    _run(G, [3000, 5], 1, G, D, 128, dt, shared=True, splits=2)
+
+
+def test_lengths_that_the_table_does_not_hold():
+    """A caller's mistake: the row ends with its table; a negative length is none."""
+    c = QuantCache(20, [64, 64, 64], 1, 64, 16, torch.bfloat16, False, extra_blocks=0)
+    desc = c.desc(pe, 2)
+    q = torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    sl = torch.tensor([70000, -3, 2 ** 31 - 1], dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 7.0, device=DEV)
+    pe.pe_quant_decode(desc, c.quant(pe, desc, DEV), q.to(DEV), c.table.to(DEV), sl, 0.125, out, pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc))
+    for s in (0, 2):
+        assert_close(out[s], *attend(q[s].double(), c.k[s][0], c.v[s][0], torch.bfloat16, 0.125), torch.bfloat16)
+    assert bool((out[1] == 0).all())
+
+
+def test_two_graphs_with_one_workspace():
+    """Two layers' calls, captured apart, with the same workspace, replayed in turn on one stream."""
+    made = []
+    ws = None
+    for seed in (21, 22):
+        c = QuantCache(seed, [700, 900, 31], 2, 128, 16, torch.bfloat16, False)
+        desc = c.desc(pe, 8, decode_splits=5)
+        ws = pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc) if ws is None else ws
+        q = torch.randn((3, 8, 128), generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+        made.append((c, desc, c.quant(pe, desc, DEV), q, q.to(DEV), c.to(DEV), torch.empty_like(q, device=DEV)))
+    torch.cuda.synchronize()
+    graphs = []
+    for c, desc, cache, q, qd, d, out in made:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            pe.pe_quant_decode(desc, cache, qd, d[2], d[3], 128 ** -0.5, out, ws)
+    for _ in range(5):
+        for g, m in zip(graphs, made):
+            m[-1].fill_(3.0)
+            g.replay()
+    torch.cuda.synchronize()
+    for c, desc, cache, q, qd, d, out in made:
+        for s in range(3):
+            for h in range(2):
+                want, bound = attend(q[s, h * 4:h * 4 + 4].double(), c.k[s][h], c.v[s][h], torch.bfloat16)
+                assert_close(out[s, h * 4:h * 4 + 4], want, bound, torch.bfloat16)
+
+
 @pytest.mark.parametrize("splits", [0, 3, 16])
 def test_replayed_while_the_cache_grows(splits):
     """One graph, the lengths and the output's old contents changing between replays, eager calls in between."""

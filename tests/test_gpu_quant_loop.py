@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2509_04377_amd import binding as pe
-from paper_2509_04377_amd.engine import FreePages, GraphedStepper, LayeredQuantCache, PagedCache, QuantCache, empty_layout
+from paper_2509_04377_amd.engine import FreePages, GraphedStepper, LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout
 
 from _paged64 import DTYPES, assert_close
 from _paged64 import attend as attend_unrounded
@@ -101,19 +101,20 @@ def _model(dt, D, shared, layers, S, Hk, G, B, budget, lens, seed, roped):
     rope = pe.make_rope(D, 10000.0, interleaved=True) if roped else None
     model = LayeredQuantCache(dtype, layers, S, Hk, Hk * G, D, B, empty_layout(R, Hk, width, n_spare, P, DEV, shared), budget, shared=shared, rope=rope)
     free = FreePages.of(torch.randperm(P, generator=g).int().to(DEV))
-    plan = model.folded.admit(_i32(lens * layers), sum(lens) * layers, free)
+    plans = model.admit(_i32(lens), sum(lens), free)
+    assert all(p.cu_seqlens.tolist()[-1] == sum(lens) for p in plans) and model.folded.seq_lens.tolist() == [min(n, budget) for n in lens] * layers
+    used = model.folded.block_table[model.folded.block_table >= 0].tolist() + model.folded.spare.flatten().tolist()
+    assert len(set(used)) == len(used) and int(free.used) == len(used)   # no page twice, in no layer
     # (one staging cache for a layer at a time)
     rows = 1 if shared else Hk
     stage = PagedCache.create(dtype, S, Hk, Hk * G, D, B, empty_layout(S, Hk, width, 1, S * rows * (width + 1), DEV, shared), budget, shared=shared)
     for l, c in enumerate(model.per_layer):
-        c.seq_lens, c.seq_lens_alt = c.seq_lens_alt, c.seq_lens
         stage.seq_lens.zero_()
         p = stage.admit(_i32(lens), sum(lens), FreePages.of(torch.arange(S * rows * (width + 1), dtype=torch.int32, device=DEV)))
         k, v = (torch.randn((sum(lens), Hk, D), generator=g).to(dtype).to(DEV) for _ in range(2))
         stage.prefill_prune(k, v, p.cu_seqlens, max(lens))
         stage.set_host_lens(lens)
         model.take_layer(l, stage)
-    assert plan.cu_seqlens.numel() == R + 1
     return model
 
 
@@ -143,6 +144,41 @@ def test_replayed_steps_of_all_layers(shared, roped):
             c = made[1].per_layer[-1]
             _check(c, c.turned if roped else bufs[2][-1], out[-1], made[1].host_lens)
     assert len(stepper.graphs) <= 4
+
+
+def test_all_layers_of_an_unrounded_cache_are_admitted():
+    """LayeredCache: pages from one list, then a prune and steps, beside a cache whose layout came from the host."""
+    layers, S, Hk, Hq, D, B, budget, lens = 2, 3, 2, 4, 64, 16, 64, [100, 64, 9]
+    R, width, n_spare = layers * S, budget // B, budget // B
+    P = R * Hk * (width + n_spare)
+    g = torch.Generator().manual_seed(1)
+    ids = torch.randperm(P, generator=g).int()
+    one = LayeredCache(torch.float32, layers, S, Hk, Hq, D, B, empty_layout(R, Hk, width, n_spare, P, DEV), budget)
+    one.admit(_i32(lens), sum(lens), FreePages.of(ids.to(DEV)))
+    layout = empty_layout(R, Hk, width, n_spare, P, "cpu")
+    at = 0
+    for r in range(R):   # the same deal, on the host
+        need = -(-min(lens[r % S], budget) // B)
+        for h in range(Hk):
+            layout.block_table[r, h, :need] = ids[at:at + need]
+            layout.spare[r, h] = ids[at + need:at + need + n_spare]
+            at += need + n_spare
+    two = LayeredCache(torch.float32, layers, S, Hk, Hq, D, B, layout, budget)
+    assert torch.equal(one.folded.block_table, two.folded.block_table) and torch.equal(one.folded.spare, two.folded.spare)
+    cu = _i32([sum(lens[:i]) for i in range(S + 1)])
+    for l in range(layers):
+        k, v = (torch.randn((sum(lens), Hk, D), generator=g).to(DEV) for _ in range(2))
+        for m in (one, two):
+            m.prefill_prune_layer(l, k, v, cu, max(lens))
+    for m in (one, two):
+        m.set_host_lens(lens)
+    for step in range(40):
+        nk, nv = (torch.randn((layers, S, Hk, D), generator=g).to(DEV) for _ in range(2))
+        q = torch.randn((layers, S, Hq, D), generator=g).to(DEV)
+        outs = [torch.empty_like(q) for _ in range(2)]
+        for m, out in zip((one, two), outs):
+            m.decode_step(nk, nv, q, out)
+        assert torch.equal(*outs) and torch.equal(one.folded.block_table, two.folded.block_table), step
 
 
 @pytest.mark.parametrize("dt,shared", [("bf16", False), ("f32", True)])
