@@ -89,7 +89,9 @@ inline int quant_splits(const pe_cache_desc* d) {
 
 // The workgroup: eight waves, four where split rows make more workgroups than compute units (192 rows of D = 128 x 2048, ragged, in four 12.7, with eight
 // waves 14.6), and tiles in flight a wave: one (256 rows of D = 128 x 2048 21.4, two 21.5; 64 x 1024 in four 6.75 / 6.9), two for D = 64 in long
-// pieces, whose wave-loads are half as long (256 rows x 2048 12.3, one 13.6; 64 rows x 4096 in four 9.0 / 9.4; pieces of 256 5.5, two 6.3).
+// pieces, whose wave-loads are half as long (256 rows x 2048 12.3, one 13.6; 64 rows x 4096 in four 9.0 / 9.4; pieces of 256 5.5, two 6.3).  The
+// order is the same where the pages come from memory and not from the caches that a repeated step finds full (256 rows x 2048: D = 128 24.8, two
+// 25.5; D = 64 14.7, one 15.3).
 inline int quant_waves(const pe_cache_desc* d, int splits) {
   return splits > 1 && (int64_t)d->num_seqs * d->num_kv_heads * splits > host::compute_units() ? 4 : 8;
 }

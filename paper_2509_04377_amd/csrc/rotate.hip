@@ -3,7 +3,8 @@
 // Bound by memory: every element is read and written once (stored keys written twice), the angles cost some thirty instructions for
 // each pair of a token, whatever the number of heads.  A workgroup takes some tokens: first its threads put the cosines and
 // sines of their pairs into LDS, then they walk over (token, head, part), 16 bytes of each half of a pair at a time (neighbouring
-// pairs: 16 bytes), two or four of them on their way before the first is used.
+// pairs: 16 bytes), the next ones on their way while these are turned.  What is written does not pass through the caches (854 MB moved, with keys
+// and values stored: 146 us or 5.9 TB/s, a copy reaches 5.2; with ordinary stores 152; fp32, 36 MB: 6.6 us, 8.2).
 //
 // Where rows are not 16-byte aligned, or a half is no multiple of 16 bytes, threads walk over single pairs instead.
 #include "pe_rope_device.h"
@@ -206,12 +207,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, co
       w.x = Vec<T>::put(x);
     }
     if (w.first >= 0) {
-      if (w.to != nullptr) w.to[w.first] = w.x;
-      if (w.page != nullptr) w.page[w.first] = w.x;
+      if (w.to != nullptr) store_vec_stream(w.to, w.first, w.x);
+      if (w.page != nullptr) store_vec_stream(w.page, w.first, w.x);
     }
     if (w.second >= 0) {
-      if (w.to != nullptr) w.to[w.second] = w.y;
-      if (w.page != nullptr) w.page[w.second] = w.y;
+      if (w.to != nullptr) store_vec_stream(w.to, w.second, w.y);
+      if (w.page != nullptr) store_vec_stream(w.page, w.second, w.y);
     }
   };
 
