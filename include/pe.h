@@ -490,7 +490,7 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
  *     elements apart (a projection's output may hold all three side by side).  positions: [num_tokens] int32, any value.
  *     q, q_out both NULL: no queries; k NULL: no keys (then k_out, slots too).  q_out, k_out: strides of their own; in place
  *     (the same address and stride) or without overlap.  slots NULL: nothing is stored (v, pools not looked at); given, k_out may be NULL.
- *     The pools must not overlap the other tensors.  shared: slots [num_tokens] (all heads of a token lie in one slot).
+ *     The pools must not overlap the other tensors, nor q_out and k_out positions and slots.  shared: slots [num_tokens] (all heads of a token lie in one slot).
  *     D must be at least rotary_dim; at most 65536 query and key heads.
  */
 typedef enum { PE_ROPE_HALF = 0, PE_ROPE_INTERLEAVED = 1 } pe_rope_pairs;
@@ -516,7 +516,7 @@ int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose,
  *         k, v: [num_phys_blocks][B][D] (shared: [num_phys_blocks][B][Hk][D]) of one byte.
  *         scales: [num_phys_blocks][2] fp32 (shared: [num_phys_blocks][Hk][2]): K's and V's.
  *         k_tail, v_tail: [S][Hk][B][D] in desc->dtype (both layouts).
- *      k, v and tails 16-byte aligned, scales 8.
+ *      k, v and tails 16-byte aligned, scales 8; the five apart from one another and from what a call is given beside them.
  *      Rounding a page: with a = the largest magnitude of its B x D elements of a head, the scale is the least power of two (2^-126 at
  *      least) with a <= 448 scale (a = 0: 1), so that element / scale is exact and is rounded once, to the nearest e4m3 number (ties to
  *      even); a floating-point number's precision does not depend on the scale, and a power of two leaves every element that is read back

@@ -557,6 +557,9 @@ def pe_rotate(desc, rope, transpose, positions, q, k, v, q_out, k_out, slots=Non
         vp, vs = _token_rows(v if slots is not None else None, "v", T, desc.num_kv_heads, desc)
         qo, qos = _token_rows(q_out, "q_out", T, desc.num_q_heads, desc)
         ko, kos = _token_rows(k_out, "k_out", T, desc.num_kv_heads, desc)
+        rows = 1 if desc.layout == PE_LAYOUT_SHARED else desc.num_kv_heads
+        if slots is not None and slots.numel() != T * rows:
+            raise ValueError("slots must be of %d tokens and %d rows, got %s" % (T, rows, tuple(slots.shape)))
         status = L.pe_rotate(ctypes.byref(desc), ctypes.byref(rope), 1 if transpose else 0, T, _addr(positions, "positions", torch.int32),
                              qp, qs, kp, ks, vp, vs, qo, qos, ko, kos, _addr_opt(slots, "slots", torch.int64),
                              _addr_opt(k_pool, "k_pool"), _addr_opt(v_pool, "v_pool"), _stream())

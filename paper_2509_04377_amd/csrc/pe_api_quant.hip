@@ -9,10 +9,27 @@ using namespace pe::host;
 
 namespace {
 
-int check_cache(const pe_quant_cache* c) {
+// The five tensors of a cache.
+struct Parts {
+  struct { const void* p; size_t bytes; } of[5];
+  bool meet(const void* p, size_t bytes) const {
+    for (const auto& x : of)
+      if (overlap(x.p, x.bytes, p, bytes)) return true;
+    return false;
+  }
+};
+
+int check_cache(const pe_cache_desc* d, const pe_quant_cache* c, Parts* parts) {
   if (c == nullptr || !c->k || !c->v || !c->scales || !c->k_tail || !c->v_tail) return PE_ERR_INVALID_ARG;
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->scales, 8) || !aligned(c->k_tail, 16) || !aligned(c->v_tail, 16))
     return PE_ERR_INVALID_ARG;
+  const size_t rows = (size_t)d->num_phys_blocks * (d->layout == PE_LAYOUT_SHARED ? (size_t)d->num_kv_heads : 1);
+  const size_t pool = rows * d->block_size * d->head_dim;
+  const size_t tail = (size_t)d->num_seqs * d->num_kv_heads * d->block_size * d->head_dim * (d->dtype == PE_F32 ? 4 : 2);
+  *parts = Parts{{{c->k, pool}, {c->v, pool}, {c->scales, rows * 8}, {c->k_tail, tail}, {c->v_tail, tail}}};
+  for (int i = 1; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(parts->of[i].p, parts->of[i].bytes, parts->of[j].p, parts->of[j].bytes)) return PE_ERR_INVALID_ARG;
   return PE_OK;
 }
 
@@ -22,11 +39,14 @@ extern "C" {
 
 int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* k_pool, const void* v_pool,
                    const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table, float* scores_out, void* stream) {
+  Parts parts;
   int st = check_desc(desc);
-  if (st == PE_OK) st = check_cache(cache);
+  if (st == PE_OK) st = check_cache(desc, cache, &parts);
   if (st != PE_OK) return st;
   if (!k_pool || !v_pool || !src_table || !seq_lens || !block_table) return PE_ERR_INVALID_ARG;
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(scores_out, 4)) return PE_ERR_INVALID_ARG;
+  const size_t page = (size_t)desc->block_size * desc->head_dim * (desc->dtype == PE_F32 ? 4 : 2);  // (how many there are is not known)
+  if (parts.meet(k_pool, page) || parts.meet(v_pool, page)) return PE_ERR_INVALID_ARG;
   if (desc->num_kv_heads > 65536 || !pe::quant_pages_launches(desc)) return PE_ERR_UNSUPPORTED;
   pe::QuantPagesArgs a;
   a.cache = *cache;
@@ -50,18 +70,23 @@ int pe_quant_append(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
                     void* q_out, const void* new_k, const void* new_v, int32_t* block_table, const int32_t* seq_lens,
                     int32_t* seq_lens_out, int32_t* freed_phys, const int32_t* spare, int32_t* spare_used, int32_t n_spare,
                     float* scores, void* stream) {
+  Parts parts;
   int st = check_desc(desc);
-  if (st == PE_OK) st = check_cache(cache);
+  if (st == PE_OK) st = check_cache(desc, cache, &parts);
   if (st != PE_OK) return st;
   if (!new_k || !new_v || !block_table || !seq_lens || !seq_lens_out || !freed_phys || !spare || !spare_used || n_spare < 1)
     return PE_ERR_INVALID_ARG;
   if (!aligned(new_k, 16) || !aligned(new_v, 16) || !aligned(scores, 4)) return PE_ERR_INVALID_ARG;
   const size_t lens = (size_t)desc->num_seqs * 4, bytes = desc->dtype == PE_F32 ? 4 : 2;
   if (overlap(seq_lens, lens, seq_lens_out, lens)) return PE_ERR_INVALID_ARG;
+  const size_t kv = (size_t)desc->num_seqs * desc->num_kv_heads * desc->head_dim * bytes;
+  if (parts.meet(new_k, kv) || parts.meet(new_v, kv)) return PE_ERR_INVALID_ARG;
   if (rope != nullptr) {
     if (!rope_ok(rope, desc->head_dim) || !positions || !q || !q_out || !aligned(q, 16) || !aligned(q_out, 16)) return PE_ERR_INVALID_ARG;
-    const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * bytes, kv = (size_t)desc->num_seqs * desc->num_kv_heads * desc->head_dim * bytes;
-    if ((q != q_out && overlap(q, o, q_out, o)) || overlap(q_out, o, new_k, kv) || overlap(q_out, o, new_v, kv)) return PE_ERR_INVALID_ARG;
+    const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * bytes;
+    if ((q != q_out && overlap(q, o, q_out, o)) || overlap(q_out, o, new_k, kv) || overlap(q_out, o, new_v, kv) || parts.meet(q_out, o) ||
+        overlap(q_out, o, positions, lens))
+      return PE_ERR_INVALID_ARG;
   }
   if (desc->num_kv_heads > 65536 || (int64_t)desc->num_seqs * desc->num_kv_heads >= 1 << 23) return PE_ERR_UNSUPPORTED;
   pe::QuantAppendArgs a;
@@ -92,15 +117,15 @@ int pe_quant_append(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
 
 int pe_quant_decode(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* q, const int32_t* block_table,
                     const int32_t* seq_lens, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  Parts parts;
   int st = check_desc(desc);
-  if (st == PE_OK) st = check_cache(cache);
+  if (st == PE_OK) st = check_cache(desc, cache, &parts);
   if (st != PE_OK) return st;
   if (!q || !block_table || !seq_lens || !out) return PE_ERR_INVALID_ARG;
   const bool bf16 = desc->dtype == PE_BF16;
   if (!aligned(q, 16) || !aligned(out, bf16 ? 2 : 4) || !finite(softmax_scale)) return PE_ERR_INVALID_ARG;
   const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * (bf16 ? 2 : 4);
-  const size_t tail = (size_t)desc->num_seqs * desc->num_kv_heads * desc->block_size * desc->head_dim * (bf16 ? 2 : 4);
-  if ((out != q && overlap(out, o, q, o)) || overlap(out, o, cache->k_tail, tail) || overlap(out, o, cache->v_tail, tail)) return PE_ERR_INVALID_ARG;
+  if ((out != q && overlap(out, o, q, o)) || parts.meet(out, o)) return PE_ERR_INVALID_ARG;
   if (desc->num_kv_heads > 65536) return PE_ERR_UNSUPPORTED;
   const int splits = pe::quant_splits(desc);
   const int ws = check_workspace(workspace, workspace_bytes, pe::decode_partials_bytes(desc->num_seqs, desc->num_q_heads, desc->head_dim, splits));

@@ -131,6 +131,12 @@ int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose,
     for (int j = 0; j < 3; ++j)
       if (!(i == j && out[i].p == in[j].p && out[i].stride == in[j].stride) && !apart(out[i], in[j])) return PE_ERR_INVALID_ARG;
   if (!apart(out[0], out[1])) return PE_ERR_INVALID_ARG;
+  const size_t slot_bytes = (size_t)num_tokens * 8 * (desc->layout == PE_LAYOUT_SHARED ? 1 : desc->num_kv_heads);
+  for (const Rows& r : out) {
+    if (r.p == nullptr) continue;
+    const size_t all = span(num_tokens, r.stride, r.width, bytes);
+    if (overlap(r.p, all, positions, (size_t)num_tokens * 4) || (slots != nullptr && overlap(r.p, all, slots, slot_bytes))) return PE_ERR_INVALID_ARG;
+  }
   if (slots != nullptr) {
     const size_t pool = (size_t)desc->num_phys_blocks * desc->block_size * desc->head_dim * bytes *
                         (desc->layout == PE_LAYOUT_SHARED ? desc->num_kv_heads : 1);

@@ -269,6 +269,7 @@ PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         (args[10] != Py_None && !v.get(args[7], T, d.num_kv_heads, d)) || !q_out.get(args[8], T, d.num_q_heads, d) ||
         !k_out.get(args[9], T, d.num_kv_heads, d))
       Py_RETURN_NONE;
+    if (args[10] != Py_None && THPVariable_Unpack(args[10]).numel() != T * (d.layout == PE_LAYOUT_SHARED ? 1 : d.num_kv_heads)) Py_RETURN_NONE;
     const auto stream = c10::hip::getCurrentHIPStream().stream();
     int status;
     Py_BEGIN_ALLOW_THREADS

@@ -215,3 +215,15 @@ def test_on_another_stream():
     side.synchronize()
     assert_close(qd, *want[0], torch.bfloat16)
     assert_close(kd, *want[1], torch.bfloat16)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_slots_of_other_tokens_are_refused(shared):
+    d = pe.make_desc(torch.bfloat16, 1, 2, 4, 64, 16, 4, 8, pe.PE_LAYOUT_SHARED if shared else pe.PE_LAYOUT_PER_HEAD)
+    on = dict(dtype=torch.bfloat16, device=DEV)
+    q, k, pool = torch.zeros((5, 4, 64), **on), torch.zeros((5, 2, 64), **on), torch.zeros((2, 8, 16) + (2,) * shared + (64,), **on)
+    for n in (0, 4, 6):
+        slots = torch.full((n,) if shared else (n, 2), -1, dtype=torch.int64, device=DEV)
+        with pytest.raises(ValueError, match="slots must be"):
+            pe.pe_rotate(d, pe.make_rope(64, 1e4), False, torch.zeros(5, dtype=torch.int32, device=DEV), q, k, k.clone(), q.clone(), None, slots,
+                         pool[0], pool[1])

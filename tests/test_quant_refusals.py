@@ -113,6 +113,32 @@ def test_decode():
     assert pe.pe_workspace_bytes(pe.PE_OP_QUANT_DECODE, _desc(decode_splits=1)) == 0
 
 
+PARTS = ("k", "v", "scales", "k_tail", "v_tail")
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_caches_whose_tensors_meet(call):
+    for shared in (False, True):
+        d = _desc(layout=pe.PE_LAYOUT_SHARED if shared else pe.PE_LAYOUT_PER_HEAD)
+        rows = 4096 * (8 if shared else 1)
+        size = dict(zip(PARTS, (rows * 16 * 128, rows * 16 * 128, rows * 8, 4 * 8 * 16 * 128 * 2, 4 * 8 * 16 * 128 * 2)))
+        for i, one in enumerate(PARTS):
+            for j, other in enumerate(PARTS):
+                if i != j:   # `one` begins in the last 16 bytes of `other`
+                    assert call(d, cache=_cache(**{one: P[j].value + size[other] - 16})) == pe.PE_ERR_INVALID_ARG, (one, other)
+
+
+def test_tensors_on_the_cache():
+    d = _desc()
+    for i in range(5):
+        for name in ("k_pool", "v_pool"):
+            assert _pages(d, **{name: _at(i, 64)}) == pe.PE_ERR_INVALID_ARG, (name, i)
+        for name in ("k", "v", "q_out"):
+            assert _append(d, **{name: _at(i, 64)}) == pe.PE_ERR_INVALID_ARG, (name, i)
+        assert _decode(d, out=_at(i, 64)) == pe.PE_ERR_INVALID_ARG, i
+    assert _append(d, q_out=P[5]) == pe.PE_ERR_INVALID_ARG   # the positions
+
+
 def test_too_many_heads():
     for call in CALLS:
         assert call(_desc(num_kv_heads=65537, num_q_heads=65537, num_seqs=1, max_blocks=2)) == pe.PE_ERR_UNSUPPORTED

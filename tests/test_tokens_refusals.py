@@ -119,6 +119,8 @@ def test_rotate_outputs_that_lie_on_something():
     for kw in (dict(q_out=near(1)), dict(k_out=near(2)), dict(q_out=P[2]), dict(k_out=P[1]), dict(k_out=P[3]), dict(q_out=P[5]), dict(k_out=P[4]),
                dict(v_pool=P[7]), dict(k_pool=P[1]), dict(v_pool=P[3]), dict(k_pool=P[5]), dict(q_out=P[1], qos=32 * 128 + 8)):
         assert _rotate(d, **kw) == pe.PE_ERR_INVALID_ARG, kw
+    for kw in (dict(q_out=P[0]), dict(k_out=near(0, 128)), dict(q_out=P[6]), dict(k_out=near(6, 64))):   # positions, slots
+        assert _rotate(d, **kw) == pe.PE_ERR_INVALID_ARG, kw
     # parts of one row a token: in place is fine (the check behind it is reached), the neighbour's place is not
     row = 48 * 128
     side = dict(qs=row, ks=row, vs=row, qos=row, kos=row, q=P[1], k=near(1, 2 * 32 * 128), v=near(1, 2 * 40 * 128))
