@@ -39,6 +39,7 @@ namespace {
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kGrow = 3.f;  // how far above the largest logit (log2) the softmax reference is set
 constexpr int kTile = 16;     // tokens
+constexpr int kMostBlock = 128;
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
@@ -62,36 +63,45 @@ __device__ __forceinline__ uint32_t widen2(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, UPPER));
 }
 
-// Elements in the activations' type as bfloat16 operands: one, or three whose sum they are (each what a truncation leaves of the rest).  `raw`: N
-// elements as they lie in memory, two of a term to a word.
+// Elements in the activations' type as bfloat16 operands: one, or three whose sum they are (each what a truncation leaves of the rest), made
+// one after the other, so that a term's registers are free for the next.
 template <typename T>
 struct Terms;
 template <>
 struct Terms<bf16_t> {
   static constexpr int N = 1;
+  static constexpr int kWords = 1;  // registers of two elements
   template <int E>
-  static __device__ __forceinline__ void load(const void* from, int64_t element, uint32_t (&t)[1][E / 2]) {
+  static __device__ __forceinline__ void load(const void* from, int64_t element, uint32_t (&raw)[E / 2]) {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(from) + element);
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) t[0][i] = w[i];
+    for (int i = 0; i < E / 2; ++i) raw[i] = w[i];
+  }
+  template <int E>
+  static __device__ __forceinline__ void take(uint32_t (&raw)[E / 2], uint32_t (&t)[E / 2]) {
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) t[i] = raw[i];
   }
 };
 template <>
 struct Terms<float> {
   static constexpr int N = 3;
+  static constexpr int kWords = 2;
   template <int E>
-  static __device__ __forceinline__ void load(const void* from, int64_t element, uint32_t (&t)[3][E / 2]) {
-    const float* w = static_cast<const float*>(from) + element;
+  static __device__ __forceinline__ void load(const void* from, int64_t element, uint32_t (&raw)[E]) {
+    const uint32_t* w = static_cast<const uint32_t*>(from) + element;
+#pragma unroll
+    for (int i = 0; i < E; ++i) raw[i] = w[i];
+  }
+  // The next term, and what is left without it.
+  template <int E>
+  static __device__ __forceinline__ void take(uint32_t (&raw)[E], uint32_t (&t)[E / 2]) {
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) {
-      float a = w[2 * i], b = w[2 * i + 1];
-#pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        const uint32_t ha = __float_as_uint(a), hb = __float_as_uint(b);
-        t[n][i] = __builtin_amdgcn_perm(hb, ha, 0x07060302u);
-        a -= __uint_as_float(ha & 0xffff0000u);
-        b -= __uint_as_float(hb & 0xffff0000u);
-      }
+      const uint32_t a = raw[2 * i], b = raw[2 * i + 1];
+      t[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      raw[2 * i] = __float_as_uint(__uint_as_float(a) - __uint_as_float(a & 0xffff0000u));
+      raw[2 * i + 1] = __float_as_uint(__uint_as_float(b) - __uint_as_float(b & 0xffff0000u));
     }
   }
 };
@@ -243,8 +253,12 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
     const int num_kv_heads, const int max_blocks, const uint32_t inv_heads, const uint32_t shape, const QuantParams p) {
   using TL = Tile<T, D, GW>;
   using VLoad = typename TL::VLoad;
+  using TM = Terms<T>;
   constexpr int NJ = TL::NJ, EV = TL::EV, NQ = TL::NQ;
   constexpr int GH = 16 / GW;  // heads computed; g_real of them exist
+  // The tail without the first 8-bit tiles on their way: their registers then leave two workgroups of eight waves a place on a compute unit (320 rows x 1024
+  // of fp32, D = 128, 21.2 us for 24.5, 288 of three tokens 4.8 / 6.9, 1024 x 2048 94 / 102; 64 rows x 1024 in four, which do not need it, 9.2 / 8.8).
+  constexpr bool kTailAlone = NQ == 3 && D == 128;
 
   __shared__ WaveStates<WAVES, GH, D> sm;
 
@@ -306,24 +320,28 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
     u32x4_t kb[DEPTH][NJ];
     VLoad vb[DEPTH][4];
     float2 sc[DEPTH];
+    const auto begin_loads = [&] {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const bool more = first + d * stride < ntiles;
-      const int64_t there = base_of(first + d * stride, phys[d]), base = more ? there : 0;
-      issue_k(kb[d], base, more ? k_off : 0, more ? 8 * row_bytes : 0);
-      issue_v(vb[d], base, more ? v_off : 0, more ? 4 * row_bytes : 0);
-      sc[d] = scales_of(more ? phys[d] : 0);
-    }
+      for (int d = 0; d < DEPTH; ++d) {
+        const bool more = first + d * stride < ntiles;
+        const int64_t there = base_of(first + d * stride, phys[d]), base = more ? there : 0;
+        issue_k(kb[d], base, more ? k_off : 0, more ? 8 * row_bytes : 0);
+        issue_v(vb[d], base, more ? v_off : 0, more ? 4 * row_bytes : 0);
+        sc[d] = scales_of(more ? phys[d] : 0);
+      }
+    };
+    if constexpr (!kTailAlone) begin_loads();
     // queries: what faces a lane's elements of K, of the column's head and part
     bf16x8_t qop[NQ][2];
     const int64_t q_head = (int64_t)s * num_kv_heads * g_real + hk * g_real + (h < g_real ? h : 0);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint32_t t[NQ][4];
-      Terms<T>::template load<8>(p.q, q_head * D + (D == 64 ? 0 : 64 * (c & 1)) + 16 * g + 8 * e, t);
+      uint32_t raw[4 * TM::kWords], t[4];
+      TM::template load<8>(p.q, q_head * D + (D == 64 ? 0 : 64 * (c & 1)) + 16 * g + 8 * e, raw);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        const u32x4_t w = {t[n][0], t[n][1], t[n][2], t[n][3]}, zero = {0u, 0u, 0u, 0u};
+        TM::template take<8>(raw, t);
+        const u32x4_t w = {t[0], t[1], t[2], t[3]}, zero = {0u, 0u, 0u, 0u};
         qop[n][e] = __builtin_bit_cast(bf16x8_t, h < g_real ? w : zero);
       }
     }
@@ -332,13 +350,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
     for (int tail = tail0; tail < tail_tiles; tail += stride) {
       const int left = len - full - tail * kTile;
       const int64_t token0 = ((int64_t)row << log2_block) + tail * kTile;
-      uint32_t kt[NJ][2][NQ][4], vt[4][NQ][EV / 2];
+      uint32_t kt[NJ][2][4 * TM::kWords], vt[4][EV / 2 * TM::kWords];
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) Terms<T>::template load<8>(p.k_tail, (token0 + k_tok + 8 * j) * D + k_elem + 8 * e, kt[j][e]);
+        for (int e = 0; e < 2; ++e) TM::template load<8>(p.k_tail, (token0 + k_tok + 8 * j) * D + k_elem + 8 * e, kt[j][e]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) Terms<T>::template load<EV>(p.v_tail, (token0 + 4 * i + g) * D + EV * m, vt[i]);
+      for (int i = 0; i < 4; ++i) TM::template load<EV>(p.v_tail, (token0 + 4 * i + g) * D + EV * m, vt[i]);
       f32x4_t prod[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) prod[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -350,9 +368,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) k[j][e][i] = kt[j][e][n][i];
+          for (int e = 0; e < 2; ++e) TM::template take<8>(kt[j][e], k[j][e]);
         if (n < 2)
           TL::template products<NQ>(k, qop, prod);
         else
@@ -365,13 +381,17 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
       for (int n = 0; n < NQ; ++n) {
         uint32_t v[4][EV / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          TM::template take<EV>(vt[i], v[i]);
 #pragma unroll
-          for (int j = 0; j < EV / 2; ++j) v[i][j] = 4 * i + g < left ? vt[i][n][j] : 0u;  // (what is no token may be anything)
+          for (int j = 0; j < EV / 2; ++j) v[i][j] = 4 * i + g < left ? v[i][j] : 0u;  // (what is no token may be anything)
+        }
         tl.accumulate_words(v, pop);
       }
+      if (WAVES * kTile >= kMostBlock) break;  // (a page's tiles: no wave has two)
     }
 
+    if constexpr (kTailAlone) begin_loads();
     int ph_next = phys[DEPTH];
     for (int tile0 = first; tile0 < ntiles; tile0 += DEPTH * stride) {
 #pragma unroll
