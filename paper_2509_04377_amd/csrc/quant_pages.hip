@@ -6,9 +6,9 @@
 // registers give the page's score (Alg. 1: the mean of the tokens' norm ratios, as score_blocks.hip has it), so that an eviction does not need
 // the page in full precision again.
 //
-// Bound by memory: a page is read once and half (fp32: a quarter) of it written.  256 rows of D = 128 x 2048 in bfloat16, 402 MB, take 70 us (5.7 TB/s;
-// from memory that the caches do not hold, and with sources in any order, 72 to 85: a copy of as many bytes takes 77).  Loads without and stores with the non-temporal
-// hint give 65 where the caches hold a part of it, else 84; stores with the hint alone 78 and 81.
+// Bound by memory: a page is read once and half (fp32: a quarter) of it written.  256 rows of D = 128 x 2048 in bfloat16, 402 MB, take 70 us (5.7 TB/s)
+// where the caches hold a part of them; else 72 to 77 with pages in order and 84 with shuffled ones, of which 2 KiB are written at a time (a copy of
+// as many bytes takes 77).  Stores with the non-temporal hint too, shuffled: 78 and 79 to 81; without it on the loads 65 and 84, on neither 84 and 85.
 #include "pe_device.h"
 #include "pe_norms.h"
 #include "pe_quant.h"
