@@ -126,8 +126,8 @@ int pe_quant_decode(const pe_cache_desc* desc, const pe_quant_cache* cache, cons
   if (!aligned(q, 16) || !aligned(out, bf16 ? 2 : 4) || !finite(softmax_scale)) return PE_ERR_INVALID_ARG;
   const size_t o = (size_t)desc->num_seqs * desc->num_q_heads * desc->head_dim * (bf16 ? 2 : 4);
   if ((out != q && overlap(out, o, q, o)) || parts.meet(out, o)) return PE_ERR_INVALID_ARG;
-  if (desc->num_kv_heads > 65536) return PE_ERR_UNSUPPORTED;
   const int splits = pe::quant_splits(desc);
+  if (desc->num_kv_heads > 65536 || !pe::quant_launches(desc, splits)) return PE_ERR_UNSUPPORTED;
   const int ws = check_workspace(workspace, workspace_bytes, pe::decode_partials_bytes(desc->num_seqs, desc->num_q_heads, desc->head_dim, splits));
   if (ws != PE_OK) return ws;
   pe::QuantDecodeArgs a;

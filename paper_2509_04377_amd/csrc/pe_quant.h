@@ -8,6 +8,7 @@
 #include "../../include/pe.h"
 #include "pe_check.h"
 #include "pe_launch.h"
+#include "pe_place.h"
 
 namespace pe {
 
@@ -97,6 +98,13 @@ inline int quant_waves(const pe_cache_desc* d, int splits) {
 }
 inline int quant_depth(const pe_cache_desc* d, int splits, int waves) {
   return d->head_dim == 64 && waves == 8 && (int64_t)d->max_blocks * d->block_size / splits >= 1024 ? 2 : 1;
+}
+
+// Whether the attention and the merge of its splits (a workgroup of up to eight waves for a query row) are launches that the runtime takes.
+inline bool quant_launches(const pe_cache_desc* d, int splits) {
+  PlaceGrid grid;
+  if (!place_grid(d->num_seqs, d->num_kv_heads, splits, true, &grid)) return false;
+  return host::one_launch(grid.x, quant_waves(d, splits) * 64) && (splits == 1 || host::one_launch((int64_t)d->num_seqs * d->num_q_heads, 512));
 }
 
 inline size_t quant_workspace_bytes(const pe_cache_desc* d) {

@@ -139,6 +139,21 @@ def test_tensors_on_the_cache():
     assert _append(d, q_out=P[5]) == pe.PE_ERR_INVALID_ARG   # the positions
 
 
+@pytest.mark.parametrize("kw,want", [
+    # few splits of very many rows, four waves each; what fits lacks its workspace
+    (dict(num_seqs=(1 << 23) - 8, decode_splits=2), pe.PE_ERR_WORKSPACE), (dict(num_seqs=1 << 23, decode_splits=2), pe.PE_ERR_UNSUPPORTED),
+    # whole rows, eight waves each
+    (dict(num_seqs=1 << 23, decode_splits=1), pe.PE_ERR_UNSUPPORTED), (dict(num_seqs=1 << 23, decode_splits=0), pe.PE_ERR_UNSUPPORTED),
+    # the merge, with eight query rows to a row
+    (dict(num_seqs=(1 << 20) - 8, num_q_heads=8, decode_splits=2), pe.PE_ERR_WORKSPACE),
+    (dict(num_seqs=1 << 20, num_q_heads=8, decode_splits=2), pe.PE_ERR_UNSUPPORTED)])
+def test_launches_of_too_many_threads(kw, want):
+    base = dict(num_kv_heads=1, num_q_heads=1, head_dim=64, max_blocks=1, num_phys_blocks=1 << 24)
+    far = dict(out=ctypes.c_void_p(1 << 60))
+    cache = _cache(**{n: (i + 1) << 50 for i, n in enumerate(PARTS)})
+    assert _decode(_desc(**dict(base, **kw)), cache=cache, ws=None, n=0, **far) == want
+
+
 def test_too_many_heads():
     for call in CALLS:
         assert call(_desc(num_kv_heads=65537, num_q_heads=65537, num_seqs=1, max_blocks=2)) == pe.PE_ERR_UNSUPPORTED
