@@ -152,7 +152,7 @@ int pe_score_blocks(const pe_cache_desc* desc, const void* k_pool, const void* v
  *     budget_tokens: C, a positive multiple of B.
  *     block_table is an INPUT: the caller has put ceil(min(L_s, C)/B) distinct physical pages in each
  *     row (ceil(min(max_seqlen, C)/B) > max_blocks is refused with PE_ERR_INVALID_ARG).  Slots of the tail
- *     page past the kept count are left untouched.
+ *     page past the kept count are left untouched.  Where an entry is -1 the tokens of that page are dropped.
  *     kept_idx_out: NULL, or [S][Hk][budget_tokens] int32 that receives the in-sequence indices of the
  *     kept tokens in ascending order, -1 padded.
  *     workspace: pe_workspace_bytes(PE_OP_PREFILL_PRUNE, desc, total_tokens).

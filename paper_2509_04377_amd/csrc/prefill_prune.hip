@@ -745,7 +745,9 @@ __global__ __launch_bounds__(THREADS) void gather_kernel(const uint4* __restrict
   for (int e = r; e < n_kept; e += kRowsPerPass) {
     const int pos = kept_before_chunk + e;
     const int64_t src = ((int64_t)(t0 + src_tok[e]) * num_kv_heads + h) * VEC_PER_ROW + u;
-    const int64_t slot = ((int64_t)bt[pos >> log2_block] << log2_block) + (pos & block_mask);
+    const int page = bt[pos >> log2_block];
+    if (page < 0) continue;  // the row did not get it
+    const int64_t slot = ((int64_t)page << log2_block) + (pos & block_mask);
     const int64_t dst = (SHARED ? slot * num_kv_heads + h : slot) * VEC_PER_ROW + u;
     k_pool[dst] = k_in[src];
     v_pool[dst] = v_in[src];
@@ -804,7 +806,9 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
     for (int e = r; e < m; e += kRowsPerPass) {
       const int pos = p0 + e;
       const int64_t src = ((int64_t)(t0 + token_of(e)) * heads + h) * VEC_PER_ROW + u;
-      const int64_t slot = ((int64_t)bt[pos >> log2_block] << log2_block) + (pos & block_mask);
+      const int page = bt[pos >> log2_block];
+      if (page < 0) continue;  // the row did not get it
+      const int64_t slot = ((int64_t)page << log2_block) + (pos & block_mask);
       const int64_t dst = (SHARED ? slot * heads + h : slot) * VEC_PER_ROW + u;
       k_pool[dst] = k_in[src];
       v_pool[dst] = v_in[src];
