@@ -463,7 +463,25 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
  *     the last token gets position 0 and slot -1 (a padded batch), tokens that find no room are not written.
  *     The outputs must not overlap the inputs or one another.  At most 65536 KV heads (else PE_ERR_UNSUPPORTED).
  *     shared: block_table [S][max_blocks], spare [S][n_spare], slots_out [total_tokens].
+ *
+ * pe_plan_tokens_ex: the same with options (NULL, or a field NULL: without).
+ *     admitted: [S], out: 1 where a sequence begins (it held no token, brings some and got its pages), 2 where one goes on, 0 where a
+ *     sequence was left as it was or brings nothing.
+ * pe_prefill_prune_admitted: pe_prefill_prune of the sequences that begin, by that array (NULL: of all).  Of every other sequence neither pages nor
+ *     seq_lens_out nor kept_idx_out is written, whatever tokens cu_seqlens has of it: running ones, and those that were left as they were.
+ *     admitted must not overlap seq_lens_out.
  */
+typedef struct pe_plan_opts {
+  int32_t* admitted;
+} pe_plan_opts;
+int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const int32_t* seq_lens, const int32_t* new_lens,
+                      const int32_t* first_positions, int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free,
+                      const int32_t* free_used, int32_t* block_table, int32_t* spare, int32_t n_spare, int32_t* seq_lens_out,
+                      int32_t* free_used_out, int32_t* cu_seqlens_out, int32_t* positions_out, int64_t* slots_out, void* stream);
+int pe_prefill_prune_admitted(const pe_cache_desc* desc, const void* k_in, const void* v_in, const int32_t* cu_seqlens,
+                              const int32_t* admitted, int64_t total_tokens, int32_t max_seqlen, int32_t budget_tokens, void* k_pool,
+                              void* v_pool, const int32_t* block_table, int32_t* seq_lens_out, int32_t* kept_idx_out, void* workspace,
+                              size_t workspace_bytes, void* stream);
 int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int32_t* new_lens, const int32_t* first_positions,
                    int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free, const int32_t* free_used,
                    int32_t* block_table, int32_t* spare, int32_t n_spare, int32_t* seq_lens_out, int32_t* free_used_out,

@@ -33,7 +33,7 @@ EXPORTS = ["pe_workspace_bytes", "pe_status_string", "pe_version", "pe_decode_sp
            "pe_append_paged_decode", "pe_score_recent_blocks", "pe_evict_blocks_cached", "pe_evict_blocks_ex", "pe_score_evict",
            "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers",
            "pe_tree_decode", "pe_append_path", "pe_page_bounds", "pe_select_pages",
-           "pe_paged_decode_weights", "pe_plan_tokens", "pe_rope_init", "pe_rotate",
+           "pe_paged_decode_weights", "pe_plan_tokens", "pe_plan_tokens_ex", "pe_prefill_prune_admitted", "pe_rope_init", "pe_rotate",
            "pe_quant_pages", "pe_quant_append", "pe_quant_decode"]
 
 
@@ -54,6 +54,10 @@ class pe_rope(ctypes.Structure):
     """Filled by make_rope()."""
     _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("magnitude", ctypes.c_float), ("filled", ctypes.c_int32),
                 ("turns", ctypes.c_uint64 * 64)]
+
+
+class pe_plan_opts(ctypes.Structure):
+    _fields_ = [("admitted", ctypes.c_void_p)]
 
 
 class pe_quant_cache(ctypes.Structure):
@@ -169,6 +173,10 @@ def lib():
         dbl, rp, cp = ctypes.c_double, ctypes.POINTER(pe_rope), ctypes.POINTER(pe_quant_cache)
         L.pe_plan_tokens.restype = ctypes.c_int
         L.pe_plan_tokens.argtypes = [dp, vp, vp, vp, i64, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.pe_plan_tokens_ex.restype = ctypes.c_int
+        L.pe_plan_tokens_ex.argtypes = [dp, ctypes.POINTER(pe_plan_opts)] + L.pe_plan_tokens.argtypes[1:]
+        L.pe_prefill_prune_admitted.restype = ctypes.c_int
+        L.pe_prefill_prune_admitted.argtypes = [dp, vp, vp, vp, vp] + L.pe_prefill_prune.argtypes[4:]
         L.pe_rope_init.restype = ctypes.c_int
         L.pe_rope_init.argtypes = [rp, i32, i32, dbl, i32, dbl, dbl, dbl, dbl, dbl]
         L.pe_rotate.restype = ctypes.c_int
@@ -182,7 +190,7 @@ def lib():
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
-                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens", "rotate",
+                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens", "plan_tokens_ex", "prefill_prune_admitted", "rotate",
                      "quant_pages", "quant_append", "quant_decode"):
             setattr(L, "addr_" + name, ctypes.cast(getattr(L, "pe_" + name), vp).value)
         _lib = L
@@ -284,18 +292,24 @@ def pe_score_blocks(desc, k_pool, v_pool, block_table, seq_lens, scores_out, wor
 
 
 def pe_prefill_prune(desc, k_in, v_in, cu_seqlens, total_tokens, max_seqlen, budget_tokens, k_pool, v_pool,
-                     block_table, seq_lens_out, kept_idx_out, workspace):
+                     block_table, seq_lens_out, kept_idx_out, workspace, admitted=None):
+    """admitted: only the sequences that a plan of tokens let begin (pe_prefill_prune_admitted)."""
     L = lib()
-    status = _host.prefill_prune(L.addr_prefill_prune, desc, k_in, v_in, cu_seqlens, total_tokens, max_seqlen, budget_tokens,
-                                 k_pool, v_pool, block_table, seq_lens_out, kept_idx_out, workspace)
+    if admitted is None:
+        status = _host.prefill_prune(L.addr_prefill_prune, desc, k_in, v_in, cu_seqlens, total_tokens, max_seqlen, budget_tokens,
+                                     k_pool, v_pool, block_table, seq_lens_out, kept_idx_out, workspace)
+    else:
+        status = _host.prefill_prune_admitted(L.addr_prefill_prune_admitted, desc, k_in, v_in, cu_seqlens, admitted, total_tokens, max_seqlen,
+                                              budget_tokens, k_pool, v_pool, block_table, seq_lens_out, kept_idx_out, workspace)
     if status is None:
         wp, wn = _ws(workspace)
-        status = L.pe_prefill_prune(ctypes.byref(desc), _addr(k_in, "k_in"), _addr(v_in, "v_in"),
-                                    _addr(cu_seqlens, "cu_seqlens", torch.int32), int(total_tokens), int(max_seqlen),
-                                    int(budget_tokens), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                                    _addr(block_table, "block_table", torch.int32),
-                                    _addr(seq_lens_out, "seq_lens_out", torch.int32),
-                                    _addr_opt(kept_idx_out, "kept_idx_out", torch.int32), wp, wn, _stream())
+        status = L.pe_prefill_prune_admitted(ctypes.byref(desc), _addr(k_in, "k_in"), _addr(v_in, "v_in"),
+                                             _addr(cu_seqlens, "cu_seqlens", torch.int32), _addr_opt(admitted, "admitted", torch.int32),
+                                             int(total_tokens), int(max_seqlen),
+                                             int(budget_tokens), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                             _addr(block_table, "block_table", torch.int32),
+                                             _addr(seq_lens_out, "seq_lens_out", torch.int32),
+                                             _addr_opt(kept_idx_out, "kept_idx_out", torch.int32), wp, wn, _stream())
     check(status, "pe_prefill_prune")
 
 
@@ -505,20 +519,29 @@ def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, soft
 
 
 def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used, block_table, spare,
-                   seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out):
+                   seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, admitted=None):
+    """With an argument behind slots_out: pe_plan_tokens_ex."""
     L = lib()
-    status = _host.plan_tokens(L.addr_plan_tokens, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages, free_used,
-                               block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out)
+    opts = (admitted,)
+    if all(o is None for o in opts):
+        status = _host.plan_tokens(L.addr_plan_tokens, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages,
+                                   free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out)
+    else:
+        status = _host.plan_tokens_ex(L.addr_plan_tokens_ex, desc, opts, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages,
+                                      free_pages, free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out,
+                                      slots_out)
     if status is None:
-        status = L.pe_plan_tokens(ctypes.byref(desc), _addr(seq_lens, "seq_lens", torch.int32), _addr(new_lens, "new_lens", torch.int32),
-                                  _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
-                                  _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
-                                  _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
-                                  _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
-                                  _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
-                                  _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
-                                  _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
-                                  _stream())
+        o = pe_plan_opts(_addr_opt(admitted, "admitted", torch.int32))
+        status = L.pe_plan_tokens_ex(ctypes.byref(desc), ctypes.byref(o), _addr(seq_lens, "seq_lens", torch.int32),
+                                     _addr(new_lens, "new_lens", torch.int32),
+                                     _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
+                                     _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
+                                     _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
+                                     _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
+                                     _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
+                                     _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
+                                     _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
+                                     _stream())
     check(status, "pe_plan_tokens")
 
 

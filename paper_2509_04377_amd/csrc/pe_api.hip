@@ -329,6 +329,14 @@ int pe_prefill_prune(const pe_cache_desc* desc, const void* k_in, const void* v_
                      int64_t total_tokens, int32_t max_seqlen, int32_t budget_tokens, void* k_pool, void* v_pool,
                      const int32_t* block_table, int32_t* seq_lens_out, int32_t* kept_idx_out, void* workspace,
                      size_t workspace_bytes, void* stream) {
+  return pe_prefill_prune_admitted(desc, k_in, v_in, cu_seqlens, nullptr, total_tokens, max_seqlen, budget_tokens, k_pool, v_pool, block_table,
+                                   seq_lens_out, kept_idx_out, workspace, workspace_bytes, stream);
+}
+
+int pe_prefill_prune_admitted(const pe_cache_desc* desc, const void* k_in, const void* v_in, const int32_t* cu_seqlens,
+                              const int32_t* admitted, int64_t total_tokens, int32_t max_seqlen, int32_t budget_tokens, void* k_pool,
+                              void* v_pool, const int32_t* block_table, int32_t* seq_lens_out, int32_t* kept_idx_out, void* workspace,
+                              size_t workspace_bytes, void* stream) {
   const int st = check_desc(desc);
   if (st != PE_OK) return st;
   if (!cu_seqlens || !k_pool || !v_pool || !block_table || !seq_lens_out) return PE_ERR_INVALID_ARG;
@@ -342,6 +350,7 @@ int pe_prefill_prune(const pe_cache_desc* desc, const void* k_in, const void* v_
   }
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(k_in, 16) || !aligned(v_in, 16))
     return PE_ERR_INVALID_ARG;
+  if (admitted != nullptr && overlap(admitted, (size_t)desc->num_seqs * 4, seq_lens_out, (size_t)desc->num_seqs * 4)) return PE_ERR_INVALID_ARG;
   const int ws = check_workspace(workspace, workspace_bytes,
                                  pe::prune_workspace_bytes(desc->num_seqs, desc->num_kv_heads, total_tokens,
                                                            desc->layout == PE_LAYOUT_SHARED));
@@ -367,6 +376,7 @@ int pe_prefill_prune(const pe_cache_desc* desc, const void* k_in, const void* v_
   a.is_bf16 = desc->dtype == PE_BF16;
   a.shared = desc->layout == PE_LAYOUT_SHARED;
   a.compute_units = compute_units();
+  a.admitted = admitted;
   return pe::launch_prefill_prune(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PE_OK : PE_ERR_HIP;
 }
 

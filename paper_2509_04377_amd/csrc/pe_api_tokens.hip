@@ -22,6 +22,14 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
                    int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free, const int32_t* free_used,
                    int32_t* block_table, int32_t* spare, int32_t n_spare, int32_t* seq_lens_out, int32_t* free_used_out,
                    int32_t* cu_seqlens_out, int32_t* positions_out, int64_t* slots_out, void* stream) {
+  return pe_plan_tokens_ex(desc, nullptr, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, num_free, free_used,
+                           block_table, spare, n_spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, stream);
+}
+
+int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const int32_t* seq_lens, const int32_t* new_lens,
+                      const int32_t* first_positions, int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free,
+                      const int32_t* free_used, int32_t* block_table, int32_t* spare, int32_t n_spare, int32_t* seq_lens_out,
+                      int32_t* free_used_out, int32_t* cu_seqlens_out, int32_t* positions_out, int64_t* slots_out, void* stream) {
   const int st = check_desc(desc);
   if (st != PE_OK) return st;
   if (!seq_lens || !new_lens || !free_pages || !free_used || !block_table || !seq_lens_out || !free_used_out) return PE_ERR_INVALID_ARG;
@@ -29,13 +37,14 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
     return PE_ERR_INVALID_ARG;
   if (budget_tokens % desc->block_size != 0) return PE_ERR_INVALID_ARG;
   if (!aligned(slots_out, 8)) return PE_ERR_INVALID_ARG;
+  const pe_plan_opts o = opts != nullptr ? *opts : pe_plan_opts{};
   const bool shared = desc->layout == PE_LAYOUT_SHARED;
   const size_t S = (size_t)desc->num_seqs, per_seq = shared ? 1 : (size_t)desc->num_kv_heads;
   if (desc->num_kv_heads > 65536 || (int64_t)per_seq * ((int64_t)desc->max_blocks + n_spare) > 0x7fffffffLL) return PE_ERR_UNSUPPORTED;
   const struct { const void* p; size_t bytes; } in[] = {{seq_lens, S * 4}, {new_lens, S * 4}, {first_positions, S * 4},
                                                         {free_pages, (size_t)num_free * 4}, {free_used, 4}},
       out[] = {{block_table, S * per_seq * desc->max_blocks * 4}, {spare, S * per_seq * n_spare * 4}, {seq_lens_out, S * 4}, {free_used_out, 4},
-               {cu_seqlens_out, (S + 1) * 4}, {positions_out, (size_t)total_tokens * 4}, {slots_out, (size_t)total_tokens * per_seq * 8}};
+               {cu_seqlens_out, (S + 1) * 4}, {positions_out, (size_t)total_tokens * 4}, {slots_out, (size_t)total_tokens * per_seq * 8}, {o.admitted, S * 4}};
   for (size_t i = 0; i < sizeof(out) / sizeof(out[0]); ++i) {
     if (out[i].p == nullptr || out[i].bytes == 0) continue;
     for (const auto& x : in)
@@ -56,6 +65,7 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
   a.cu_out = cu_seqlens_out;
   a.positions_out = positions_out;
   a.slots_out = slots_out;
+  a.admitted = o.admitted;
   a.total_tokens = total_tokens;
   a.num_free = num_free;
   a.n_spare = n_spare;

@@ -190,6 +190,17 @@ struct QuantCache {
   bool get(PyObject* o) { return structure(o, quant_cache_type, &cache); }
 };
 
+struct PlanOpts {  // (admitted,)
+  pe_plan_opts o{};
+  std::tuple<const pe_plan_opts*> c{&o};
+  bool get(PyObject* t) {
+    IntsOrNone admitted;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 1 || !admitted.get(PyTuple_GET_ITEM(t, 0))) return false;
+    o.admitted = std::get<0>(admitted.c);
+    return true;
+  }
+};
+
 template <typename... Args, size_t... I>
 bool get_all(std::tuple<Args...>& a, PyObject* const* o, std::index_sequence<I...>) {
   return (std::get<I>(a).get(o[I]) && ...);
@@ -375,6 +386,9 @@ PyMethodDef methods[] = {
     // workspace
     method<call<decltype(&pe_prefill_prune), Tensor, Tensor, Ints, Number<int64_t>, Number<int32_t>, Number<int32_t>, Tensor, Tensor,
                 Ints, Ints, IntsOrNone, Workspace>>("prefill_prune"),
+    // k_in, v_in, cu_seqlens, admitted, and the same
+    method<call<decltype(&pe_prefill_prune_admitted), Tensor, Tensor, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Number<int32_t>, Tensor,
+                Tensor, Ints, Ints, IntsOrNone, Workspace>>("prefill_prune_admitted"),
     // k_pool, v_pool, block_table, seq_lens, budget_tokens, scores_inout
     method<call<decltype(&pe_score_triggered_blocks), Tensor, Tensor, Ints, Ints, Number<int32_t>, Floats>>(
         "score_triggered_blocks"),
@@ -403,6 +417,9 @@ PyMethodDef methods[] = {
     // seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out
     method<call<decltype(&pe_plan_tokens), Ints, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Ints, Numel, Ints, Ints, IntsOrNone,
                 LastDimOrNone, Ints, Ints, IntsOrNone, IntsOrNone, WordsOrNone>>("plan_tokens"),
+    // opts, and the same
+    method<call<decltype(&pe_plan_tokens_ex), PlanOpts, Ints, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Ints, Numel, Ints, Ints, IntsOrNone,
+                LastDimOrNone, Ints, Ints, IntsOrNone, IntsOrNone, WordsOrNone>>("plan_tokens_ex"),
     method<rotate>("rotate"),
     // cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out
     method<call<decltype(&pe_quant_pages), QuantCache, Tensor, Tensor, Ints, Ints, Ints, FloatsOrNone>>("quant_pages"),

@@ -121,6 +121,7 @@ struct PruneArgs {
   bool is_bf16;
   bool shared = false;  // one decision per sequence (head-mean token scores), pages [B][Hk][D]
   int compute_units = 256;
+  const int32_t* admitted = nullptr;  // of each sequence; null, or 1: it is pruned
 };
 hipError_t launch_prefill_prune(const PruneArgs& a, hipStream_t stream);
 size_t prune_workspace_bytes(int num_seqs, int num_kv_heads, int64_t total_tokens, bool shared);

@@ -114,6 +114,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
       if (lane == 0) dealt_of[wave] = mine;
       if (s < num_seqs) {
         a.seq_lens_out[s] = served ? (int32_t)kept : len;
+        if (a.admitted != nullptr) a.admitted[s] = !served || n == 0 ? 0 : len == 0 ? 1 : 2;
         if (a.cu_out != nullptr) {
           if (s == 0) a.cu_out[0] = 0;
           a.cu_out[s + 1] = (int32_t)(t_end < 0x7fffffffLL ? t_end : 0x7fffffffLL);

@@ -15,6 +15,8 @@
 //                     share of what is kept.
 // A token is kept iff score > T, or score == T and at least q equal-score tokens precede it.
 //
+// With `admitted` only its sequences of 1 are selected and copied (the sweep goes over all tokens as they lie); the others' workgroups return.
+//
 // Head-shared mode (one decision per sequence, pages [B][Hk][D]): a token's score is the mean of its heads' scores (head
 // order, fp64, one rounding), taken by the sweep itself where none of its workgroups ends inside a token, else by a
 // kernel behind it.  The selection is made on that one score row, the copy head by head with its result.
@@ -540,7 +542,8 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_kernel(co
                                                              uint32_t* __restrict__ sel, int32_t* __restrict__ before,
                                                              int32_t* __restrict__ seq_lens_out,
                                                              int32_t* __restrict__ kept_idx_out, int64_t total_tokens,
-                                                             int64_t chunk_slots, int num_kv_heads, int budget) {
+                                                             int64_t chunk_slots, int num_kv_heads, int budget,
+                                                             const int32_t* __restrict__ admitted) {
   using Row = RowScores<NV, LV>;
   constexpr int kHeldChunks = Row::kHeld / kChunk;
   static_assert(kHeldChunks <= kSelMaxHeldChunks, "chunk counters");
@@ -550,6 +553,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_kernel(co
   __shared__ uint32_t held_count[kSelMaxHeldChunks];
   const int row = (int)blockIdx.x;
   const int s = row / num_kv_heads, h = row % num_kv_heads;
+  if (admitted != nullptr && admitted[s] != 1) return;
   const int t0 = cu_seqlens[s];
   const int L = cu_seqlens[s + 1] - t0;
   const int keep = L < budget ? L : budget;
@@ -637,7 +641,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_kernel(co
 
 // The smallest holding that covers rows of max_seqlen tokens (or the largest there is): a larger one than needed costs loads,
 // branches and, beyond 16 scores a thread, the second workgroup of a compute unit.
-using SelectKernel = void (*)(const float*, const int32_t*, uint32_t*, int32_t*, int32_t*, int32_t*, int64_t, int64_t, int, int);
+using SelectKernel = void (*)(const float*, const int32_t*, uint32_t*, int32_t*, int32_t*, int32_t*, int64_t, int64_t, int, int, const int32_t*);
 SelectKernel select_kernel_for(int max_seqlen) {
   const int vecs = (max_seqlen + 4 * kSelThreads - 1) / (4 * kSelThreads);
   if (vecs <= 1) return select_kernel<1, 0>;
@@ -668,7 +672,7 @@ __global__ __launch_bounds__(THREADS) void gather_kernel(const uint4* __restrict
                                                          int32_t* __restrict__ kept_idx_out, int64_t total_tokens,
                                                          int64_t chunk_slots, int num_kv_heads, int rows,
                                                          int log2_block, int max_blocks, int budget, int row0,
-                                                         int chunk0) {
+                                                         int chunk0, const int32_t* __restrict__ admitted) {
   constexpr int kTokPerThread = kChunk / THREADS;
   __shared__ uint32_t wave_sum[THREADS / kWave];
   __shared__ int32_t src_tok[kChunk];  // kept tokens of this chunk, in order: in-sequence index
@@ -682,7 +686,7 @@ __global__ __launch_bounds__(THREADS) void gather_kernel(const uint4* __restrict
   const int sel_row = SHARED ? s : row, sel_h = SHARED ? 0 : h;  // whose scores decide
   const int t0 = cu_seqlens[s];
   const int L = cu_seqlens[s + 1] - t0;
-  if (chunk * kChunk >= L) return;
+  if (chunk * kChunk >= L || (admitted != nullptr && admitted[s] != 1)) return;
   const int tid = (int)threadIdx.x;
   const int lane = lane_id();
   const int wave = tid / kWave;
@@ -772,7 +776,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
     const uint4* __restrict__ k_in, const uint4* __restrict__ v_in, const float* __restrict__ scores,
     const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ block_table, uint4* __restrict__ k_pool,
     uint4* __restrict__ v_pool, int32_t* __restrict__ seq_lens_out, int32_t* __restrict__ kept_idx_out, int64_t total_tokens,
-    int log2_block, int max_blocks, int budget, int log2_parts, int seq0) {
+    int log2_block, int max_blocks, int budget, int log2_parts, int seq0, const int32_t* __restrict__ admitted) {
   using Row = RowScores<NV, 0>;
   __shared__ SelectLds sm;
   uint32_t* const list = sm.hist;  // tokens of the positions at hand, once the threshold is known
@@ -780,6 +784,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
   // (head, sequence, part): the parts of a row lie side by side on one XCD where the number of rows is a multiple of eight
   const int h = (int)blockIdx.x, heads = (int)gridDim.x, s = seq0 + (int)blockIdx.y, part = (int)blockIdx.z;
   const int sel_row = SHARED ? s : s * heads + h, sel_h = SHARED ? 0 : h;
+  if (admitted != nullptr && admitted[s] != 1) return;
   const int t0 = cu_seqlens[s];
   const int L = cu_seqlens[s + 1] - t0;
   const int keep = L < budget ? L : budget;
@@ -959,13 +964,13 @@ hipError_t launch(const PruneArgs& a, hipStream_t stream) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)a.num_kv_heads, (unsigned)ns, 1u << log2_parts), dim3(kSelThreads), 0, stream,
                          (const uint4*)a.k_in, (const uint4*)a.v_in, sel_scores, a.cu_seqlens, a.block_table, (uint4*)a.k_pool,
                          (uint4*)a.v_pool, a.seq_lens_out, a.kept_idx_out, a.total_tokens, ilog2(a.block_size), a.max_blocks,
-                         a.budget, log2_parts, s0);
+                         a.budget, log2_parts, s0, a.admitted);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return e;
   }
   hipLaunchKernelGGL(select_kernel_for(a.max_seqlen), dim3((unsigned)rows), dim3(kSelThreads), 0, stream, sel_scores, a.cu_seqlens,
-                     w.sel, w.before, a.seq_lens_out, a.kept_idx_out, a.total_tokens, w.chunk_slots, heads, a.budget);
+                     w.sel, w.before, a.seq_lens_out, a.kept_idx_out, a.total_tokens, w.chunk_slots, heads, a.budget, a.admitted);
   if ((e = hipGetLastError()) != hipSuccess || chunks_per_row == 0) return e;
   // Plain stores for what is kept.  With the non-temporal hint prunes of 32 x 16384 tokens that go into the same pools again and
   // again take 454 us instead of 467, but those of a model's layers, one after the other and each into its own pool, 475 instead of
@@ -980,7 +985,7 @@ hipError_t launch(const PruneArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(gather, dim3((unsigned)copied * (unsigned)nc), dim3(threads), 0, stream, (const uint4*)a.k_in,
                        (const uint4*)a.v_in, sel_scores, a.cu_seqlens, w.sel, w.before, a.block_table, (uint4*)a.k_pool,
                        (uint4*)a.v_pool, a.kept_idx_out, a.total_tokens, w.chunk_slots, a.num_kv_heads, copied,
-                       ilog2(a.block_size), a.max_blocks, a.budget, s0 * a.num_kv_heads, c0);
+                       ilog2(a.block_size), a.max_blocks, a.budget, s0 * a.num_kv_heads, c0, a.admitted);
     return (e = hipGetLastError()) == hipSuccess;
   });
   return e;

@@ -81,6 +81,7 @@ class Plan:
     cu_seqlens: torch.Tensor   # [S + 1] int32
     positions: torch.Tensor    # [T] int32
     slots: torch.Tensor        # [T, Hk] int64 (shared: [T])
+    admitted: torch.Tensor = None  # [S] int32: 1 a sequence that begins, 2 one that goes on, 0 one that was left as it was or brings nothing
 
 
 def empty_layout(num_seqs, num_kv_heads, max_blocks, n_spare, num_phys_blocks, device="cuda", shared=False):
@@ -96,7 +97,8 @@ class Admits:
 
     def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, plan=None, whole=False):
         """Pages for the tokens that every sequence brings (new_lens [S] int32 on the device, packed total_tokens of them or fewer), up to
-        the budget, and for sequences that begin their spare pages too.  Sequences that do not get their pages stay as they were.  whole: the
+        the budget, and for sequences that begin their spare pages too.  Sequences that do not get their pages stay as they were; which
+        those are the plan's `admitted` says, on the device, and the cache keeps it for its prefill_prune().  whole: the
         tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
         lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
         set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
@@ -105,10 +107,13 @@ class Admits:
             rows = self.block_table.shape[1:-1]   # (shared: none)
             plan = Plan(torch.empty(self.desc.num_seqs + 1, dtype=torch.int32, device=dev), torch.empty(total_tokens, dtype=torch.int32, device=dev),
                         torch.empty((total_tokens,) + tuple(rows), dtype=torch.int64, device=dev))
+        if plan.admitted is None:
+            plan.admitted = torch.empty(self.desc.num_seqs, dtype=torch.int32, device=dev)
         if self.seq_lens_alt is None:
             self.seq_lens_alt = torch.empty_like(self.seq_lens)
         _launch(pe.pe_plan_tokens, self.desc, self.seq_lens, new_lens, first_positions, int(total_tokens), 0 if whole else self.budget, free.pages, free.used,
-                self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots)
+                self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots, plan.admitted)
+        self.admitted = plan.admitted
         self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
         free.used, free.used_alt = free.used_alt, free.used
         return plan
@@ -143,6 +148,7 @@ class PagedCache(Admits):
     fused_evict: bool = False  # score + evict of a trigger step in one pass over the pages (pe_score_evict)
     selection: "Selection" = None  # attend to selected pages only (select_pages)
     attention: "Attention" = None  # `scores` are the attention that pages got (evict_by_attention)
+    admitted: torch.Tensor = None  # [S] int32, of the last admit(): prefill_prune() writes its sequences of 1; None: all
 
     @staticmethod
     def create(dtype, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device="cuda",
@@ -182,11 +188,13 @@ class PagedCache(Admits):
         return self.desc.layout == pe.PE_LAYOUT_SHARED
 
     def prefill_prune(self, k_in, v_in, cu_seqlens, max_seqlen, kept_idx_out=None, workspace=None):
+        """Prompts into the pages, up to the budget.  Behind admit() those of the sequences that it let begin: running sequences, and
+        those that did not get their pages, stay as they are."""
         total = k_in.shape[0]
         if workspace is None:
             workspace = pe.alloc_workspace(pe.PE_OP_PREFILL_PRUNE, self.desc, total, device=k_in.device)
         _launch(pe.pe_prefill_prune, self.desc, k_in, v_in, cu_seqlens, total, max_seqlen, self.budget, self.k_pool, self.v_pool,
-                         self.block_table, self.seq_lens, kept_idx_out, workspace)
+                         self.block_table, self.seq_lens, kept_idx_out, workspace, self.admitted)
 
     def rotate_store(self, rope, plan: Plan, q, k, v, q_out, k_out=None):
         """rotate(), and the turned keys and the values into the pages that admit() planned for them (prompts that are kept whole)."""
@@ -378,6 +386,7 @@ class PagedCache(Admits):
         fields = {name: getattr(d, name) for name, _ in d._fields_}
         views = {name: getattr(self, name)[sl] for name in ("block_table", "seq_lens", "spare", "spare_used", "freed_phys",
                                                             "evicted_logical", "scores", "host_lens")}
+        views["admitted"] = None if self.admitted is None else self.admitted[sl]
         return replace(self, desc=pe.pe_cache_desc(**{**fields, "num_seqs": end - first}), **views, seq_lens_alt=None, selection=None,
                        host_scored=None if self.host_scored is None else self.host_scored[sl])
 
@@ -617,6 +626,7 @@ class QuantCache(Admits):
     budget: int
     workspace: torch.Tensor
     host_lens: list
+    admitted: torch.Tensor = None   # of the last admit()
     rope: pe.pe_rope = None         # turns keys and queries on their way (positions: see decode_step)
     positions: torch.Tensor = None  # [S] int32, of the new token of every sequence: the caller's, changed in place from step to step
     turned: torch.Tensor = None     # [S, Hq, D]: the queries, turned
@@ -645,7 +655,7 @@ class QuantCache(Admits):
                           table.to(device).contiguous(), torch.zeros(num_seqs, **i32), torch.zeros(num_seqs, **i32), spare.to(device).contiguous(),
                           torch.zeros(per_row, **i32), torch.full(per_row, -1, **i32), torch.full(per_row, -1, **i32),
                           torch.full((num_seqs, num_kv_heads, layout.max_blocks), float("inf"), dtype=torch.float32, **on), int(budget),
-                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, rope,
+                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, None, rope,
                           torch.zeros(num_seqs, **i32) if rope is not None else None,
                           torch.empty((num_seqs, num_q_heads, head_dim), dtype=dtype, **on) if rope is not None else None)
 
@@ -693,7 +703,7 @@ class QuantCache(Admits):
         d, sl = self.desc, slice(first, end)
         desc = pe.pe_cache_desc(**{**{name: getattr(d, name) for name, _ in d._fields_}, "num_seqs": end - first})
         names = ("k_tail", "v_tail", "block_table", "seq_lens", "seq_lens_alt", "spare", "spare_used", "freed_phys", "evicted_logical", "scores",
-                 "host_lens", "positions", "turned")
+                 "host_lens", "positions", "turned", "admitted")
         views = {name: None if getattr(self, name) is None else getattr(self, name)[sl] for name in names}
         return replace(self, desc=desc, cache=pe.make_quant_cache(desc, self.k, self.v, self.scales, views["k_tail"], views["v_tail"]), **views,
                        workspace=pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=self.k.device))
