@@ -467,12 +467,17 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
  * pe_plan_tokens_ex: the same with options (NULL, or a field NULL: without).
  *     admitted: [S], out: 1 where a sequence begins (it held no token, brings some and got its pages), 2 where one goes on, 0 where a
  *     sequence was left as it was or brings nothing.
+ *     spare_used, freed_phys: [S][Hk] (shared: [S]), in/out: 0 (where n_spare > 0) and -1 in the rows of sequences that begin, whose place an
+ *     earlier sequence may have had: what pe_append_kv counts from is then the new list, and a page that was freed is no longer linked.
+ *     Without them the caller sees to it.
  * pe_prefill_prune_admitted: pe_prefill_prune of the sequences that begin, by that array (NULL: of all).  Of every other sequence neither pages nor
  *     seq_lens_out nor kept_idx_out is written, whatever tokens cu_seqlens has of it: running ones, and those that were left as they were.
  *     admitted must not overlap seq_lens_out.
  */
 typedef struct pe_plan_opts {
   int32_t* admitted;
+  int32_t* spare_used;
+  int32_t* freed_phys;
 } pe_plan_opts;
 int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const int32_t* seq_lens, const int32_t* new_lens,
                       const int32_t* first_positions, int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free,

@@ -44,7 +44,8 @@ int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const
   const struct { const void* p; size_t bytes; } in[] = {{seq_lens, S * 4}, {new_lens, S * 4}, {first_positions, S * 4},
                                                         {free_pages, (size_t)num_free * 4}, {free_used, 4}},
       out[] = {{block_table, S * per_seq * desc->max_blocks * 4}, {spare, S * per_seq * n_spare * 4}, {seq_lens_out, S * 4}, {free_used_out, 4},
-               {cu_seqlens_out, (S + 1) * 4}, {positions_out, (size_t)total_tokens * 4}, {slots_out, (size_t)total_tokens * per_seq * 8}, {o.admitted, S * 4}};
+               {cu_seqlens_out, (S + 1) * 4}, {positions_out, (size_t)total_tokens * 4}, {slots_out, (size_t)total_tokens * per_seq * 8}, {o.admitted, S * 4},
+               {o.spare_used, S * per_seq * 4}, {o.freed_phys, S * per_seq * 4}};
   for (size_t i = 0; i < sizeof(out) / sizeof(out[0]); ++i) {
     if (out[i].p == nullptr || out[i].bytes == 0) continue;
     for (const auto& x : in)
@@ -66,6 +67,8 @@ int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const
   a.positions_out = positions_out;
   a.slots_out = slots_out;
   a.admitted = o.admitted;
+  a.spare_used = n_spare > 0 ? o.spare_used : nullptr;
+  a.freed_phys = o.freed_phys;
   a.total_tokens = total_tokens;
   a.num_free = num_free;
   a.n_spare = n_spare;

@@ -190,13 +190,17 @@ struct QuantCache {
   bool get(PyObject* o) { return structure(o, quant_cache_type, &cache); }
 };
 
-struct PlanOpts {  // (admitted,)
+struct PlanOpts {  // (admitted, spare_used, freed_phys)
   pe_plan_opts o{};
   std::tuple<const pe_plan_opts*> c{&o};
   bool get(PyObject* t) {
-    IntsOrNone admitted;
-    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 1 || !admitted.get(PyTuple_GET_ITEM(t, 0))) return false;
+    IntsOrNone admitted, spare_used, freed_phys;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 3 || !admitted.get(PyTuple_GET_ITEM(t, 0)) || !spare_used.get(PyTuple_GET_ITEM(t, 1)) ||
+        !freed_phys.get(PyTuple_GET_ITEM(t, 2)))
+      return false;
     o.admitted = std::get<0>(admitted.c);
+    o.spare_used = std::get<0>(spare_used.c);
+    o.freed_phys = std::get<0>(freed_phys.c);
     return true;
   }
 };

@@ -23,6 +23,8 @@ struct PlanArgs {
   int32_t* positions_out;  // may be null
   int64_t* slots_out;      // may be null
   int32_t* admitted;       // may be null
+  int32_t* spare_used;     // may be null
+  int32_t* freed_phys;     // may be null
   int64_t total_tokens;
   int num_free, n_spare, budget, num_seqs, rows_per_seq, block_size, max_blocks;
 };

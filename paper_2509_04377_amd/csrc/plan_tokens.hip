@@ -126,6 +126,14 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) dealt = dealt_of[w] > dealt ? dealt_of[w] : dealt;
     }
+    if (a.spare_used != nullptr || a.freed_phys != nullptr) {  // rows of sequences that begin: what an earlier one left
+      for (int idx = (int)blockIdx.x * kThreads + me; idx < count * rows; idx += (int)gridDim.x * kThreads) {
+        const int i = idx / rows;
+        if (q.served[i] == 0 || q.len[i] != 0 || q.token_end[i] == (i > 0 ? q.token_end[i - 1] : before.tokens)) continue;
+        if (a.spare_used != nullptr) a.spare_used[(int64_t)s0 * rows + idx] = 0;
+        if (a.freed_phys != nullptr) a.freed_phys[(int64_t)s0 * rows + idx] = -1;
+      }
+    }
     const int64_t t_last = q.token_end[count - 1] < a.total_tokens ? q.token_end[count - 1] : a.total_tokens;
     const int64_t p_last = q.page_end[count - 1] < left ? q.page_end[count - 1] : left;
 

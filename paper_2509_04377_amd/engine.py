@@ -98,7 +98,9 @@ class Admits:
     def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, plan=None, whole=False):
         """Pages for the tokens that every sequence brings (new_lens [S] int32 on the device, packed total_tokens of them or fewer), up to
         the budget, and for sequences that begin their spare pages too.  Sequences that do not get their pages stay as they were; which
-        those are the plan's `admitted` says, on the device, and the cache keeps it for its prefill_prune().  whole: the
+        those are the plan's `admitted` says, on the device, and the cache keeps it for its prefill_prune().  A sequence begins where seq_lens
+        are 0 (its place may have been another's: its spare list counts from its start again, and the pages that the other one
+        held are the caller's to hand back).  whole: the
         tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
         lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
         set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
@@ -112,7 +114,8 @@ class Admits:
         if self.seq_lens_alt is None:
             self.seq_lens_alt = torch.empty_like(self.seq_lens)
         _launch(pe.pe_plan_tokens, self.desc, self.seq_lens, new_lens, first_positions, int(total_tokens), 0 if whole else self.budget, free.pages, free.used,
-                self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots, plan.admitted)
+                self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots, plan.admitted,
+                self.spare_used, self.freed_phys)
         self.admitted = plan.admitted
         self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
         free.used, free.used_alt = free.used_alt, free.used

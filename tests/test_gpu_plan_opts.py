@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2509_04377_amd import binding as pe
+from paper_2509_04377_amd.engine import FreePages, PagedCache, QuantCache, empty_layout
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -69,3 +70,60 @@ def test_who_was_admitted(case):
     admitted = torch.full((len(c.lens),), -9, dtype=torch.int32, device=DEV)
     assert c.run(admitted=admitted) == c.run()
     assert admitted.tolist() == c.served()
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("given", [("spare_used", "freed_phys"), ("spare_used",), ("freed_phys",)])
+def test_rows_that_begin_forget_the_sequence_before(case, given):
+    c = _Call(**case)
+    S, rows = len(c.lens), c.rows
+    opts = {name: torch.full((S, rows), 5, dtype=torch.int32, device=DEV) for name in given}
+    assert c.run(**opts) == c.run()
+    for name, t in opts.items():
+        new = 5 if name == "spare_used" and not c.n_spare else 0 if name == "spare_used" else -1
+        assert t.tolist() == [[new if a == 1 else 5] * rows for a in c.served()], name
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "quant"])
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_place_that_is_used_again(kind, shared):
+    """A sequence that used all of its spare pages and freed some ends; the next one in its place appends as the first one did."""
+    dtype, S, Hk, G, D, B, budget, n_spare = torch.float32 if kind == "f32" else torch.bfloat16, 2, 2, 2, 64, 16, 48, 3
+    rows, width = 1 if shared else Hk, 3
+    P = 3 * S * rows * (width + n_spare)
+    ids = torch.randperm(P, generator=torch.Generator().manual_seed(4)).int().to(DEV)
+
+    def life(dirty):
+        empty = empty_layout(S, Hk, width, n_spare, P, DEV, shared)
+        c = (QuantCache if kind == "quant" else PagedCache).create(dtype, S, Hk, Hk * G, D, B, empty, budget, shared=shared)
+        free = FreePages.of(ids[P // 2:].contiguous())
+        if dirty:   # what a former sequence leaves
+            c.spare_used.fill_(n_spare)
+            c.freed_phys.fill_(int(ids[0]))
+            c.block_table.fill_(int(ids[1]))
+            c.spare.fill_(int(ids[2]))
+        lens = [10, 20]
+        g = torch.Generator().manual_seed(5)
+        plan = c.admit(_i32(lens), sum(lens), free)
+        k, v = (torch.randn((sum(lens), Hk, D), generator=g).to(dtype).to(DEV) for _ in range(2))
+        if kind == "quant":
+            stage = PagedCache.create(dtype, S, Hk, Hk * G, D, B, empty_layout(S, Hk, width, 1, P, DEV, shared), budget, shared=shared)
+            p = stage.admit(_i32(lens), sum(lens), FreePages.of(ids))
+            stage.prefill_prune(k, v, p.cu_seqlens, max(lens))
+            stage.set_host_lens(lens)
+            c.take(stage)
+        else:
+            c.prefill_prune(k, v, plan.cu_seqlens, max(lens))
+            c.set_host_lens(lens)
+        got = []
+        for _ in range(3 * B):
+            nk, nv = (torch.randn((S, Hk, D), generator=g).to(dtype).to(DEV) for _ in range(2))
+            out = torch.empty((S, Hk * G, D), dtype=dtype, device=DEV)
+            c.decode_step(nk, nv, torch.randn(out.shape, generator=g).to(dtype).to(DEV), out)
+            got.append(out)
+        held = [[c.block_table.view(S, rows, width)[s, h, :-(-n // B)].tolist() for h in range(rows)] for s, n in enumerate(c.seq_lens.tolist())]
+        assert all(p >= 0 for s in held for r in s for p in r) and len({p for s in held for r in s for p in r}) == sum(len(r) for s in held for r in s)
+        return got, held, c.spare_used.tolist(), c.freed_phys.tolist()
+
+    (a, *rest), (b, *other) = life(False), life(True)
+    assert rest == other and all(torch.equal(x, y) for x, y in zip(a, b))

@@ -25,9 +25,11 @@ def _plan(n_spare=2, **opts):
                                       a["used"], a["table"], a["spare"], n_spare, a["lens_out"], a["used_out"], a["cu"], a["pos"], a["slots"], None)
 
 
+@pytest.mark.parametrize("out", ["admitted", "spare_used", "freed_phys"])
 @pytest.mark.parametrize("other", NAMES)
-def test_what_is_written_lies_by_itself(other):
-    assert _plan(admitted=AT[other]) == pe.PE_ERR_INVALID_ARG
+def test_what_is_written_lies_by_itself(out, other):
+    assert _plan(**{out: AT[other]}) == pe.PE_ERR_INVALID_ARG
+    assert _plan(admitted=P[15], spare_used=P[15]) == _plan(freed_phys=ctypes.c_void_p(P[15].value + 4 * 31), spare_used=P[15]) == pe.PE_ERR_INVALID_ARG
 
 
 def test_the_prune_s_answer_and_lengths_are_apart():
