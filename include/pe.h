@@ -470,6 +470,10 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
  *     spare_used, freed_phys: [S][Hk] (shared: [S]), in/out: 0 (where n_spare > 0) and -1 in the rows of sequences that begin, whose place an
  *     earlier sequence may have had: what pe_append_kv counts from is then the new list, and a page that was freed is no longer linked.
  *     Without them the caller sees to it.
+ *     copies: caches of this shape, lengths and new tokens (a model's layers) that get their pages out of the list one call after the other,
+ *     this one first (0: as 1): a sequence is served only if the list holds its pages for all of them.
+ *     only: [S], in: sequences with 0 are left as they were.  In the calls for the other copies, the first one's admitted: a sequence is then
+ *     served in all copies or in none.
  * pe_prefill_prune_admitted: pe_prefill_prune of the sequences that begin, by that array (NULL: of all).  Of every other sequence neither pages nor
  *     seq_lens_out nor kept_idx_out is written, whatever tokens cu_seqlens has of it: running ones, and those that were left as they were.
  *     admitted must not overlap seq_lens_out.
@@ -478,6 +482,8 @@ typedef struct pe_plan_opts {
   int32_t* admitted;
   int32_t* spare_used;
   int32_t* freed_phys;
+  const int32_t* only;
+  int32_t copies;
 } pe_plan_opts;
 int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const int32_t* seq_lens, const int32_t* new_lens,
                       const int32_t* first_positions, int64_t total_tokens, int32_t budget_tokens, const int32_t* free_pages, int32_t num_free,

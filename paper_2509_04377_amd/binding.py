@@ -57,7 +57,8 @@ class pe_rope(ctypes.Structure):
 
 
 class pe_plan_opts(ctypes.Structure):
-    _fields_ = [("admitted", ctypes.c_void_p), ("spare_used", ctypes.c_void_p), ("freed_phys", ctypes.c_void_p)]
+    _fields_ = [("admitted", ctypes.c_void_p), ("spare_used", ctypes.c_void_p), ("freed_phys", ctypes.c_void_p),
+                ("only", ctypes.c_void_p), ("copies", ctypes.c_int32)]
 
 
 class pe_quant_cache(ctypes.Structure):
@@ -520,11 +521,11 @@ def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, soft
 
 def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used, block_table, spare,
                    seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, admitted=None,
-                   spare_used=None, freed_phys=None):
+                   spare_used=None, freed_phys=None, only=None, copies=1):
     """With an argument behind slots_out: pe_plan_tokens_ex."""
     L = lib()
-    opts = (admitted, spare_used, freed_phys)
-    if all(o is None for o in opts):
+    opts = (admitted, spare_used, freed_phys, only, copies)
+    if all(o is None for o in opts[:4]) and copies == 1:
         status = _host.plan_tokens(L.addr_plan_tokens, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages,
                                    free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out)
     else:
@@ -532,7 +533,8 @@ def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budg
                                       free_pages, free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out,
                                       slots_out)
     if status is None:
-        o = pe_plan_opts(*(_addr_opt(x, name, torch.int32) for x, name in zip(opts, ("admitted", "spare_used", "freed_phys"))))
+        o = pe_plan_opts(*(_addr_opt(x, name, torch.int32) for x, name in zip(opts[:4], ("admitted", "spare_used", "freed_phys", "only"))),
+                         int(copies))
         status = L.pe_plan_tokens_ex(ctypes.byref(desc), ctypes.byref(o), _addr(seq_lens, "seq_lens", torch.int32),
                                      _addr(new_lens, "new_lens", torch.int32),
                                      _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),

@@ -38,11 +38,12 @@ int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const
   if (budget_tokens % desc->block_size != 0) return PE_ERR_INVALID_ARG;
   if (!aligned(slots_out, 8)) return PE_ERR_INVALID_ARG;
   const pe_plan_opts o = opts != nullptr ? *opts : pe_plan_opts{};
+  if (o.copies < 0) return PE_ERR_INVALID_ARG;
   const bool shared = desc->layout == PE_LAYOUT_SHARED;
   const size_t S = (size_t)desc->num_seqs, per_seq = shared ? 1 : (size_t)desc->num_kv_heads;
   if (desc->num_kv_heads > 65536 || (int64_t)per_seq * ((int64_t)desc->max_blocks + n_spare) > 0x7fffffffLL) return PE_ERR_UNSUPPORTED;
   const struct { const void* p; size_t bytes; } in[] = {{seq_lens, S * 4}, {new_lens, S * 4}, {first_positions, S * 4},
-                                                        {free_pages, (size_t)num_free * 4}, {free_used, 4}},
+                                                        {free_pages, (size_t)num_free * 4}, {free_used, 4}, {o.only, S * 4}},
       out[] = {{block_table, S * per_seq * desc->max_blocks * 4}, {spare, S * per_seq * n_spare * 4}, {seq_lens_out, S * 4}, {free_used_out, 4},
                {cu_seqlens_out, (S + 1) * 4}, {positions_out, (size_t)total_tokens * 4}, {slots_out, (size_t)total_tokens * per_seq * 8}, {o.admitted, S * 4},
                {o.spare_used, S * per_seq * 4}, {o.freed_phys, S * per_seq * 4}};
@@ -69,6 +70,8 @@ int pe_plan_tokens_ex(const pe_cache_desc* desc, const pe_plan_opts* opts, const
   a.admitted = o.admitted;
   a.spare_used = n_spare > 0 ? o.spare_used : nullptr;
   a.freed_phys = o.freed_phys;
+  a.only = o.only;
+  a.copies = o.copies > 1 ? o.copies : 1;
   a.total_tokens = total_tokens;
   a.num_free = num_free;
   a.n_spare = n_spare;

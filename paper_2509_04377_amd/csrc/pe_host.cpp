@@ -190,17 +190,20 @@ struct QuantCache {
   bool get(PyObject* o) { return structure(o, quant_cache_type, &cache); }
 };
 
-struct PlanOpts {  // (admitted, spare_used, freed_phys)
+struct PlanOpts {  // (admitted, spare_used, freed_phys, only, copies)
   pe_plan_opts o{};
   std::tuple<const pe_plan_opts*> c{&o};
   bool get(PyObject* t) {
-    IntsOrNone admitted, spare_used, freed_phys;
-    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 3 || !admitted.get(PyTuple_GET_ITEM(t, 0)) || !spare_used.get(PyTuple_GET_ITEM(t, 1)) ||
-        !freed_phys.get(PyTuple_GET_ITEM(t, 2)))
+    IntsOrNone admitted, spare_used, freed_phys, only;
+    Number<int32_t> copies;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 5 || !admitted.get(PyTuple_GET_ITEM(t, 0)) || !spare_used.get(PyTuple_GET_ITEM(t, 1)) ||
+        !freed_phys.get(PyTuple_GET_ITEM(t, 2)) || !only.get(PyTuple_GET_ITEM(t, 3)) || !copies.get(PyTuple_GET_ITEM(t, 4)))
       return false;
     o.admitted = std::get<0>(admitted.c);
     o.spare_used = std::get<0>(spare_used.c);
     o.freed_phys = std::get<0>(freed_phys.c);
+    o.only = std::get<0>(only.c);
+    o.copies = std::get<0>(copies.c);
     return true;
   }
 };

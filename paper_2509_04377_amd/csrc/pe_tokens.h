@@ -25,8 +25,9 @@ struct PlanArgs {
   int32_t* admitted;       // may be null
   int32_t* spare_used;     // may be null
   int32_t* freed_phys;     // may be null
+  const int32_t* only;     // may be null
   int64_t total_tokens;
-  int num_free, n_spare, budget, num_seqs, rows_per_seq, block_size, max_blocks;
+  int num_free, n_spare, budget, num_seqs, rows_per_seq, block_size, max_blocks, copies;
 };
 constexpr int kPlanThreads = 256;
 hipError_t launch_plan_tokens(const PlanArgs& a, int compute_units, hipStream_t stream);

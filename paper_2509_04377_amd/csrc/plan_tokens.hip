@@ -63,7 +63,8 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
   const int B = a.block_size, log2_block = __builtin_ctz((unsigned)B), rows = a.rows_per_seq;
   const int64_t given = *free_used;
   const int64_t used = given < 0 ? 0 : given > num_free ? num_free : given;
-  const int64_t left = num_free - used;
+  // (what the list holds; of several copies, what is one's share: the sums ascend, so that a share that holds a sum holds those before it)
+  const int64_t left = a.copies > 1 ? (int64_t)((uint32_t)(num_free - used) / (uint32_t)a.copies) : num_free - used;
   Sums before{0, 0};
   int64_t dealt = 0;
 
@@ -83,6 +84,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
       kept = a.budget > 0 && after > a.budget ? (holds > a.budget ? holds : a.budget) : after;
       const int64_t pages = (kept + B - 1) >> log2_block;
       fits = len >= 0 && pages <= a.max_blocks && kept <= 0x7fffffffLL;
+      if (a.only != nullptr) fits = fits && a.only[s] != 0;
       if (fits) per_row = (int)(pages - have) + (holds == 0 && n > 0 ? a.n_spare : 0);
     }
     const int need = per_row * rows;  // (the host keeps it under 2^31)

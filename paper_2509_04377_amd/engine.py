@@ -104,22 +104,28 @@ class Admits:
         tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
         lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
         set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
-        dev = self.block_table.device
+        return self._admit(new_lens, total_tokens, free, first_positions, plan, whole)
+
+    def _admit(self, new_lens, total_tokens, free, first_positions, plan, whole, only=None, copies=1):
         if plan is None:
-            rows = self.block_table.shape[1:-1]   # (shared: none)
-            plan = Plan(torch.empty(self.desc.num_seqs + 1, dtype=torch.int32, device=dev), torch.empty(total_tokens, dtype=torch.int32, device=dev),
-                        torch.empty((total_tokens,) + tuple(rows), dtype=torch.int64, device=dev))
+            plan = self.new_plan(total_tokens)
         if plan.admitted is None:
-            plan.admitted = torch.empty(self.desc.num_seqs, dtype=torch.int32, device=dev)
+            plan.admitted = torch.empty(self.desc.num_seqs, dtype=torch.int32, device=self.block_table.device)
         if self.seq_lens_alt is None:
             self.seq_lens_alt = torch.empty_like(self.seq_lens)
         _launch(pe.pe_plan_tokens, self.desc, self.seq_lens, new_lens, first_positions, int(total_tokens), 0 if whole else self.budget, free.pages, free.used,
                 self.block_table, self.spare, self.seq_lens_alt, free.used_alt, plan.cu_seqlens, plan.positions, plan.slots, plan.admitted,
-                self.spare_used, self.freed_phys)
+                self.spare_used, self.freed_phys, only, copies)
         self.admitted = plan.admitted
         self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
         free.used, free.used_alt = free.used_alt, free.used
         return plan
+
+    def new_plan(self, total_tokens):
+        """Room for the plan of so many tokens."""
+        i32, rows = dict(dtype=torch.int32, device=self.block_table.device), tuple(self.block_table.shape[1:-1])   # (shared: none)
+        return Plan(torch.empty(self.desc.num_seqs + 1, **i32), torch.empty(total_tokens, **i32),
+                    torch.empty((total_tokens,) + rows, dtype=torch.int64, device=i32["device"]), torch.empty(self.desc.num_seqs, **i32))
 
     def rotate(self, rope, positions, q, k, q_out, k_out, transpose=False):
         """Rotary positions of q [T, Hq, D] and k [T, Hk, D]; in place or apart, tokens any stride apart."""
@@ -481,9 +487,17 @@ class LayeredAdmits:
     """admit() for a driver of several layers."""
 
     def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, whole=False):
-        """The caches' admit() in every layer, one after the other out of one list of pages: a plan for each."""
-        plans = [c.admit(new_lens, total_tokens, free, first_positions, whole=whole) for c in self.per_layer]
-        f = self.folded   # (each layer has swapped its part of the lengths)
+        """The caches' admit() in every layer, one after the other out of one list of pages: a plan for each.  A sequence is served in all
+        layers or, where the list does not hold its pages for all of them, in none."""
+        f, plans = self.folded, []
+        admitted = torch.empty((self.layers, self.S), dtype=torch.int32, device=f.block_table.device)
+        for l, c in enumerate(self.per_layer):
+            plan = c.new_plan(total_tokens)
+            plan.admitted = admitted[l]
+            plans.append(c._admit(new_lens, total_tokens, free, first_positions, plan, whole, None if l == 0 else admitted[0],
+                                  self.layers if l == 0 else 1))
+        f.admitted = admitted.view(-1)
+        # (each layer has swapped its part of the lengths)
         f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens
         return plans
 

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2509_04377_amd import binding as pe
-from paper_2509_04377_amd.engine import FreePages, PagedCache, QuantCache, empty_layout
+from paper_2509_04377_amd.engine import FreePages, LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -51,8 +51,8 @@ class _Call:
         torch.cuda.synchronize()
         return [t.tolist() for t in out] + [slots.tolist(), table.tolist(), None if spare is None else spare.tolist()]
 
-    def served(self):
-        return _served(self.lens, self.new, self.budget, self.left, self.rows, self.n_spare, self.width, self.B)
+    def served(self, copies=1):
+        return _served(self.lens, self.new, self.budget, self.left // copies, self.rows, self.n_spare, self.width, self.B)
 
 
 CASES = [
@@ -82,6 +82,53 @@ def test_rows_that_begin_forget_the_sequence_before(case, given):
     for name, t in opts.items():
         new = 5 if name == "spare_used" and not c.n_spare else 0 if name == "spare_used" else -1
         assert t.tolist() == [[new if a == 1 else 5] * rows for a in c.served()], name
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("copies", [1, 2, 5])
+def test_copies_serve_a_sequence_all_or_none(case, copies):
+    c = _Call(**case)
+    S, served, dealt = len(c.lens), c.served(copies), set()
+    assert copies == 1 or "left" not in case or served != c.served()   # (the list ends on the way)
+    first = torch.full((S,), -9, dtype=torch.int32, device=DEV)
+    for i in range(copies):
+        admitted = first if i == 0 else torch.full((S,), -9, dtype=torch.int32, device=DEV)
+        lens_out, used, _, _, slots, table, spare = c.run(admitted=admitted, only=None if i == 0 else first, copies=copies if i == 0 else 1)
+        assert admitted.tolist() == served, i
+        for s, a in enumerate(served):
+            assert a or lens_out[s] == c.lens[s]
+        # what was dealt: new entries of the tables, and spare pages
+        new = torch.tensor(table)[torch.tensor(table) != c.table.cpu()].tolist() + ([p for x in spare for r in x for p in r if p >= 0] if spare else [])
+        # (the table began with numbers of its own: an entry may have got the one it had)
+        taken = set(c.free[int(c.used):used[0]].tolist())
+        assert set(new) <= taken and not taken & dealt and len(taken) == used[0] - int(c.used)
+        dealt |= taken
+        c.used.fill_(used[0])
+
+
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_list_that_ends_in_a_later_layer(quant, shared):
+    """Layers agree on who was admitted, and steps go on with what they have."""
+    layers, S, Hk, G, D, B, budget, n_spare, width = 3, 3, 2, 2, 64, 16, 64, 2, 4
+    R, rows = layers * S, 1 if shared else Hk
+    need = rows * (width + n_spare)                    # of a sequence and layer
+    P = layers * need + 2 * need - 1                   # the first sequence in all layers, the second in one of them and almost a second
+    make = LayeredQuantCache if quant else LayeredCache
+    m = make(torch.bfloat16, layers, S, Hk, Hk * G, D, B, empty_layout(R, Hk, width, n_spare, P, DEV, shared), budget, shared=shared)
+    free = FreePages.of(torch.randperm(P, generator=torch.Generator().manual_seed(6)).int().to(DEV))
+    plans = m.admit(_i32([100, 70, 0]), 170, free)
+    assert [p.admitted.tolist() for p in plans] == [[1, 0, 0]] * layers and m.folded.admitted.tolist() == [1, 0, 0] * layers
+    assert m.folded.seq_lens.tolist() == [64, 0, 0] * layers and int(free.used) == layers * need
+    table = m.folded.block_table.view(layers, S, rows, width)
+    assert bool((table[:, 0] >= 0).all()) and bool((table[:, 1:] == -1).all())
+    for l, c in enumerate(m.per_layer):
+        assert c.seq_lens.tolist() == [64, 0, 0] and c.seq_lens.data_ptr() == m.folded.seq_lens[l * S:].data_ptr()
+    left = 2 * need - 1
+    assert 3 * layers * rows <= left < 4 * layers * rows
+    assert [p.admitted.tolist() for p in m.admit(_i32([0, 17, 1]), 18, free)] == [[0, 0, 0]] * layers   # 2 + 2 pages a row: not for all layers
+    assert [p.admitted.tolist() for p in m.admit(_i32([0, 0, 16]), 16, free)] == [[0, 0, 1]] * layers   # 1 + 2
+    assert m.folded.seq_lens.tolist() == [64, 0, 16] * layers
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "quant"])

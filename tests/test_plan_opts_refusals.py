@@ -32,6 +32,13 @@ def test_what_is_written_lies_by_itself(out, other):
     assert _plan(admitted=P[15], spare_used=P[15]) == _plan(freed_phys=ctypes.c_void_p(P[15].value + 4 * 31), spare_used=P[15]) == pe.PE_ERR_INVALID_ARG
 
 
+def test_options():
+    assert _plan(copies=-1) == pe.PE_ERR_INVALID_ARG
+    for out in ("lens_out", "table", "spare", "cu", "pos", "slots", "used_out"):
+        assert _plan(only=AT[out]) == pe.PE_ERR_INVALID_ARG, out
+    assert _plan(only=P[15], admitted=P[15]) == _plan(only=P[15], spare_used=P[15]) == _plan(only=P[15], freed_phys=P[15]) == pe.PE_ERR_INVALID_ARG
+
+
 def test_the_prune_s_answer_and_lengths_are_apart():
     for shared in (pe.PE_LAYOUT_PER_HEAD, pe.PE_LAYOUT_SHARED):
         d = _desc(layout=shared)
