@@ -62,6 +62,14 @@ def evicts_within(n, tokens, block_size: int, budget: int) -> bool:
     return tokens > full - n
 
 
+def told_lens(prompt_lens, before, num_seqs, budget, whole) -> List[int]:
+    """The lengths that a host mirror is told: see set_host_lens."""
+    if len(prompt_lens) != num_seqs:
+        raise ValueError("prompt_lens: one length per sequence, %d, got %d" % (num_seqs, len(prompt_lens)))
+    before = before or [0] * num_seqs
+    return [n if L is None else int(L) if whole else min(int(L), budget) for L, n in zip(prompt_lens, before)]
+
+
 @dataclass
 class FreePages:
     """The pages that no sequence has yet, on the device: pages[used:] are free.  One list serves all caches of a pool."""
@@ -126,6 +134,21 @@ class Admits:
         i32, rows = dict(dtype=torch.int32, device=self.block_table.device), tuple(self.block_table.shape[1:-1])   # (shared: none)
         return Plan(torch.empty(self.desc.num_seqs + 1, **i32), torch.empty(total_tokens, **i32),
                     torch.empty((total_tokens,) + rows, dtype=torch.int64, device=i32["device"]), torch.empty(self.desc.num_seqs, **i32))
+
+    def set_host_lens(self, prompt_lens, whole=False):
+        """Tell the host mirror what was given: of a prompt that was pruned min(L, C) tokens are held, whole=True: L; None: that sequence is what
+        it was (it runs on, or admit() left it).  What else the host has counted begins anew; the attention that pages got stays with the
+        sequences of None."""
+        self.host_lens = told_lens(prompt_lens, self.host_lens, self.desc.num_seqs, self.budget, whole)
+        self.host_scored = None
+        if self.selection is not None:
+            self.selection.seen = None
+        if self.attention is not None:
+            if any(L is None for L in prompt_lens):
+                if self.attention.started:
+                    self.scores[[s for s, L in enumerate(prompt_lens) if L is not None]] = float("inf")   # (nothing before)
+            else:
+                self.attention.started = False
 
     def rotate(self, rope, positions, q, k, q_out, k_out, transpose=False):
         """Rotary positions of q [T, Hq, D] and k [T, Hk, D]; in place or apart, tokens any stride apart."""
@@ -208,14 +231,6 @@ class PagedCache(Admits):
     def rotate_store(self, rope, plan: Plan, q, k, v, q_out, k_out=None):
         """rotate(), and the turned keys and the values into the pages that admit() planned for them (prompts that are kept whole)."""
         _launch(pe.pe_rotate, self.desc, rope, False, plan.positions, q, k, v, q_out, k_out, plan.slots, self.k_pool, self.v_pool)
-
-    def set_host_lens(self, prompt_lens):
-        """Tell the host mirror what the prune was given: cached length = min(L, C)."""
-        self.host_lens = [min(int(L), self.budget) for L in prompt_lens]
-        if self.selection is not None:
-            self.selection.seen = None
-        if self.attention is not None:
-            self.attention.started = False
 
     def triggers(self) -> List[bool]:
         return triggers(self.host_lens, self.desc.block_size, self.budget)
@@ -484,7 +499,15 @@ class Attention:
 
 
 class LayeredAdmits:
-    """admit() for a driver of several layers."""
+    """admit() and set_host_lens() for a driver of several layers."""
+
+    def set_host_lens(self, prompt_lens, whole=False):
+        """The caches' set_host_lens(): the same lengths in every layer."""
+        now, f = told_lens(prompt_lens, self.host_lens, self.S, self.budget, whole), self.folded
+        for c, times in [(f, self.layers)] + [(c, 1) for c in self.per_layer]:
+            c.host_lens = self.host_lens * times
+            c.set_host_lens(list(prompt_lens) * times, whole)
+        self.host_lens = now
 
     def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, whole=False):
         """The caches' admit() in every layer, one after the other out of one list of pages: a plan for each.  A sequence is served in all
@@ -535,11 +558,6 @@ class LayeredCache(LayeredAdmits):
 
     def prefill_prune_layer(self, layer, k_in, v_in, cu_seqlens, max_seqlen, kept_idx_out=None, workspace=None):
         self.per_layer[layer].prefill_prune(k_in, v_in, cu_seqlens, max_seqlen, kept_idx_out, workspace)
-
-    def set_host_lens(self, prompt_lens):
-        self.host_lens = [min(int(L), self.budget) for L in prompt_lens]
-        for c in [self.folded] + self.per_layer:
-            c.set_host_lens(list(prompt_lens) * (self.layers if c is self.folded else 1))
 
     def _triggers(self):
         return triggers(self.host_lens, self.B, self.budget)

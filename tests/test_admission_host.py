@@ -1,0 +1,88 @@
+"""The host's part of admissions: its mirror of the lengths behind prompts that are pruned or kept whole, beside sequences that run on
+(no GPU: the launches are off)."""
+import pytest
+import torch
+
+from paper_2509_04377_amd.engine import LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout, host_only
+
+S, Hk, Hq, D, B, BUDGET, WIDTH = 3, 2, 4, 64, 16, 64, 12
+
+
+@pytest.fixture(autouse=True)
+def no_gpu_memory(monkeypatch):
+    """Workspaces and tensors on the CPU, whose addresses no call will see."""
+    from paper_2509_04377_amd import binding as pe
+    monkeypatch.setattr(pe, "_addr", lambda t, name, dtype=None: t.data_ptr())
+    monkeypatch.setattr(pe, "alloc_workspace", lambda *a, **kw: torch.empty(0))
+
+
+def _make(kind, num_seqs=S):
+    cls = dict(paged=PagedCache, quant=QuantCache, layers=LayeredCache, quant_layers=LayeredQuantCache)[kind]
+    layers = (2,) if "layers" in kind else ()
+    rows = num_seqs * (layers[0] if layers else 1)
+    args = (torch.float32,) + layers + (num_seqs, Hk, Hq, D, B, empty_layout(rows, Hk, WIDTH, 2, 64, "cpu"), BUDGET)
+    return cls(*args, device="cpu") if layers else cls.create(*args, device="cpu")
+
+
+KINDS = ["paged", "quant", "layers", "quant_layers"]
+
+
+def _mirrors(c):
+    return [c.host_lens] + ([c.folded.host_lens[i:i + S] for i in (0, S)] if hasattr(c, "folded") else [])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_lengths_that_are_told(kind):
+    c = _make(kind)
+    for lens, whole, want in (([100, 64, 3], False, [64, 64, 3]), ([100, None, 0], True, [100, 64, 0]), ([None, 70, None], False, [100, 64, 0]),
+                              ([None, 0, None], True, [100, 0, 0])):
+        c.set_host_lens(lens, whole)
+        assert all(m == want for m in _mirrors(c)), (lens, whole)
+    for lens in ([1, 2], [1, 2, 3, 4]):
+        with pytest.raises(ValueError, match="one length per sequence"):
+            c.set_host_lens(lens)
+    assert c.host_lens == [100, 0, 0]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_steps_go_on_from_what_was_told(kind):
+    """A prompt kept whole beyond the budget loses a page where it has filled one, as the device counts."""
+    c = _make(kind)
+    c.set_host_lens([100, 64, 3], whole=True)
+    want = [100, 64, 3]
+    shape = (2, S) if "layers" in kind else (S,)
+    new, q = torch.zeros(shape + (Hk, D)), torch.zeros(shape + (Hq, D))
+    with host_only():
+        for step in range(40):
+            want = [n - B if n > 0 and n % B == 0 and n >= BUDGET else n for n in want]
+            c.decode_step(new, new, q, torch.zeros_like(q))
+            want = [n + 1 for n in want]
+            if step == 20:
+                c.set_host_lens([None, 7, None])
+                want[1] = 7
+            assert c.host_lens == want, step
+
+
+@pytest.mark.parametrize("kind", ["paged", "layers"])
+def test_what_was_counted_of_a_place_is_forgotten(kind):
+    c = _make(kind)
+    f = c.folded if kind == "layers" else c
+    f.host_scored = [4] * f.desc.num_seqs
+    c.set_host_lens([None, 9, None])
+    assert f.host_scored is None   # (the pages that a cached score is of are another sequence's)
+
+
+@pytest.mark.parametrize("kind", ["paged", "layers"])
+def test_attention_stays_with_sequences_that_run_on(kind):
+    c = _make(kind)
+    c.evict_by_attention()
+    caches = [c.folded] + c.per_layer if kind == "layers" else [c]
+    for x in caches:
+        x.attention.started = True
+        x.scores.fill_(2.0)
+    c.set_host_lens([None, 9, None])
+    for x in caches:
+        rows = x.scores.view(-1, S, Hk, WIDTH)
+        assert x.attention.started and bool((rows[:, [0, 2]] == 2.0).all()) and bool(torch.isinf(rows[:, 1]).all())
+    c.set_host_lens([5, 9, 1])
+    assert not any(x.attention.started for x in caches)
