@@ -558,6 +558,9 @@ int pe_rotate(const pe_cache_desc* desc, const pe_rope* rope, int32_t transpose,
  * fp32 number, as sums may be taken in another order), +INF behind them.  Entries of -1 are passed over.  The pools of `cache` and k_pool, v_pool must
  * not overlap.
  *
+ * pe_quant_pages_admitted: the same for the sequences that a plan (8) let begin or go on, admitted[s] != 0 (NULL: for all).  Of the others
+ * nothing is written, no score either.  admitted must not overlap what is written.
+ *
  * pe_quant_append: a decode step's new token of every sequence, as pe_append_kv but that it goes to slot seq_lens[s] % B of the row's tail; where
  * that fills the page, the page is rounded into page seq_lens[s] / B of the row and, with scores not NULL, its score is written to
  * scores[s][hk][seq_lens[s] / B].  A new page is linked (slot 0) as in pe_append_kv.  seq_lens is only read; seq_lens_out must not overlap
@@ -575,6 +578,9 @@ typedef struct pe_quant_cache {
 } pe_quant_cache;
 int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* k_pool, const void* v_pool,
                    const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table, float* scores_out, void* stream);
+int pe_quant_pages_admitted(const pe_cache_desc* desc, const pe_quant_cache* cache, const int32_t* admitted, const void* k_pool,
+                            const void* v_pool, const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table,
+                            float* scores_out, void* stream);
 int pe_quant_append(const pe_cache_desc* desc, const pe_quant_cache* cache, const pe_rope* rope, const int32_t* positions, const void* q,
                     void* q_out, const void* new_k, const void* new_v, int32_t* block_table, const int32_t* seq_lens,
                     int32_t* seq_lens_out, int32_t* freed_phys, const int32_t* spare, int32_t* spare_used, int32_t n_spare,

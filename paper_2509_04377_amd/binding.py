@@ -33,7 +33,7 @@ EXPORTS = ["pe_workspace_bytes", "pe_status_string", "pe_version", "pe_decode_sp
            "pe_append_paged_decode", "pe_score_recent_blocks", "pe_evict_blocks_cached", "pe_evict_blocks_ex", "pe_score_evict",
            "pe_score_triggered_blocks", "pe_paged_decode_static", "pe_append_paged_decode_layers",
            "pe_tree_decode", "pe_append_path", "pe_page_bounds", "pe_select_pages",
-           "pe_paged_decode_weights", "pe_plan_tokens", "pe_plan_tokens_ex", "pe_prefill_prune_admitted", "pe_rope_init", "pe_rotate",
+           "pe_paged_decode_weights", "pe_plan_tokens", "pe_plan_tokens_ex", "pe_prefill_prune_admitted", "pe_quant_pages_admitted", "pe_rope_init", "pe_rotate",
            "pe_quant_pages", "pe_quant_append", "pe_quant_decode"]
 
 
@@ -184,6 +184,8 @@ def lib():
         L.pe_rotate.argtypes = [dp, rp, i32, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
         L.pe_quant_pages.restype = ctypes.c_int
         L.pe_quant_pages.argtypes = [dp, cp, vp, vp, vp, vp, vp, vp, vp]
+        L.pe_quant_pages_admitted.restype = ctypes.c_int
+        L.pe_quant_pages_admitted.argtypes = [dp, cp, vp] + L.pe_quant_pages.argtypes[2:]
         L.pe_quant_append.restype = ctypes.c_int
         L.pe_quant_append.argtypes = [dp, cp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
         L.pe_quant_decode.restype = ctypes.c_int
@@ -192,7 +194,7 @@ def lib():
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
                      "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens", "plan_tokens_ex", "prefill_prune_admitted", "rotate",
-                     "quant_pages", "quant_append", "quant_decode"):
+                     "quant_pages", "quant_pages_admitted", "quant_append", "quant_decode"):
             setattr(L, "addr_" + name, ctypes.cast(getattr(L, "pe_" + name), vp).value)
         _lib = L
     return _lib
@@ -613,14 +615,20 @@ def make_quant_cache(desc, k, v, scales, k_tail, v_tail):
     return cache
 
 
-def pe_quant_pages(desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out=None):
+def pe_quant_pages(desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out=None, admitted=None):
+    """admitted: only the sequences that a plan of tokens let begin or go on (pe_quant_pages_admitted)."""
     L = lib()
-    status = _host.quant_pages(L.addr_quant_pages, desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out)
+    if admitted is None:
+        status = _host.quant_pages(L.addr_quant_pages, desc, cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out)
+    else:
+        status = _host.quant_pages_admitted(L.addr_quant_pages_admitted, desc, cache, admitted, k_pool, v_pool, src_table, seq_lens, block_table,
+                                            scores_out)
     if status is None:
-        status = L.pe_quant_pages(ctypes.byref(desc), ctypes.byref(cache), _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
-                                  _addr(src_table, "src_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
-                                  _addr(block_table, "block_table", torch.int32), _addr_opt(scores_out, "scores_out", torch.float32),
-                                  _stream())
+        status = L.pe_quant_pages_admitted(ctypes.byref(desc), ctypes.byref(cache), _addr_opt(admitted, "admitted", torch.int32),
+                                           _addr(k_pool, "k_pool"), _addr(v_pool, "v_pool"),
+                                           _addr(src_table, "src_table", torch.int32), _addr(seq_lens, "seq_lens", torch.int32),
+                                           _addr(block_table, "block_table", torch.int32), _addr_opt(scores_out, "scores_out", torch.float32),
+                                           _stream())
     check(status, "pe_quant_pages")
 
 

@@ -39,6 +39,12 @@ extern "C" {
 
 int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const void* k_pool, const void* v_pool,
                    const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table, float* scores_out, void* stream) {
+  return pe_quant_pages_admitted(desc, cache, nullptr, k_pool, v_pool, src_table, seq_lens, block_table, scores_out, stream);
+}
+
+int pe_quant_pages_admitted(const pe_cache_desc* desc, const pe_quant_cache* cache, const int32_t* admitted, const void* k_pool,
+                            const void* v_pool, const int32_t* src_table, const int32_t* seq_lens, const int32_t* block_table,
+                            float* scores_out, void* stream) {
   Parts parts;
   int st = check_desc(desc);
   if (st == PE_OK) st = check_cache(desc, cache, &parts);
@@ -47,6 +53,10 @@ int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(scores_out, 4)) return PE_ERR_INVALID_ARG;
   const size_t page = (size_t)desc->block_size * desc->head_dim * (desc->dtype == PE_F32 ? 4 : 2);  // (how many there are is not known)
   if (parts.meet(k_pool, page) || parts.meet(v_pool, page)) return PE_ERR_INVALID_ARG;
+  const size_t scored = (size_t)desc->num_seqs * desc->num_kv_heads * desc->max_blocks * 4;
+  if (admitted != nullptr && (parts.meet(admitted, (size_t)desc->num_seqs * 4) ||
+                              (scores_out != nullptr && overlap(admitted, (size_t)desc->num_seqs * 4, scores_out, scored))))
+    return PE_ERR_INVALID_ARG;
   if (desc->num_kv_heads > 65536 || !pe::quant_pages_launches(desc)) return PE_ERR_UNSUPPORTED;
   pe::QuantPagesArgs a;
   a.cache = *cache;
@@ -55,6 +65,7 @@ int pe_quant_pages(const pe_cache_desc* desc, const pe_quant_cache* cache, const
   a.src_table = src_table;
   a.seq_lens = seq_lens;
   a.block_table = block_table;
+  a.admitted = admitted;
   a.scores = scores_out;
   a.num_seqs = desc->num_seqs;
   a.num_kv_heads = desc->num_kv_heads;

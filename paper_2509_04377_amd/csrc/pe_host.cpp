@@ -430,6 +430,8 @@ PyMethodDef methods[] = {
     method<rotate>("rotate"),
     // cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out
     method<call<decltype(&pe_quant_pages), QuantCache, Tensor, Tensor, Ints, Ints, Ints, FloatsOrNone>>("quant_pages"),
+    // cache, admitted, and the same
+    method<call<decltype(&pe_quant_pages_admitted), QuantCache, Ints, Tensor, Tensor, Ints, Ints, Ints, FloatsOrNone>>("quant_pages_admitted"),
     // cache, rope, positions, q, q_out, new_k, new_v, block_table, seq_lens, seq_lens_out, freed_phys, spare, spare_used, spare, scores
     method<call<decltype(&pe_quant_append), QuantCache, RopeOrNone, IntsOrNone, TensorOrNone, TensorOrNone, Tensor, Tensor, Ints, Ints, Ints,
                 Ints, Ints, Ints, LastDim, FloatsOrNone>>("quant_append"),

@@ -22,6 +22,7 @@ struct QuantPagesArgs {
   float* scores;  // may be null
   int num_seqs, num_kv_heads, head_dim, block_size, max_blocks;
   bool is_bf16, shared;
+  const int32_t* admitted;  // may be null
 };
 // false: a launch that the runtime does not take
 bool quant_pages_launches(const pe_cache_desc* d);

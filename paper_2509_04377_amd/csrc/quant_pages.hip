@@ -144,6 +144,7 @@ __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_pages
   const int row = (int)(blockIdx.x / (unsigned)groups_per_row), s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
   const int j = (int)(blockIdx.x - (unsigned)row * (unsigned)groups_per_row) * kPages + slot;
   const int len = a.seq_lens[s];
+  if (a.admitted != nullptr && a.admitted[s] == 0) return;  // (the workgroup has no other row)
   const int most = len < 0 ? 0 : len / B, full = most < a.max_blocks ? most : a.max_blocks;
   const int64_t table_row = (int64_t)(a.shared ? s : row) * a.max_blocks;
   const int heads = a.shared ? a.num_kv_heads : 1;          // token rows between a head's consecutive tokens

@@ -696,11 +696,14 @@ class QuantCache(Admits):
 
     def take(self, paged: PagedCache):
         """The tokens of an unrounded cache of the same shape (behind its prefill_prune, say) become this one's: its full pages are rounded
-        into the pages of this table, which has as many, and scored; the rest goes to the tail."""
-        _launch(pe.pe_quant_pages, self.desc, self.cache, paged.k_pool, paged.v_pool, paged.block_table, paged.seq_lens, self.block_table, self.scores)
+        into the pages of this table, which has as many, and scored; the rest goes to the tail.  Behind admit() those of the sequences that it
+        let begin or go on here: the others stay as they are.  The mirror takes the other cache's numbers, and keeps its own where those are 0; it is
+        to be told (there or here) of a sequence that was left here and not there."""
+        _launch(pe.pe_quant_pages, self.desc, self.cache, paged.k_pool, paged.v_pool, paged.block_table, paged.seq_lens, self.block_table, self.scores,
+                self.admitted)
         if not HostOnly.active:
-            self.seq_lens.copy_(paged.seq_lens)
-        self.host_lens = list(paged.host_lens)
+            self.seq_lens.copy_(paged.seq_lens if self.admitted is None else torch.where(self.admitted != 0, paged.seq_lens, self.seq_lens))
+        self.host_lens = [n if n or self.admitted is None else mine for n, mine in zip(paged.host_lens, self.host_lens)]
 
     def triggers(self) -> List[bool]:
         return triggers(self.host_lens, self.desc.block_size, self.budget)
@@ -762,8 +765,10 @@ class LayeredQuantCache(LayeredAdmits):
         self.fused = False
 
     def take_layer(self, layer, paged: PagedCache):
-        self.per_layer[layer].take(paged)
-        self.host_lens = list(self.per_layer[layer].host_lens)
+        c = self.per_layer[layer]
+        c.host_lens = list(self.host_lens)
+        c.take(paged)
+        self.host_lens = list(c.host_lens)
 
     def _triggers(self):
         return triggers(self.host_lens, self.B, self.budget)

@@ -46,3 +46,11 @@ def test_the_prune_s_answer_and_lengths_are_apart():
             ctypes.byref(d), P[0], P[1], P[2], admitted, 100, 50, 64, P[3], P[4], P[5], P[6], None, None, 0, None)
         assert call(P[6]) == call(ctypes.c_void_p(P[6].value + 12)) == pe.PE_ERR_INVALID_ARG
         assert call(P[7]) == call(None) == pe.PE_ERR_WORKSPACE      # (the check behind it)
+
+
+def test_the_pages_answer_lies_by_itself():
+    cache = pe.pe_quant_cache(*(p.value for p in P[:5]))
+    call = lambda admitted: pe.lib().pe_quant_pages_admitted(   # noqa: E731
+        ctypes.byref(_desc()), ctypes.byref(cache), admitted, P[5], P[6], P[7], P[8], P[9], P[10], None)
+    for p in P[:5] + [P[10], ctypes.c_void_p(P[10].value - 12)]:
+        assert call(p) == pe.PE_ERR_INVALID_ARG
