@@ -112,6 +112,8 @@ class Admits:
         tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
         lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
         set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
+        if self.part_of_another:
+            raise ValueError("admit() is the whole cache's (all layers'): the lengths that it swaps are")
         return self._admit(new_lens, total_tokens, free, first_positions, plan, whole)
 
     def _admit(self, new_lens, total_tokens, free, first_positions, plan, whole, only=None, copies=1):
@@ -181,6 +183,7 @@ class PagedCache(Admits):
     selection: "Selection" = None  # attend to selected pages only (select_pages)
     attention: "Attention" = None  # `scores` are the attention that pages got (evict_by_attention)
     admitted: torch.Tensor = None  # [S] int32, of the last admit(): prefill_prune() writes its sequences of 1; None: all
+    part_of_another: bool = False  # rows(), or a layer: its arrays of lengths are another cache's to swap
 
     @staticmethod
     def create(dtype, num_seqs, num_kv_heads, num_q_heads, head_dim, block_size, layout, budget, device="cuda",
@@ -405,14 +408,15 @@ class PagedCache(Admits):
             first = end
 
     def rows(self, first, end):
-        """The same cache's sequences first .. end - 1, as a cache (views; host_lens and host_scored are copies)."""
+        """The same cache's sequences first .. end - 1, as a cache (views; host_lens and host_scored are copies): to prune, score and evict
+        in, and to read; admissions and steps, which swap the lengths' arrays, are the whole cache's."""
         d, sl = self.desc, slice(first, end)
         fields = {name: getattr(d, name) for name, _ in d._fields_}
         views = {name: getattr(self, name)[sl] for name in ("block_table", "seq_lens", "spare", "spare_used", "freed_phys",
                                                             "evicted_logical", "scores", "host_lens")}
         views["admitted"] = None if self.admitted is None else self.admitted[sl]
         return replace(self, desc=pe.pe_cache_desc(**{**fields, "num_seqs": end - first}), **views, seq_lens_alt=None, selection=None,
-                       host_scored=None if self.host_scored is None else self.host_scored[sl])
+                       part_of_another=True, host_scored=None if self.host_scored is None else self.host_scored[sl])
 
     # ---- attention over selected pages ----
 
@@ -543,7 +547,7 @@ class LayeredCache(LayeredAdmits):
                                 layout.num_phys_blocks, pe.PE_LAYOUT_SHARED if shared else pe.PE_LAYOUT_PER_HEAD,
                                 **(decode_opts or {}))
             c = PagedCache(desc, f.k_pool, f.v_pool, f.block_table[sl], f.seq_lens[sl], f.spare[sl],
-                              f.spare_used[sl], f.freed_phys[sl], f.evicted_logical[sl], f.scores[sl], int(budget))
+                              f.spare_used[sl], f.freed_phys[sl], f.evicted_logical[sl], f.scores[sl], int(budget), part_of_another=True)
             self.per_layer.append(c)
         # one split workspace serves every layer: launches are ordered on one stream
         self.decode_ws = pe.alloc_workspace(pe.PE_OP_PAGED_DECODE, self.per_layer[0].desc, device=device)
@@ -662,6 +666,7 @@ class QuantCache(Admits):
     workspace: torch.Tensor
     host_lens: list
     admitted: torch.Tensor = None   # of the last admit()
+    part_of_another: bool = False
     rope: pe.pe_rope = None         # turns keys and queries on their way (positions: see decode_step)
     positions: torch.Tensor = None  # [S] int32, of the new token of every sequence: the caller's, changed in place from step to step
     turned: torch.Tensor = None     # [S, Hq, D]: the queries, turned
@@ -690,7 +695,7 @@ class QuantCache(Admits):
                           table.to(device).contiguous(), torch.zeros(num_seqs, **i32), torch.zeros(num_seqs, **i32), spare.to(device).contiguous(),
                           torch.zeros(per_row, **i32), torch.full(per_row, -1, **i32), torch.full(per_row, -1, **i32),
                           torch.full((num_seqs, num_kv_heads, layout.max_blocks), float("inf"), dtype=torch.float32, **on), int(budget),
-                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, None, rope,
+                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, None, False, rope,
                           torch.zeros(num_seqs, **i32) if rope is not None else None,
                           torch.empty((num_seqs, num_q_heads, head_dim), dtype=dtype, **on) if rope is not None else None)
 
@@ -737,13 +742,14 @@ class QuantCache(Admits):
         self.host_lens = [n + 1 for n in self.host_lens]
 
     def rows(self, first, end):
-        """The same cache's sequences first .. end - 1, as a cache (views of the same pages; host_lens is a copy)."""
+        """The same cache's sequences first .. end - 1, as a cache (views of the same pages; host_lens is a copy), as PagedCache.rows: to take
+        prompts and evict in, and to read."""
         d, sl = self.desc, slice(first, end)
         desc = pe.pe_cache_desc(**{**{name: getattr(d, name) for name, _ in d._fields_}, "num_seqs": end - first})
         names = ("k_tail", "v_tail", "block_table", "seq_lens", "seq_lens_alt", "spare", "spare_used", "freed_phys", "evicted_logical", "scores",
                  "host_lens", "positions", "turned", "admitted")
         views = {name: None if getattr(self, name) is None else getattr(self, name)[sl] for name in names}
-        return replace(self, desc=desc, cache=pe.make_quant_cache(desc, self.k, self.v, self.scales, views["k_tail"], views["v_tail"]), **views,
+        return replace(self, desc=desc, part_of_another=True, cache=pe.make_quant_cache(desc, self.k, self.v, self.scales, views["k_tail"], views["v_tail"]), **views,
                        workspace=pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=self.k.device))
 
 

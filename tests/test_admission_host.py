@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-from paper_2509_04377_amd.engine import LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout, host_only
+from paper_2509_04377_amd.engine import FreePages, LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout, host_only
 
 S, Hk, Hq, D, B, BUDGET, WIDTH = 3, 2, 4, 64, 16, 64, 12
 
@@ -86,3 +86,20 @@ def test_attention_stays_with_sequences_that_run_on(kind):
         assert x.attention.started and bool((rows[:, [0, 2]] == 2.0).all()) and bool(torch.isinf(rows[:, 1]).all())
     c.set_host_lens([5, 9, 1])
     assert not any(x.attention.started for x in caches)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_part_of_a_cache_admits_nobody(kind):
+    """Its new lengths would lie in an array that the cache does not read."""
+    c = _make(kind)
+    f = c.folded if "layers" in kind else c
+    free = FreePages.of(torch.arange(8, dtype=torch.int32))
+    before = f.seq_lens.data_ptr()
+    for part in [f.rows(0, 2)] + (c.per_layer if "layers" in kind else []):
+        with pytest.raises(ValueError, match="the whole cache's"):
+            part.admit(torch.ones(part.desc.num_seqs, dtype=torch.int32), 2, free)
+    with host_only():
+        c.admit(torch.ones(S, dtype=torch.int32), S, free)
+    assert f.seq_lens.data_ptr() != before
+    for l, part in enumerate(c.per_layer if "layers" in kind else []):
+        assert part.seq_lens.data_ptr() == f.seq_lens[l * S:].data_ptr() and part.seq_lens_alt.data_ptr() == f.seq_lens_alt[l * S:].data_ptr()
