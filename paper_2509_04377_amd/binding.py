@@ -193,7 +193,7 @@ def lib():
         # addresses of the functions that are called through _pe_host
         for name in ("paged_decode", "append_paged_decode", "append_paged_decode_layers", "prefill_prune",
                      "score_triggered_blocks", "score_recent_blocks", "evict_blocks", "evict_blocks_cached", "evict_blocks_ex",
-                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens", "plan_tokens_ex", "prefill_prune_admitted", "rotate",
+                     "tree_decode", "append_path", "paged_decode_weights", "page_bounds", "select_pages", "plan_tokens_ex", "prefill_prune_admitted", "rotate",
                      "quant_pages", "quant_pages_admitted", "quant_append", "quant_decode"):
             setattr(L, "addr_" + name, ctypes.cast(getattr(L, "pe_" + name), vp).value)
         _lib = L
@@ -521,31 +521,36 @@ def pe_paged_decode_weights(desc, q, k_pool, v_pool, block_table, seq_lens, soft
     check(status, "pe_paged_decode_weights")
 
 
+def _with_room(address, t, name, room):
+    if t.numel() < room:
+        raise ValueError("%s must have room for %d numbers, got %s" % (name, room, tuple(t.shape)))
+    return address
+
+
 def pe_plan_tokens(desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used, block_table, spare,
                    seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, admitted=None,
                    spare_used=None, freed_phys=None, only=None, copies=1):
-    """With an argument behind slots_out: pe_plan_tokens_ex."""
+    """What is behind slots_out: the options of pe_plan_tokens_ex."""
     L = lib()
-    opts = (admitted, spare_used, freed_phys, only, copies)
-    if all(o is None for o in opts[:4]) and copies == 1:
-        status = _host.plan_tokens(L.addr_plan_tokens, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages,
-                                   free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out)
-    else:
-        status = _host.plan_tokens_ex(L.addr_plan_tokens_ex, desc, opts, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages,
-                                      free_pages, free_used, block_table, spare, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out,
-                                      slots_out)
+    status = _host.plan_tokens(L.addr_plan_tokens_ex, desc, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used,
+                               block_table, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, admitted, spare_used,
+                               freed_phys, only, copies)
     if status is None:
-        o = pe_plan_opts(*(_addr_opt(x, name, torch.int32) for x, name in zip(opts[:4], ("admitted", "spare_used", "freed_phys", "only"))),
+        S, T, n_spare = desc.num_seqs, int(total_tokens), 0 if spare is None else int(spare.shape[-1])
+        of_seq = 1 if desc.layout == PE_LAYOUT_SHARED else desc.num_kv_heads
+        rows = S * of_seq
+        i32 = lambda t, name, room: _with_room(_addr(t, name, torch.int32), t, name, room)   # noqa: E731
+        opt = lambda t, name, room: None if t is None else i32(t, name, room)   # noqa: E731
+        o = pe_plan_opts(opt(admitted, "admitted", S), opt(spare_used, "spare_used", rows), opt(freed_phys, "freed_phys", rows), opt(only, "only", S),
                          int(copies))
-        status = L.pe_plan_tokens_ex(ctypes.byref(desc), ctypes.byref(o), _addr(seq_lens, "seq_lens", torch.int32),
-                                     _addr(new_lens, "new_lens", torch.int32),
-                                     _addr_opt(first_positions, "first_positions", torch.int32), int(total_tokens), int(budget_tokens),
-                                     _addr(free_pages, "free_pages", torch.int32), int(free_pages.numel()),
-                                     _addr(free_used, "free_used", torch.int32), _addr(block_table, "block_table", torch.int32),
-                                     _addr_opt(spare, "spare", torch.int32), 0 if spare is None else int(spare.shape[-1]),
-                                     _addr(seq_lens_out, "seq_lens_out", torch.int32), _addr(free_used_out, "free_used_out", torch.int32),
-                                     _addr_opt(cu_seqlens_out, "cu_seqlens_out", torch.int32),
-                                     _addr_opt(positions_out, "positions_out", torch.int32), _addr_opt(slots_out, "slots_out", torch.int64),
+        status = L.pe_plan_tokens_ex(ctypes.byref(desc), ctypes.byref(o), i32(seq_lens, "seq_lens", S), i32(new_lens, "new_lens", S),
+                                     opt(first_positions, "first_positions", S), T, int(budget_tokens), i32(free_pages, "free_pages", 1),
+                                     int(free_pages.numel()), i32(free_used, "free_used", 1), i32(block_table, "block_table", rows * desc.max_blocks),
+                                     opt(spare, "spare", rows * n_spare), n_spare, i32(seq_lens_out, "seq_lens_out", S),
+                                     i32(free_used_out, "free_used_out", 1), opt(cu_seqlens_out, "cu_seqlens_out", S + 1),
+                                     opt(positions_out, "positions_out", T),
+                                     None if slots_out is None else _with_room(_addr(slots_out, "slots_out", torch.int64), slots_out, "slots_out",
+                                                                               T * of_seq),
                                      _stream())
     check(status, "pe_plan_tokens")
 

@@ -190,24 +190,6 @@ struct QuantCache {
   bool get(PyObject* o) { return structure(o, quant_cache_type, &cache); }
 };
 
-struct PlanOpts {  // (admitted, spare_used, freed_phys, only, copies)
-  pe_plan_opts o{};
-  std::tuple<const pe_plan_opts*> c{&o};
-  bool get(PyObject* t) {
-    IntsOrNone admitted, spare_used, freed_phys, only;
-    Number<int32_t> copies;
-    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 5 || !admitted.get(PyTuple_GET_ITEM(t, 0)) || !spare_used.get(PyTuple_GET_ITEM(t, 1)) ||
-        !freed_phys.get(PyTuple_GET_ITEM(t, 2)) || !only.get(PyTuple_GET_ITEM(t, 3)) || !copies.get(PyTuple_GET_ITEM(t, 4)))
-      return false;
-    o.admitted = std::get<0>(admitted.c);
-    o.spare_used = std::get<0>(spare_used.c);
-    o.freed_phys = std::get<0>(freed_phys.c);
-    o.only = std::get<0>(only.c);
-    o.copies = std::get<0>(copies.c);
-    return true;
-  }
-};
-
 template <typename... Args, size_t... I>
 bool get_all(std::tuple<Args...>& a, PyObject* const* o, std::index_sequence<I...>) {
   return (std::get<I>(a).get(o[I]) && ...);
@@ -238,6 +220,55 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
   } catch (const std::exception&) {  // e.g. a tensor without storage
+    Py_RETURN_NONE;
+  }
+}
+
+// args: address of pe_plan_tokens_ex, descriptor, seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_used,
+// block_table, spare, seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out, admitted, spare_used, freed_phys, only, copies
+PyObject* plan_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 21) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return nullptr;
+  }
+  const auto fn = reinterpret_cast<decltype(&pe_plan_tokens_ex)>(PyLong_AsVoidPtr(args[0]));
+  if (fn == nullptr) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no function");
+    return nullptr;
+  }
+  try {
+    Desc desc;
+    Number<int64_t> total;
+    Number<int32_t> budget, copies;
+    Numel num_free;
+    LastDimOrNone n_spare;
+    WordsOrNone slots;
+    if (!desc.get(args[1]) || !total.get(args[5]) || !budget.get(args[6]) || !num_free.get(args[7]) || !n_spare.get(args[10]) ||
+        !slots.get(args[15]) || !copies.get(args[20]))
+      Py_RETURN_NONE;
+    const pe_cache_desc& d = desc.d;
+    const int64_t S = d.num_seqs, of_seq = d.layout == PE_LAYOUT_SHARED ? 1 : d.num_kv_heads, rows = S * of_seq, T = std::get<0>(total.c);
+    const int32_t spare_each = std::get<0>(n_spare.c);
+    // the tensors and how many numbers they have room for
+    const int at[] = {2, 3, 4, 7, 8, 9, 10, 11, 12, 13, 14, 16, 17, 18, 19};
+    const int64_t room[] = {S, S, S, 1, 1, rows * d.max_blocks, rows * spare_each, S, 1, S + 1, T, S, rows, rows, S};
+    constexpr int kTensors = sizeof(at) / sizeof(at[0]);
+    int32_t* p[kTensors];
+    for (int i = 0; i < kTensors; ++i) {
+      IntsOrNone t;
+      if (!t.get(args[at[i]]) || (args[at[i]] != Py_None && THPVariable_Unpack(args[at[i]]).numel() < room[i])) Py_RETURN_NONE;
+      p[i] = std::get<0>(t.c);
+    }
+    if (args[15] != Py_None && THPVariable_Unpack(args[15]).numel() < T * of_seq) Py_RETURN_NONE;
+    const pe_plan_opts opts{p[11], p[12], p[13], p[14], std::get<0>(copies.c)};
+    const auto stream = c10::hip::getCurrentHIPStream().stream();
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn(&d, &opts, p[0], p[1], p[2], T, std::get<0>(budget.c), p[3], std::get<0>(num_free.c), p[4], p[5], p[6], spare_each, p[7], p[8], p[9],
+                p[10], std::get<0>(slots.c), (void*)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+  } catch (const std::exception&) {
     Py_RETURN_NONE;
   }
 }
@@ -420,13 +451,7 @@ PyMethodDef methods[] = {
     method<call<decltype(&pe_page_bounds), Tensor, Ints, Ints, Number<int32_t>, Tensor>>("page_bounds"),
     // q, bounds, block_table, seq_lens, num_pages, block_table_out, seq_lens_out, page_idx_out, workspace
     method<call<decltype(&pe_select_pages), Tensor, Tensor, Ints, Ints, Number<int32_t>, Ints, Ints, IntsOrNone, Workspace>>("select_pages"),
-    // seq_lens, new_lens, first_positions, total_tokens, budget_tokens, free_pages, free_pages, free_used, block_table, spare, spare,
-    // seq_lens_out, free_used_out, cu_seqlens_out, positions_out, slots_out
-    method<call<decltype(&pe_plan_tokens), Ints, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Ints, Numel, Ints, Ints, IntsOrNone,
-                LastDimOrNone, Ints, Ints, IntsOrNone, IntsOrNone, WordsOrNone>>("plan_tokens"),
-    // opts, and the same
-    method<call<decltype(&pe_plan_tokens_ex), PlanOpts, Ints, Ints, IntsOrNone, Number<int64_t>, Number<int32_t>, Ints, Numel, Ints, Ints, IntsOrNone,
-                LastDimOrNone, Ints, Ints, IntsOrNone, IntsOrNone, WordsOrNone>>("plan_tokens_ex"),
+    method<plan_tokens>("plan_tokens"),
     method<rotate>("rotate"),
     // cache, k_pool, v_pool, src_table, seq_lens, block_table, scores_out
     method<call<decltype(&pe_quant_pages), QuantCache, Tensor, Tensor, Ints, Ints, Ints, FloatsOrNone>>("quant_pages"),

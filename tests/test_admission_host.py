@@ -103,3 +103,57 @@ def test_a_part_of_a_cache_admits_nobody(kind):
     assert f.seq_lens.data_ptr() != before
     for l, part in enumerate(c.per_layer if "layers" in kind else []):
         assert part.seq_lens.data_ptr() == f.seq_lens[l * S:].data_ptr() and part.seq_lens_alt.data_ptr() == f.seq_lens_alt[l * S:].data_ptr()
+
+
+class _Took(Exception):
+    pass
+
+
+def _plan_room(**small):
+    """pe_plan_tokens on tensors of the right sizes, but for those that lack one number."""
+    from paper_2509_04377_amd import binding as pe
+    T, R = 7, S * Hk
+    need = dict(seq_lens=S, new_lens=S, first_positions=S, free_pages=9, free_used=1, block_table=R * WIDTH, spare=R * 2, seq_lens_out=S,
+                free_used_out=1, cu_seqlens_out=S + 1, positions_out=T, slots_out=T * Hk, admitted=S, spare_used=R, freed_phys=R, only=S)
+    t = {name: torch.zeros(n - small.get(name, 0), dtype=torch.int64 if name == "slots_out" else torch.int32) for name, n in need.items()}
+    t["spare"] = t["spare"].view(-1, 2) if "spare" not in small else torch.zeros((R - 1, 2), dtype=torch.int32)
+    desc = pe.make_desc(torch.float32, S, Hk, Hq, D, B, WIDTH, 64)
+    pe.pe_plan_tokens(desc, *(t[n] for n in ("seq_lens", "new_lens", "first_positions")), T, 0, *(t[n] for n in (
+        "free_pages", "free_used", "block_table", "spare", "seq_lens_out", "free_used_out", "cu_seqlens_out", "positions_out", "slots_out",
+        "admitted", "spare_used", "freed_phys", "only")))
+
+
+@pytest.mark.parametrize("name", ["seq_lens", "new_lens", "first_positions", "free_used", "block_table", "spare", "seq_lens_out", "free_used_out",
+                                  "cu_seqlens_out", "positions_out", "slots_out", "admitted", "spare_used", "freed_phys", "only"])
+def test_a_plan_needs_room_for_its_tokens(name, monkeypatch):
+    """Nothing is launched that would write (or read) behind a tensor's end."""
+    from paper_2509_04377_amd import binding as pe
+
+    class _Library:
+        addr_plan_tokens_ex = 1
+
+        def pe_plan_tokens_ex(self, *args):
+            raise _Took
+
+    library = _Library()
+    monkeypatch.setattr(pe, "lib", lambda: library)
+    monkeypatch.setattr(pe, "_host", pe._NoHost())
+    monkeypatch.setattr(pe, "_stream", lambda: None)
+    with pytest.raises(_Took):      # all are large enough
+        _plan_room()
+    with pytest.raises(ValueError, match=name + " must have room for"):
+        _plan_room(**{name: 1})
+
+
+@pytest.mark.parametrize("kind", ["paged", "quant"])
+def test_a_plan_to_write_into_that_is_too_small(kind, monkeypatch):
+    from paper_2509_04377_amd import binding as pe
+    c = _make(kind)
+    free = FreePages.of(torch.arange(8, dtype=torch.int32))
+    monkeypatch.setattr(pe, "_stream", lambda: None)
+    new = torch.ones(S, dtype=torch.int32)
+    plan = c.new_plan(5)
+    before = c.seq_lens, free.used
+    with pytest.raises(ValueError, match="positions_out must have room for 6"):
+        c.admit(new, 6, free, plan=plan)
+    assert c.seq_lens is before[0] and free.used is before[1] and c.admitted is None   # as it was

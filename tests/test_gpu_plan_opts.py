@@ -174,3 +174,61 @@ def test_a_place_that_is_used_again(kind, shared):
 
     (a, *rest), (b, *other) = life(False), life(True)
     assert rest == other and all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_plan_that_is_too_small_is_refused(native, monkeypatch):
+    """By the native marshalling and without it, before anything is launched; a larger one is fine."""
+    pe.lib()
+    if not native:
+        monkeypatch.setattr(pe, "_host", pe._NoHost())
+    S, width, P = 2, 4, 32
+    c = PagedCache.create(torch.bfloat16, S, 2, 2, 64, 16, empty_layout(S, 2, width, 1, P, DEV), 64)
+    free = FreePages.of(torch.arange(P, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError, match="positions_out must have room for 6"):
+        c.admit(_i32([3, 3]), 6, free, plan=c.new_plan(5))
+    plan = c.new_plan(6)
+    for name, t in (("slots_out", "slots"), ("cu_seqlens_out", "cu_seqlens"), ("admitted", "admitted")):
+        whole = getattr(plan, t)
+        setattr(plan, t, whole[:-1])
+        with pytest.raises(ValueError, match=name + " must have room for"):
+            c.admit(_i32([3, 3]), 6, free, plan=plan)
+        setattr(plan, t, whole)
+    with pytest.raises(ValueError, match="new_lens must have room for"):
+        c.admit(_i32([3]), 6, free)
+    assert c.seq_lens.tolist() == [0, 0] and int(free.used) == 0
+    plan = c.admit(_i32([3, 2]), 6, free, plan=c.new_plan(9))
+    assert c.seq_lens.tolist() == [3, 2] and plan.positions[:6].tolist() == [0, 1, 2, 0, 1, 0] and int(free.used) == 8
+
+
+def test_admissions_go_the_native_way_and_as_through_ctypes(monkeypatch):
+    pe.lib()
+    native, seen = pe._host, []
+
+    class _Recorder:
+        def __getattr__(self, name):
+            def call(*args):
+                seen.append((name, getattr(native, name)(*args)))
+                return seen[-1][1]
+            return call
+
+    def run():
+        S, width, n_spare, P, lens = 2, 4, 2, 48, [70, 9]
+        g = torch.Generator().manual_seed(8)
+        make = lambda cls: cls.create(torch.bfloat16, S, 2, 4, 64, 16, empty_layout(S, 2, width, n_spare, P, DEV), 64)   # noqa: E731
+        a, b = make(PagedCache), make(QuantCache)
+        plans = [c.admit(_i32(lens), 80, FreePages.of(torch.arange(P, dtype=torch.int32, device=DEV))) for c in (a, b)]
+        k, v = (torch.randn((79, 2, 64), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+        a.prefill_prune(k, v, plans[0].cu_seqlens, 70)
+        a.set_host_lens(lens)
+        b.take(a)
+        torch.cuda.synchronize()
+        return [x for p in plans for x in (p.cu_seqlens, p.positions, p.slots, p.admitted)] + [
+            a.k_pool, a.v_pool, a.block_table, a.seq_lens, a.spare, b.k.view(torch.uint8), b.scales, b.k_tail, b.scores, b.seq_lens, b.spare_used]
+
+    monkeypatch.setattr(pe, "_host", _Recorder())
+    one = run()
+    assert [name for name, _ in seen] == ["plan_tokens", "plan_tokens", "prefill_prune_admitted", "quant_pages_admitted"]
+    assert all(status == pe.PE_OK for _, status in seen)
+    monkeypatch.setattr(pe, "_host", pe._NoHost())
+    assert all(torch.equal(x, y) for x, y in zip(one, run()))
