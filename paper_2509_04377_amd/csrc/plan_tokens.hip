@@ -49,7 +49,9 @@ struct __attribute__((aligned(16))) Token {  // of a piece: where the pages of i
 };
 constexpr int kInTable = 1 << 16;
 
-// (The leading arguments are what a workgroup waits for first: they come in registers, the others with a load.)
+// (The leading arguments are what a workgroup waits for first: they come in registers, the others with a load.  OPTIONS: there are some; as
+// questions in one kernel they cost the plans without 0.2 us of 4.3, 0.4 of 10.0.)
+template <bool OPTIONS>
 __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* free_used, const int32_t* seq_lens, const int32_t* new_lens,
                                                                const int32_t* first_positions, const int num_seqs, const int num_free,
                                                                const uint32_t token_pieces, const uint32_t pieces, const uint32_t inv_rows,
@@ -64,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
   const int64_t given = *free_used;
   const int64_t used = given < 0 ? 0 : given > num_free ? num_free : given;
   // (what the list holds; of several copies, what is one's share: the sums ascend, so that a share that holds a sum holds those before it)
-  const int64_t left = a.copies > 1 ? (int64_t)((uint32_t)(num_free - used) / (uint32_t)a.copies) : num_free - used;
+  const int64_t left = OPTIONS && a.copies > 1 ? (int64_t)((uint32_t)(num_free - used) / (uint32_t)a.copies) : num_free - used;
   Sums before{0, 0};
   int64_t dealt = 0;
 
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
       kept = a.budget > 0 && after > a.budget ? (holds > a.budget ? holds : a.budget) : after;
       const int64_t pages = (kept + B - 1) >> log2_block;
       fits = len >= 0 && pages <= a.max_blocks && kept <= 0x7fffffffLL;
-      if (a.only != nullptr) fits = fits && a.only[s] != 0;
+      if (OPTIONS && a.only != nullptr) fits = fits && a.only[s] != 0;
       if (fits) per_row = (int)(pages - have) + (holds == 0 && n > 0 ? a.n_spare : 0);
     }
     const int need = per_row * rows;  // (the host keeps it under 2^31)
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
       if (lane == 0) dealt_of[wave] = mine;
       if (s < num_seqs) {
         a.seq_lens_out[s] = served ? (int32_t)kept : len;
-        if (a.admitted != nullptr) a.admitted[s] = !served || n == 0 ? 0 : len == 0 ? 1 : 2;
+        if (OPTIONS && a.admitted != nullptr) a.admitted[s] = !served || n == 0 ? 0 : len == 0 ? 1 : 2;
         if (a.cu_out != nullptr) {
           if (s == 0) a.cu_out[0] = 0;
           a.cu_out[s + 1] = (int32_t)(t_end < 0x7fffffffLL ? t_end : 0x7fffffffLL);
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) dealt = dealt_of[w] > dealt ? dealt_of[w] : dealt;
     }
-    if (a.spare_used != nullptr || a.freed_phys != nullptr) {  // rows of sequences that begin: what an earlier one left
+    if (OPTIONS && (a.spare_used != nullptr || a.freed_phys != nullptr)) {  // rows of sequences that begin: what an earlier one left
       for (int idx = (int)blockIdx.x * kThreads + me; idx < count * rows; idx += (int)gridDim.x * kThreads) {
         const int i = idx / rows;
         if (q.served[i] == 0 || q.len[i] != 0 || q.token_end[i] == (i > 0 ? q.token_end[i - 1] : before.tokens)) continue;
@@ -217,7 +219,9 @@ hipError_t launch_plan_tokens(const PlanArgs& a, int compute_units, hipStream_t 
   const uint32_t most = 8u * (uint32_t)compute_units, groups = pieces < most ? pieces : most;
   // idx / rows is the upper half of idx * inv_rows as long as idx * rows < 2^32 (idx < kThreads * rows); ~0: divided
   const uint32_t rows = (uint32_t)a.rows_per_seq, inv_rows = rows == 1 ? 0u : rows < 4096 ? (uint32_t)((1ull << 32) / rows + 1) : ~0u;
-  hipLaunchKernelGGL(plan_tokens_kernel, dim3(groups < 1 ? 1 : groups), dim3(kThreads), 0, stream, a.free_used, a.seq_lens,
+  const bool options = a.admitted != nullptr || a.spare_used != nullptr || a.freed_phys != nullptr || a.only != nullptr || a.copies > 1;
+  const auto kernel = options ? plan_tokens_kernel<true> : plan_tokens_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3(groups < 1 ? 1 : groups), dim3(kThreads), 0, stream, a.free_used, a.seq_lens,
                      a.new_lens, a.first_positions, a.num_seqs, a.num_free, token_pieces, pieces, inv_rows, a);
   return hipGetLastError();
 }

@@ -553,7 +553,6 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_kernel(co
   __shared__ uint32_t held_count[kSelMaxHeldChunks];
   const int row = (int)blockIdx.x;
   const int s = row / num_kv_heads, h = row % num_kv_heads;
-  if (admitted != nullptr && admitted[s] != 1) return;
   const int t0 = cu_seqlens[s];
   const int L = cu_seqlens[s + 1] - t0;
   const int keep = L < budget ? L : budget;
@@ -568,6 +567,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_kernel(co
   rs.deal(wave);
   rs.load();
 
+  if (admitted != nullptr && admitted[s] != 1) return;  // (behind the loads, which then do not wait for the question)
   if (h == 0 && tid == 0) seq_lens_out[s] = keep;
   if (kept_idx_out != nullptr)
     for (int i = keep + tid; i < budget; i += kSelThreads) kept_idx_out[(int64_t)row * budget + i] = -1;
@@ -784,7 +784,6 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
   // (head, sequence, part): the parts of a row lie side by side on one XCD where the number of rows is a multiple of eight
   const int h = (int)blockIdx.x, heads = (int)gridDim.x, s = seq0 + (int)blockIdx.y, part = (int)blockIdx.z;
   const int sel_row = SHARED ? s : s * heads + h, sel_h = SHARED ? 0 : h;
-  if (admitted != nullptr && admitted[s] != 1) return;
   const int t0 = cu_seqlens[s];
   const int L = cu_seqlens[s + 1] - t0;
   const int keep = L < budget ? L : budget;
@@ -792,7 +791,8 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
   const int tid = (int)threadIdx.x;
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const bool reports = !SHARED || h == 0;
-  if (part == 0) {
+  const bool begins = admitted == nullptr || admitted[s] == 1;
+  if (part == 0 && begins) {
     if (h == 0 && tid == 0) seq_lens_out[s] = keep;
     if (kept_idx_out != nullptr && reports)
       for (int i = keep + tid; i < budget; i += kSelThreads) kept_idx_out[(int64_t)sel_row * budget + i] = -1;
@@ -802,7 +802,7 @@ __global__ __launch_bounds__(kSelThreads, NV <= 4 ? 8 : 4) void select_gather_ke
   const int lo = part * share, hi = lo + share < keep ? lo + share : keep;
   // (a row longer than the caller has said is pruned like any other as long as it is held here and its table row holds it, else its
   // pages are left alone)
-  if (lo >= hi || L > Row::kHeld || (keep - 1) >> log2_block >= max_blocks) return;
+  if (!begins || lo >= hi || L > Row::kHeld || (keep - 1) >> log2_block >= max_blocks) return;
 
   const int32_t* bt = block_table + (int64_t)sel_row * max_blocks;
   const int block_mask = (1 << log2_block) - 1;
