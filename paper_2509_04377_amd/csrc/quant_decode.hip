@@ -17,8 +17,8 @@
 //
 //   PV (16x16x16; A = V transposed, B = weights): lane l holds elements EV m .. EV m + EV - 1 of tokens 4 i + g (EV = D / 16); element e of the
 //   four, brought together by byte permutes in front of the conversion, is a column of A whose contraction index is the token order in
-//   which the lane holds its weights, which are the other operand as they stand.  The classes of a head feed the terms of its weights: bfloat16: two, which are the weight to within 2^-17 (a value
-//   that is rounded to 8 bits on its way out does not show more); fp32: three, which are all of it (with two classes in two turns).
+//   which the lane holds its weights, which are the other operand as they stand.  The classes of a head feed the terms of its weights: bfloat16: two, rounded, which are the weight to within 2^-17
+//   (the first one cut off instead, to within 2^-16); fp32: three, which are all of it (with two classes in two turns).
 //
 // A page's K scale goes to the logits, V's to the weights on their way into the product.  Softmax: online, base 2, one reference a head and
 // wave, set kGrow above the largest logit and moved only when one exceeds it, so that rescaling and the exchange between lanes are rare.
@@ -127,7 +127,6 @@ struct Tile {
 
   uint32_t cut;    // all ones in the upper half for classes that take a second or third term ..
   uint32_t cut2;   // .. a third
-  uint32_t nudge;  // half a step of a term that is rounded
   float unit;      // 0 for classes without a term
   float l_run, m_run, m_ref;
   f32x4_t acc[EV];
@@ -136,12 +135,10 @@ struct Tile {
     if constexpr (NQ == 1) {
       cut = c == 1 ? 0xffff0000u : 0u;
       cut2 = 0u;
-      nudge = c == 1 ? 0x8000u : 0u;
       unit = c < 2 ? 1.f : 0.f;
     } else {
       cut = c >= 1 ? 0xffff0000u : 0u;
       cut2 = c >= 2 ? 0xffff0000u : 0u;
-      nudge = 0u;
       unit = c < 3 ? 1.f : 0.f;
     }
     l_run = 0.f;
@@ -201,10 +198,13 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float w = p[i] * s;
-      if constexpr (TURN == 0) {
+      if constexpr (NQ == 1) {  // both rounded: half a step is added before the lower half goes
+        w -= __uint_as_float((__float_as_uint(w) + 0x8000u) & cut);
+        t[i] = __float_as_uint(w) + 0x8000u;
+      } else if constexpr (TURN == 0) {
         w -= __uint_as_float(__float_as_uint(w) & cut);
-        if constexpr (NQ == 3 && GW == 4) w -= __uint_as_float(__float_as_uint(w) & cut2);
-        t[i] = __float_as_uint(w) + nudge;
+        if constexpr (GW == 4) w -= __uint_as_float(__float_as_uint(w) & cut2);
+        t[i] = __float_as_uint(w);
       } else {
         w -= __uint_as_float(__float_as_uint(w) & 0xffff0000u);
         w -= __uint_as_float(__float_as_uint(w) & 0xffff0000u);
