@@ -144,13 +144,13 @@ __global__ __launch_bounds__((Groups<T, D, B>::kWaves * kWave)) void quant_pages
   const int row = (int)(blockIdx.x / (unsigned)groups_per_row), s = row / a.num_kv_heads, hk = row - s * a.num_kv_heads;
   const int j = (int)(blockIdx.x - (unsigned)row * (unsigned)groups_per_row) * kPages + slot;
   const int len = a.seq_lens[s];
-  if (a.admitted != nullptr && a.admitted[s] == 0) return;  // (the workgroup has no other row)
   const int most = len < 0 ? 0 : len / B, full = most < a.max_blocks ? most : a.max_blocks;
   const int64_t table_row = (int64_t)(a.shared ? s : row) * a.max_blocks;
   const int heads = a.shared ? a.num_kv_heads : 1;          // token rows between a head's consecutive tokens
   const bool has = j < full;
   const int from = has || (j == full && j < a.max_blocks && len > 0 && len % B != 0) ? a.src_table[table_row + j] : -1;
   const int to = has ? a.block_table[table_row + j] : -1;
+  if (a.admitted != nullptr && a.admitted[s] == 0) return;  // (the workgroup has no other row; behind the loads, which do not wait for it)
   const bool real = has && from >= 0 && to >= 0;
   const int64_t head_row = a.shared ? hk : 0;
   // (16-byte vectors; without a page the pool's first: any address inside will do)
