@@ -507,7 +507,9 @@ int pe_plan_tokens(const pe_cache_desc* desc, const int32_t* seq_lens, const int
  *        PE_ROPE_BY_PARTS  with r = original f_i / 2 pi (turns within the original context) and g = clamp((r - low) / (high - low), 0, 1):
  *                          f_i (g + (1 - g) / factor) -- fast pairs as they are, slow ones as LINEAR.
  *     and m = magnitude (1: none).  transpose != 0: angles -p f_i, the gradient of the inputs from that of the outputs (with the same m).
- *     Computed in 32 bits from angles that are exact modulo a turn up to the last of 64 bits at any position, rounded once to desc->dtype.
+ *     Computed in 32 bits and rounded once to desc->dtype, from angles that are p (f_i / 2 pi) modulo a turn, exact, with f_i / 2 pi in units of 2^-64
+ *     turns and within two of them (BY_PARTS with high - low much smaller than high: of what these leave): off by 2^-63 turns a
+ *     position, 2^-32 turns (1.5e-9) at the furthest, 2^31.
  *
  * pe_rope_init fills a caller's structure on the host, once for a model: 1 <= rotary_dim / 2 <= 64, rotary_dim even; base > 1; factor >= 1;
  * BY_PARTS: 0 <= low < high, original > 0 (not looked at otherwise); magnitude > 0; all finite.  Its fields are the library's.

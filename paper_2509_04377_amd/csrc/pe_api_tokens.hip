@@ -2,6 +2,7 @@
 // the caller's stream.
 #include "../../include/pe.h"
 
+#include <float.h>
 #include <math.h>
 
 #include "pe_check.h"
@@ -95,17 +96,22 @@ int pe_rope_init(pe_rope* rope, int32_t rotary_dim, int32_t pairs, double base, 
   if (scaling != PE_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return PE_ERR_INVALID_ARG;
   if (scaling == PE_ROPE_BY_PARTS && (!(low >= 0.0) || !(high > low) || !isfinite(high) || !(original > 0.0) || !isfinite(original)))
     return PE_ERR_INVALID_ARG;
-  const double two_pi = 6.283185307179586476925286766559;
+  // With 64 bits of mantissa: a power, a quotient and the exponent's rounding, half a step each and the last one ln f times, leave f / 2 pi <= 0.16
+  // off by less than a unit, and its rounding by half a one.
+#if !defined(__HIP_DEVICE_COMPILE__)
+  static_assert(LDBL_MANT_DIG >= 64, "an x86 host's long double");
+#endif
+  const long double two_pi = 6.283185307179586476925286766559005768L;
   for (int i = 0; i < rotary_dim / 2; ++i) {
-    double f = pow(base, -2.0 * i / rotary_dim);
+    long double f = powl((long double)base, -2.0L * i / rotary_dim);
     if (scaling == PE_ROPE_LINEAR) {
       f /= factor;
     } else if (scaling == PE_ROPE_BY_PARTS) {
-      const double g = (original * f / two_pi - low) / (high - low);
-      const double keep = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
-      f *= keep + (1.0 - keep) / factor;
+      const long double g = (original * f / two_pi - low) / ((long double)high - low);
+      const long double keep = g < 0.0L ? 0.0L : g > 1.0L ? 1.0L : g;
+      f *= keep + (1.0L - keep) / factor;
     }
-    rope->turns[i] = (uint64_t)rint(f / two_pi * 18446744073709551616.0);  // f <= 1: less than a sixth of a turn
+    rope->turns[i] = (uint64_t)rintl(f / two_pi * 18446744073709551616.0L);  // f <= 1: less than a sixth of a turn
   }
   rope->rotary_dim = rotary_dim;
   rope->pairs = pairs;
