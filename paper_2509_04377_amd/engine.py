@@ -704,6 +704,11 @@ class QuantCache(Admits):
         into the pages of this table, which has as many, and scored; the rest goes to the tail.  Behind admit() those of the sequences that it
         let begin or go on here: the others stay as they are.  The mirror takes the other cache's numbers, and keeps its own where those are 0; it is
         to be told (there or here) of a sequence that was left here and not there."""
+        other = [n for n in ("dtype", "num_seqs", "num_kv_heads", "head_dim", "block_size", "max_blocks", "layout")
+                 if getattr(self.desc, n) != getattr(paged.desc, n)]
+        if other:
+            raise ValueError("a cache of another shape: " + ", ".join("%s %d, here %d" % (n, getattr(paged.desc, n), getattr(self.desc, n))
+                                                                      for n in other))
         _launch(pe.pe_quant_pages, self.desc, self.cache, paged.k_pool, paged.v_pool, paged.block_table, paged.seq_lens, self.block_table, self.scores,
                 self.admitted)
         if not HostOnly.active:

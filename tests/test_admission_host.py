@@ -157,3 +157,24 @@ def test_a_plan_to_write_into_that_is_too_small(kind, monkeypatch):
     with pytest.raises(ValueError, match="positions_out must have room for 6"):
         c.admit(new, 6, free, plan=plan)
     assert c.seq_lens is before[0] and free.used is before[1] and c.admitted is None   # as it was
+
+
+@pytest.mark.parametrize("quant", ["quant", "quant_layers"])
+def test_only_caches_of_one_shape_are_taken(quant):
+    """Another width or number of sequences would have the other cache's table read behind its rows, other types and pages its pools."""
+    to = _make(quant)
+    take = (lambda c: to.take_layer(1, c)) if quant == "quant_layers" else to.take
+    made = dict(dtype=torch.float32, num_seqs=S, num_kv_heads=Hk, num_q_heads=Hq, head_dim=D, block_size=B, width=WIDTH, shared=False)
+    for what, change in (("dtype", dict(dtype=torch.bfloat16)), ("num_seqs", dict(num_seqs=2)), ("num_kv_heads", dict(num_kv_heads=4)),
+                         ("head_dim", dict(head_dim=128)), ("block_size", dict(block_size=32)), ("max_blocks", dict(width=WIDTH - 1)),
+                         ("max_blocks", dict(width=WIDTH + 1)), ("layout", dict(shared=True)), (None, dict(num_q_heads=8))):
+        a = dict(made, **change)
+        layout = empty_layout(a["num_seqs"], a["num_kv_heads"], a["width"], 1, 64, "cpu", a["shared"])
+        c = PagedCache.create(a["dtype"], a["num_seqs"], a["num_kv_heads"], a["num_q_heads"], a["head_dim"], a["block_size"], layout, BUDGET, device="cpu",
+                              shared=a["shared"])
+        with host_only():
+            if what is None:
+                take(c)
+            else:
+                with pytest.raises(ValueError, match="another shape: " + what):
+                    take(c)
