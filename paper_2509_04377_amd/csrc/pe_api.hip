@@ -232,7 +232,7 @@ uint64_t launch_tag() {
 
 extern "C" {
 
-int pe_version(void) { return 500; }  // 0.5.0: plans of tokens, rotary positions, caches in 8 bits
+int pe_version(void) { return 501; }  // 0.5.1: plans with options, prunes and rounded pages of admitted sequences
 
 const char* pe_status_string(int status) {
   switch (status) {

@@ -15,6 +15,8 @@
 //                     share of what is kept.
 // A token is kept iff score > T, or score == T and at least q equal-score tokens precede it.
 //
+// A page that a row did not get (-1) is passed over, which takes 1 % where all is copied (64 prompts of 300 tokens, all kept 37.6 -> 38.1 us,
+// four of 4096 22.6 -> 22.9; 32 of 16384 437, no more).
 // With `admitted` only its sequences of 1 are selected and copied (the sweep goes over all tokens as they lie); the others' workgroups return.
 //
 // Head-shared mode (one decision per sequence, pages [B][Hk][D]): a token's score is the mean of its heads' scores (head

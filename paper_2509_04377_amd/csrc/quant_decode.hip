@@ -17,8 +17,9 @@
 //
 //   PV (16x16x16; A = V transposed, B = weights): lane l holds elements EV m .. EV m + EV - 1 of tokens 4 i + g (EV = D / 16); element e of the
 //   four, brought together by byte permutes in front of the conversion, is a column of A whose contraction index is the token order in
-//   which the lane holds its weights, which are the other operand as they stand.  The classes of a head feed the terms of its weights: bfloat16: two, rounded, which are the weight to within 2^-17
-//   (the first one cut off instead, to within 2^-16); fp32: three, which are all of it (with two classes in two turns).
+//   which the lane holds its weights, which are the other operand as they stand.  The classes of a head feed the terms of its weights:
+//   bfloat16: two, rounded, which are the weight to within 2^-17 (with the first one cut off 2^-16, in as much time); fp32: three, which are all
+//   of it (with two classes in two turns).
 //
 // A page's K scale goes to the logits, V's to the weights on their way into the product.  Softmax: online, base 2, one reference a head and
 // wave, set kGrow above the largest logit and moved only when one exceeds it, so that rescaling and the exchange between lanes are rare.
@@ -272,7 +273,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void quant_decode_kernel(
   const int stride = splits * WAVES, first = split * WAVES + wave;
   const int tiles_log2 = log2_block - ilog2(kTile), in_page = (1 << tiles_log2) - 1;
 
-  // (an unused entry, -1, is replaced by page 0: its tokens are masked, so any address inside the pool will do)
+  // (an unused entry, -1, is replaced by page 0: its tokens are behind the row's end and masked, so any address inside the pool will do.  A page
+  // that is missing in front of the end, which an append without a spare page leaves behind, is the caller's: what is read there is page 0.)
   const auto lookup = [&](int tile) {
     int pi = tile >> tiles_log2;
     pi = pi < max_blocks ? pi : max_blocks - 1;

@@ -6,7 +6,9 @@
 // pairs: 16 bytes), the next ones on their way while these are turned.  What is written does not pass through the caches (854 MB moved, with keys
 // and values stored: 146 us or 5.9 TB/s, a copy reaches 5.2; with ordinary stores 152; fp32, 36 MB: 6.6 us, 8.2).
 //
-// Where rows are not 16-byte aligned, or a half is no multiple of 16 bytes, threads walk over single pairs instead.
+// Where rows are not 16-byte aligned, or a half is no multiple of 16 bytes, threads walk over single pairs instead, 2 bytes (fp32: 4) an access with
+// a division and a look at the slot for each: 32004 tokens of 32 + 8 heads of D = 128, stored, bfloat16, rotary 40 294 us, rotary 128 in rows
+// 2 bytes off 292 (2.9 TB/s; 146 by vectors), neighbours as pairs 281 to 288; 8000 tokens of fp32, rotary 40 95 us, rows 4 bytes off 109 (63).
 #include "pe_rope_device.h"
 #include "pe_tokens.h"
 

@@ -665,12 +665,12 @@ class QuantCache(Admits):
     budget: int
     workspace: torch.Tensor
     host_lens: list
-    admitted: torch.Tensor = None   # of the last admit()
-    part_of_another: bool = False
     rope: pe.pe_rope = None         # turns keys and queries on their way (positions: see decode_step)
     positions: torch.Tensor = None  # [S] int32, of the new token of every sequence: the caller's, changed in place from step to step
     turned: torch.Tensor = None     # [S, Hq, D]: the queries, turned
     evict_opts: pe.pe_evict_opts = None
+    admitted: torch.Tensor = None   # of the last admit()
+    part_of_another: bool = False
     cached_scores = fused_evict = False   # (what GraphedStepper asks a cache about: not here)
     selection = attention = host_scored = None
 
@@ -695,7 +695,7 @@ class QuantCache(Admits):
                           table.to(device).contiguous(), torch.zeros(num_seqs, **i32), torch.zeros(num_seqs, **i32), spare.to(device).contiguous(),
                           torch.zeros(per_row, **i32), torch.full(per_row, -1, **i32), torch.full(per_row, -1, **i32),
                           torch.full((num_seqs, num_kv_heads, layout.max_blocks), float("inf"), dtype=torch.float32, **on), int(budget),
-                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, None, False, rope,
+                          pe.alloc_workspace(pe.PE_OP_QUANT_DECODE, desc, device=device), [0] * num_seqs, rope,
                           torch.zeros(num_seqs, **i32) if rope is not None else None,
                           torch.empty((num_seqs, num_q_heads, head_dim), dtype=dtype, **on) if rope is not None else None)
 
