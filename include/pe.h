@@ -131,7 +131,8 @@ int pe_decode_splits(const pe_cache_desc* desc);
  *        scores_out[s][hk][j] = (1/B) * sum over the page's B tokens of ||V_i||_2 / ||K_i||_2,
  *     accumulated in fp64 and rounded once to fp32.  Every other entry (partial tail page, unused)
  *     is +INF.  A token with ||V|| = 0 contributes 0; otherwise ||K|| = 0 contributes +INF.
- *     scores_out: [S][Hk][max_blocks] fp32, fully overwritten.  Reads pools/table/lens only.
+ *     scores_out: [S][Hk][max_blocks] fp32, fully overwritten.  Reads pools/table/lens only.  An entry of -1 among the full pages is
+ *     read as page 0 (as in the attention).
  *     workspace: none needed (may be NULL / 0).
  *     shared: block_table is [S][max_blocks]; scores_out keeps its shape and holds the per-head page scores
  *     (the head mean is taken where the decision is, in (3)).

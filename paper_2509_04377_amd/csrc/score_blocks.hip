@@ -74,8 +74,9 @@ struct PageGeom {
   static constexpr int NCH = B / CH;
   using CS = ChunkScore<T, D, CH>;
   static constexpr int64_t kVecPerPage = (int64_t)NCH * CS::kVecPerChunk;
+  // (a page that a row did not get, -1, is read as page 0, as in the attention: any address inside the pool will do)
   static __device__ __forceinline__ int64_t chunk_base(int phys, int c) {
-    return (int64_t)phys * kVecPerPage + (int64_t)c * CS::kVecPerChunk;
+    return (int64_t)(phys < 0 ? 0 : phys) * kVecPerPage + (int64_t)c * CS::kVecPerChunk;
   }
 };
 
