@@ -302,6 +302,8 @@ int pe_paged_decode_static(const pe_cache_desc* desc, const void* q, const void*
  * spare[s][hk][spare_used[s][hk]++].  Then seq_lens[s] += 1.
  * new_k, new_v: [S][Hk][D].  spare: [S][Hk][n_spare] int32.  spare_used, freed_phys: [S][Hk] int32,
  * updated in place.  Preconditions: seq_lens[s] < max_blocks*B; the spare list is not exhausted.
+ * A negative length, here and in the other calls that append: no sequence has this place.  It is left untouched, with its length, no eviction takes
+ * from it, and what an attention puts out for it means nothing.
  * shared: one page per sequence takes the rows of all heads; spare [S][n_spare], spare_used and freed_phys [S].
  */
 int pe_append_kv(const pe_cache_desc* desc, const void* new_k, const void* new_v, void* k_pool, void* v_pool,
@@ -453,6 +455,7 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
  *     rows gets the pages that this takes beyond those it has, and a sequence that begins (seq_lens[s] == 0, n > 0) n_spare pages
  *     more a row into `spare` (NULL with n_spare 0: none), the list that pe_append_kv takes pages from.  Pages are dealt row by row, in the order
  *     of the sequences: free_pages[free_used[0]], free_pages[free_used[0] + 1], ..., first those of the table, then the spare ones.
+ *     A negative seq_lens[s] (no sequence has this place) counts as 0 where n > 0, and stays where n is 0 or the pages are not there.
  *     A sequence whose pages the list does not hold, or whose table row is too short, is left as it was, and so is every later one that
  *     needs pages where it was the list: seq_lens_out[s] = seq_lens[s], its tokens' slots -1.
  *     block_table: in/out, only the new entries are written.  seq_lens_out: [S], what each sequence holds then.  free_used_out: [1], the pages
@@ -466,7 +469,7 @@ int pe_paged_decode_weights(const pe_cache_desc* desc, const void* q, const void
  *     shared: block_table [S][max_blocks], spare [S][n_spare], slots_out [total_tokens].
  *
  * pe_plan_tokens_ex: the same with options (NULL, or a field NULL: without).
- *     admitted: [S], out: 1 where a sequence begins (it held no token, brings some and got its pages), 2 where one goes on, 0 where a
+ *     admitted: [S], out: 1 where a sequence begins (its place held no token, it brings some and got its pages), 2 where one goes on, 0 where a
  *     sequence was left as it was or brings nothing.
  *     spare_used, freed_phys: [S][Hk] (shared: [S]), in/out: 0 (where n_spare > 0) and -1 in the rows of sequences that begin, whose place an
  *     earlier sequence may have had: what pe_append_kv counts from is then the new list, and a page that was freed is no longer linked.

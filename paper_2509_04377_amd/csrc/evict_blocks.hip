@@ -156,7 +156,10 @@ __global__ __launch_bounds__(kThreads) void append_kv_kernel(const uint4* __rest
   const int len = seq_lens[s];
   const int slot = len % block_size;
   const int jb = len / block_size;
-  if (len < 0 || jb >= max_blocks) return;  // caller precondition violated: leave everything untouched
+  if (len < 0 || jb >= max_blocks) {  // no sequence, or a caller precondition violated: leave everything untouched
+    if (threadIdx.x == 0 && seq_lens_out != nullptr) seq_lens_out[s] = len;
+    return;
+  }
   if (slot == 0) {
     for (int h = (int)threadIdx.x; h < num_kv_heads; h += kThreads) {
       const int64_t row = (int64_t)s * num_kv_heads + h;

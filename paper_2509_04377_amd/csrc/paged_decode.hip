@@ -415,7 +415,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_decode_kernel(
           reinterpret_cast<uint4*>(const_cast<void*>(v_pool_p))[vec] = nv[0];
         }
       }
-      if (hk == 0 && lane == 0) p.seq_lens_out[s] = len_pool + 1;
+      if (hk == 0 && lane == 0) p.seq_lens_out[s] = len_pool + (len_pool >= 0 ? 1 : 0);  // (below 0: no sequence)
     }
   }
   // The placeholder loads behind a wave's last tile are still on their way during the merge; their registers are in use until

@@ -459,7 +459,7 @@ void paged_decode_bf16_kernel(
           if (tl.v_tok == 0) v_to[base + v_slice] = nv;
         }
       }
-      if (hk == 0 && lane == 0) p.seq_lens_out[s] = len_pool + 1;
+      if (hk == 0 && lane == 0) p.seq_lens_out[s] = len_pool + (len_pool >= 0 ? 1 : 0);  // (below 0: no sequence)
     }
   }
   // The loads behind a wave's last tiles are still on their way while the rows are merged.  Their registers are not to be given

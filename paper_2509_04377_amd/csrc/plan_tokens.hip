@@ -80,14 +80,14 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
     if (s < num_seqs) {
       len = seq_lens[s];
       n = new_lens[s];
-      first = first_positions != nullptr ? first_positions[s] : len;
       n = n < 0 ? 0 : n;
-      const int64_t holds = len < 0 ? 0 : len;
+      const int64_t holds = len < 0 ? 0 : len;  // (below 0: no sequence, one can begin here)
+      first = first_positions != nullptr ? first_positions[s] : (int)holds;
       have = (int)((holds + B - 1) >> log2_block);
       after = holds + n;
       kept = a.budget > 0 && after > a.budget ? (holds > a.budget ? holds : a.budget) : after;
       const int64_t pages = (kept + B - 1) >> log2_block;
-      fits = len >= 0 && pages <= a.max_blocks && kept <= 0x7fffffffLL;
+      fits = (len >= 0 || n > 0) && pages <= a.max_blocks && kept <= 0x7fffffffLL;
       if (OPTIONS && a.only != nullptr) fits = fits && a.only[s] != 0;
       if (fits) per_row = (int)(pages - have) + (holds == 0 && n > 0 ? a.n_spare : 0);
     }
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
     q.page_end[me] = p_end;
     q.have[me] = have;
     q.per_row[me] = per_row;
-    q.len[me] = len;
+    q.len[me] = len < 0 ? 0 : len;
     q.served[me] = served ? (kept == after ? 2 : 1) : 0;
     q.first[me] = first;
     if (blockIdx.x == 0) {
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void plan_tokens_kernel(const int32_t* fr
       if (lane == 0) dealt_of[wave] = mine;
       if (s < num_seqs) {
         a.seq_lens_out[s] = served ? (int32_t)kept : len;
-        if (OPTIONS && a.admitted != nullptr) a.admitted[s] = !served || n == 0 ? 0 : len == 0 ? 1 : 2;
+        if (OPTIONS && a.admitted != nullptr) a.admitted[s] = !served || n == 0 ? 0 : len <= 0 ? 1 : 2;
         if (a.cu_out != nullptr) {
           if (s == 0) a.cu_out[0] = 0;
           a.cu_out[s + 1] = (int32_t)(t_end < 0x7fffffffLL ? t_end : 0x7fffffffLL);

@@ -56,6 +56,11 @@ def triggers(host_lens, block_size: int, budget: int) -> List[bool]:
     return [n > 0 and n % block_size == 0 and n >= budget for n in host_lens]
 
 
+def stepped(host_lens) -> List[int]:
+    """The lengths behind a step's new tokens; -1: no sequence, which gets none."""
+    return [n + 1 if n >= 0 else n for n in host_lens]
+
+
 def evicts_within(n, tokens, block_size: int, budget: int) -> bool:
     """Whether a sequence of n cached tokens that takes on so many more is to lose a page on the way."""
     full = max(-(-max(n, budget) // block_size), 1) * block_size   # the first length from n on at which a page goes
@@ -106,9 +111,8 @@ class Admits:
     def admit(self, new_lens, total_tokens, free: FreePages, first_positions=None, plan=None, whole=False):
         """Pages for the tokens that every sequence brings (new_lens [S] int32 on the device, packed total_tokens of them or fewer), up to
         the budget, and for sequences that begin their spare pages too.  Sequences that do not get their pages stay as they were; which
-        those are the plan's `admitted` says, on the device, and the cache keeps it for its prefill_prune().  A sequence begins where seq_lens
-        are 0 (its place may have been another's: its spare list counts from its start again, and the pages that the other one
-        held are the caller's to hand back).  whole: the
+        those are the plan's `admitted` says, on the device, and the cache keeps it for its prefill_prune().  A sequence begins in a place that
+        holds nothing, or that end() has emptied, with a spare list that counts from its start.  whole: the
         tokens are not pruned, and one that would take a sequence beyond its table row leaves it as it was (slots are for these).  The
         lengths on the device are those with the new tokens then (what follows writes the tokens); the mirror is told by
         set_host_lens.  plan: one to write into (the same tensors again, as a captured step needs)."""
@@ -130,6 +134,33 @@ class Admits:
         self.seq_lens, self.seq_lens_alt = self.seq_lens_alt, self.seq_lens
         free.used, free.used_alt = free.used_alt, free.used
         return plan
+
+    def end(self, places):
+        """The sequences in these places end.  What is returned (int32, on the device) are the pages that they had, spare ones and all, for a list
+        that deals them out again.  Until admit() lets another one begin, such a place has no sequence: its length is -1, steps leave it alone and
+        what they put out for it means nothing.  Due too for places that are empty from the start, as soon as others take steps."""
+        if self.part_of_another:
+            raise ValueError("end() is the whole cache's (all layers')")
+        places = sorted(set(places))
+        pages = self._vacate(places)
+        self.set_host_lens([-1 if s in places else None for s in range(self.desc.num_seqs)], whole=True)
+        return pages
+
+    def _vacate(self, places):
+        """end() on the device."""
+        dev, S, B = self.block_table.device, self.desc.num_seqs, self.desc.block_size
+        if any(not 0 <= s < S for s in places):
+            raise ValueError("places are 0 to %d, got %s" % (S - 1, places))
+        at = torch.tensor(places, dtype=torch.int64, device=dev)
+        table, spare = (t.view(S, -1, t.shape[-1])[at] for t in (self.block_table, self.spare))
+        used, freed = (t.view(S, -1)[at] for t in (self.spare_used, self.freed_phys))
+        held = (self.seq_lens[at].clamp(min=0) + (B - 1)).div(B, rounding_mode="floor")
+        mine = torch.arange(table.shape[-1], device=dev) < held[:, None, None]
+        left = torch.arange(spare.shape[-1], device=dev) >= used[..., None]
+        pages = torch.cat((table[mine.expand(table.shape)], spare[left], freed.flatten()))
+        for t, nothing in ((self.block_table, -1), (self.spare, -1), (self.spare_used, 0), (self.freed_phys, -1), (self.seq_lens, -1)):
+            t[at] = nothing
+        return pages[pages >= 0]
 
     def new_plan(self, total_tokens):
         """Room for the plan of so many tokens."""
@@ -264,7 +295,7 @@ class PagedCache(Admits):
             self.score_and_evict()
             self.evicted(trig)
         self.append_and_attend(new_k, new_v, q, out, softmax_scale, fused)
-        self.host_lens = [n + 1 for n in self.host_lens]
+        self.host_lens = stepped(self.host_lens)
 
     def evicted(self, which):
         """Bookkeeping behind an eviction of these sequences."""
@@ -369,6 +400,8 @@ class PagedCache(Admits):
         if len(left) != len(self.host_lens) or min(left) < 0 or max(left) > path.shape[-1]:
             raise ValueError("host_path_lens: one length per sequence, 0 to path.shape[-1]")
         room = self.desc.max_blocks * B
+        if any(n < 0 and m > 0 for n, m in zip(self.host_lens, left)):
+            raise ValueError("a path in a place that has no sequence")
         if self.budget > room and any(n + m > room for n, m in zip(self.host_lens, left)):
             raise ValueError("the path is longer than what is left of a table row, and nothing is evicted below the budget")
         if self.attention is not None and not self.attention.started and any(evicts_within(n, m, B, self.budget)
@@ -503,7 +536,16 @@ class Attention:
 
 
 class LayeredAdmits:
-    """admit() and set_host_lens() for a driver of several layers."""
+    """admit(), end() and set_host_lens() for a driver of several layers."""
+
+    def end(self, places):
+        """The caches' end(), in every layer."""
+        places = sorted(set(places))
+        if any(not 0 <= s < self.S for s in places):
+            raise ValueError("places are 0 to %d, got %s" % (self.S - 1, places))
+        pages = self.folded._vacate([l * self.S + s for l in range(self.layers) for s in places])
+        self.set_host_lens([-1 if s in places else None for s in range(self.S)], whole=True)
+        return pages
 
     def set_host_lens(self, prompt_lens, whole=False):
         """The caches' set_host_lens(): the same lengths in every layer."""
@@ -610,7 +652,7 @@ class LayeredCache(LayeredAdmits):
             f.attention.started = True
         if fused:   # every layer wrote its new lengths into the other array
             f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens
-        self.host_lens = [n + 1 for n in self.host_lens]
+        self.host_lens = stepped(self.host_lens)
         return any(trig)
 
     def tree_decode_layer(self, layer, q, k_draft, v_draft, tree_mask, out, draft_lens=None, softmax_scale=None, workspace=None):
@@ -713,7 +755,7 @@ class QuantCache(Admits):
                 self.admitted)
         if not HostOnly.active:
             self.seq_lens.copy_(paged.seq_lens if self.admitted is None else torch.where(self.admitted != 0, paged.seq_lens, self.seq_lens))
-        self.host_lens = [n if n or self.admitted is None else mine for n, mine in zip(paged.host_lens, self.host_lens)]
+        self.host_lens = [n if n > 0 or self.admitted is None else mine for n, mine in zip(paged.host_lens, self.host_lens)]
 
     def triggers(self) -> List[bool]:
         return triggers(self.host_lens, self.desc.block_size, self.budget)
@@ -744,7 +786,7 @@ class QuantCache(Admits):
         if any(self.triggers()):
             self.score_and_evict()
         self.append_and_attend(new_k, new_v, q, out, softmax_scale)
-        self.host_lens = [n + 1 for n in self.host_lens]
+        self.host_lens = stepped(self.host_lens)
 
     def rows(self, first, end):
         """The same cache's sequences first .. end - 1, as a cache (views of the same pages; host_lens is a copy), as PagedCache.rows: to take
@@ -794,7 +836,7 @@ class LayeredQuantCache(LayeredAdmits):
         for l, c in enumerate(self.per_layer):
             c.append_and_attend(new_k[l], new_v[l], q[l], out[l], softmax_scale)
         f.seq_lens, f.seq_lens_alt = f.seq_lens_alt, f.seq_lens   # (each layer has swapped its part)
-        self.host_lens = [n + 1 for n in self.host_lens]
+        self.host_lens = stepped(self.host_lens)
         return any(trig)
 
 

@@ -178,3 +178,60 @@ def test_only_caches_of_one_shape_are_taken(quant):
             else:
                 with pytest.raises(ValueError, match="another shape: " + what):
                     take(c)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("kind", KINDS)
+def test_sequences_that_end(kind, shared):
+    """Their pages come back once, their places are as if nobody had been there, and the mirror leaves them out of steps."""
+    cls = dict(paged=PagedCache, quant=QuantCache, layers=LayeredCache, quant_layers=LayeredQuantCache)[kind]
+    n, rows, spares = 2 if "layers" in kind else 1, 1 if shared else Hk, 3
+    args = (Hk, Hq, D, B, empty_layout(n * S, Hk, WIDTH, spares, 999, "cpu", shared), BUDGET)
+    c = cls(torch.float32, n, S, *args, device="cpu", shared=shared) if n > 1 else cls.create(torch.float32, S, *args, device="cpu", shared=shared)
+    f = c.folded if n > 1 else c
+    ids = torch.arange(n * S * rows * (WIDTH + spares), dtype=torch.int32).view(n, S, rows, WIDTH + spares)
+    f.block_table.view(n, S, rows, WIDTH)[:] = ids[..., :WIDTH]     # (behind the length too: what is left there of earlier ones)
+    f.spare.view(n, S, rows, spares)[:] = ids[..., WIDTH:]
+    f.spare_used.view(n, S, rows)[:] = torch.tensor([0, 2, 3])[:, None]
+    f.seq_lens.view(n, S)[:] = torch.tensor([33, 64, 5])
+    f.freed_phys.view(n, S, rows)[:, 1, 0] = 900
+    c.set_host_lens([33, 64, 5])
+    before = [t.clone() for t in (f.block_table, f.spare, f.spare_used, f.seq_lens, f.freed_phys)]
+    got = c.end(iter([1, 2, 1]))
+    want = [x for l in range(n) for s, held, used in ((1, 4, 2), (2, 1, 3)) for h in range(rows)
+            for x in ids[l, s, h, :held].tolist() + ids[l, s, h, WIDTH + used:].tolist()] + [900] * n
+    assert sorted(got.tolist()) == sorted(want) and got.dtype == torch.int32
+    assert c.host_lens == [33, -1, -1]
+    for t, was, nothing in zip((f.block_table, f.spare, f.spare_used, f.seq_lens, f.freed_phys), before, (-1, -1, 0, -1, -1)):
+        t, was = t.view((n, S) + t.shape[1:]), was.view((n, S) + t.shape[1:])
+        assert torch.equal(t[:, 0], was[:, 0]) and bool((t[:, 1:] == nothing).all())
+    assert c.end([2]).numel() == 0
+    lead = (n, S) if n > 1 else (S,)
+    new, q = torch.zeros(lead + (Hk, D)), torch.zeros(lead + (Hq, D))
+    with host_only():
+        for step in range(40):
+            c.decode_step(new, new, q, torch.zeros_like(q))
+    assert c.host_lens == [_stepped(33, 40), -1, -1]
+    for bad in ([3], [-1], [0, 7]):
+        with pytest.raises(ValueError, match="places are 0 to 2"):
+            c.end(bad)
+    with pytest.raises(ValueError, match="the whole cache's"):
+        f.rows(0, 2).end([0])
+
+
+def _stepped(n, steps):
+    for _ in range(steps):
+        n += 1 - (B if n % B == 0 and n >= BUDGET else 0)
+    return n
+
+
+def test_no_path_where_there_is_no_sequence():
+    c = _make("paged")
+    c.end([1])
+    drafts = torch.zeros((S, 4, Hk, D))
+    path, lens = torch.zeros((S, 4), dtype=torch.int32), torch.tensor([1, 1, 0], dtype=torch.int32)
+    with host_only():
+        with pytest.raises(ValueError, match="no sequence"):
+            c.accept_path(drafts, drafts, path, lens, [1, 1, 0])
+        c.accept_path(drafts, drafts, path, lens, [3, 0, 2])
+    assert c.host_lens == [3, -1, 2]

@@ -232,3 +232,18 @@ def test_admissions_go_the_native_way_and_as_through_ctypes(monkeypatch):
     assert all(status == pe.PE_OK for _, status in seen)
     monkeypatch.setattr(pe, "_host", pe._NoHost())
     assert all(torch.equal(x, y) for x, y in zip(one, run()))
+
+
+@pytest.mark.parametrize("case", [dict(lens=[0, 7, 0, 0, 64, 0], new=[33, 2, 0, 16, 1, -3], rows=2, B=16, width=8, n_spare=1),
+                                  dict(lens=[0, 0, 0], new=[200, 64, 1], rows=2, B=16, width=8, budget=64, n_spare=1, left=14),
+                                  dict(lens=[0, 16, 0], new=[17, 0, 1], rows=1, B=32, width=4, shared=True)])
+@pytest.mark.parametrize("below", [-1, -2 ** 31])
+def test_places_without_a_sequence(case, below):
+    """As places that hold nothing, but that what does not begin stays without one."""
+    a = _Call(**case)
+    b = _Call(**dict(case, lens=[below if n == 0 else n for n in case["lens"]]))
+    answers = [torch.full((len(a.lens),), -9, dtype=torch.int32, device=DEV) for _ in range(2)]
+    want, got = a.run(admitted=answers[0]), b.run(admitted=answers[1])
+    assert answers[0].tolist() == answers[1].tolist() == a.served()
+    assert got[0] == [below if n == 0 and m == 0 else w for n, m, w in zip(a.lens, a.served(), want[0])]
+    assert got[1:] == want[1:]
