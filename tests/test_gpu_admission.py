@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2509_04377_amd import binding as pe
-from paper_2509_04377_amd.engine import FreePages, LayeredCache, PagedCache, QuantCache, empty_layout
+from paper_2509_04377_amd.engine import FreePages, GraphedStepper, LayeredCache, LayeredQuantCache, PagedCache, QuantCache, empty_layout
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -136,3 +136,55 @@ def test_pages_of_admitted_sequences_only(dt, B, shared):
                 assert torch.equal(a[pages], b[pages]) if m else bool((a[pages] == 9).all()), (mask, s)
             for a, b in zip(got[1], whole[1]):
                 assert torch.equal(a[s], b[s]) if m else bool((a[s] == 9).all()), (mask, s)
+
+
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("shared", [False, True])
+def test_replayed_steps_between_admissions(shared, quant):
+    """Sequences end and others begin between the steps of a stepper: every replay against the eager step of a model of its own."""
+    layers, width, n_spare = 2, 4, 4
+    rows = 1 if shared else Hk
+    P = layers * S * rows * (width + n_spare)
+    made, frees = [], []
+    for _ in range(2):
+        m = (LayeredQuantCache if quant else LayeredCache)(torch.bfloat16, layers, S, Hk, Hk * G, D, B, empty_layout(layers * S, Hk, width, n_spare, P, DEV, shared),
+                                                           BUDGET, shared=shared)
+        assert m.end(range(S)).numel() == 0
+        made.append(m)
+        frees.append(FreePages.of(torch.randperm(P, generator=torch.Generator().manual_seed(7)).int().to(DEV)))
+    bufs = [torch.zeros((layers, S, h, D), dtype=torch.bfloat16, device=DEV) for h in (Hk, Hk, Hk * G, Hk * G)]
+    out = torch.zeros_like(bufs[3])
+    stepper = GraphedStepper(made[0], *bufs)
+    comes = {0: [90, 0, 30], 25: [0, 64, 0], 45: [20, 0, 0], 60: [0, 0, 130]}
+    ends = {40: [0], 58: [2], 70: [1]}
+    for step in range(90):
+        if step in comes:
+            lens = comes[step]
+            kv = [[_randn(torch.Generator().manual_seed(100 * step + 10 * l + i), sum(lens), Hk, D) for i in range(2)] for l in range(layers)]
+            for i, m in enumerate(made):
+                plans = m.admit(_i32(lens), sum(lens), frees[i])
+                assert plans[0].admitted.tolist() == [int(n > 0) for n in lens]
+                for l in range(layers):
+                    if quant:
+                        stage = PagedCache.create(torch.bfloat16, S, Hk, Hk * G, D, B, empty_layout(S, Hk, width, 1, 99, DEV, shared), BUDGET, shared=shared)
+                        p = stage.admit(_i32(lens), sum(lens), FreePages.of(torch.arange(99, dtype=torch.int32, device=DEV)))
+                        stage.prefill_prune(*kv[l], p.cu_seqlens, max(lens))
+                        stage.set_host_lens(lens)
+                        m.take_layer(l, stage)
+                    else:
+                        m.prefill_prune_layer(l, *kv[l], plans[l].cu_seqlens, max(lens))
+                m.set_host_lens([n or None for n in lens])
+        g = torch.Generator().manual_seed(step)
+        for t in bufs[:3]:
+            t.copy_(torch.randn(t.shape, generator=g))
+        assert stepper.step() == made[1].decode_step(bufs[0], bufs[1], bufs[2], out)
+        torch.cuda.synchronize()
+        live = [s for s, n in enumerate(made[1].host_lens) if n >= 0]
+        assert torch.equal(bufs[3][:, live], out[:, live]), step
+        a, b = made[0].folded, made[1].folded
+        assert made[0].host_lens == made[1].host_lens and a.seq_lens.tolist() == b.seq_lens.tolist() == made[1].host_lens * layers, step
+        assert torch.equal(a.block_table, b.block_table) and torch.equal(a.spare_used, b.spare_used)
+        if step in ends:
+            for i, m in enumerate(made):
+                frees[i] = FreePages.of(torch.cat((frees[i].pages[int(frees[i].used):], m.end(ends[step]))))
+    assert len(stepper.graphs) <= 4
