@@ -249,14 +249,15 @@ PyObject* plan_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const pe_cache_desc& d = desc.d;
     const int64_t S = d.num_seqs, of_seq = d.layout == PE_LAYOUT_SHARED ? 1 : d.num_kv_heads, rows = S * of_seq, T = std::get<0>(total.c);
     const int32_t spare_each = std::get<0>(n_spare.c);
-    // the tensors and how many numbers they have room for
-    const int at[] = {2, 3, 4, 7, 8, 9, 10, 11, 12, 13, 14, 16, 17, 18, 19};
+    // the tensors, which of them may be None (negative), and how many numbers they have room for
+    const int at[] = {2, 3, -4, 7, 8, 9, -10, 11, 12, -13, -14, -16, -17, -18, -19};
     const int64_t room[] = {S, S, S, 1, 1, rows * d.max_blocks, rows * spare_each, S, 1, S + 1, T, S, rows, rows, S};
     constexpr int kTensors = sizeof(at) / sizeof(at[0]);
     int32_t* p[kTensors];
     for (int i = 0; i < kTensors; ++i) {
+      PyObject* const o = args[at[i] < 0 ? -at[i] : at[i]];
       IntsOrNone t;
-      if (!t.get(args[at[i]]) || (args[at[i]] != Py_None && THPVariable_Unpack(args[at[i]]).numel() < room[i])) Py_RETURN_NONE;
+      if (o == Py_None ? at[i] > 0 : !t.get(o) || THPVariable_Unpack(o).numel() < room[i]) Py_RETURN_NONE;
       p[i] = std::get<0>(t.c);
     }
     if (args[15] != Py_None && THPVariable_Unpack(args[15]).numel() < T * of_seq) Py_RETURN_NONE;

@@ -196,6 +196,8 @@ def test_a_plan_that_is_too_small_is_refused(native, monkeypatch):
         setattr(plan, t, whole)
     with pytest.raises(ValueError, match="new_lens must have room for"):
         c.admit(_i32([3]), 6, free)
+    with pytest.raises(pe.PeError, match="new_lens is None"):
+        c.admit(None, 6, free)
     assert c.seq_lens.tolist() == [0, 0] and int(free.used) == 0
     plan = c.admit(_i32([3, 2]), 6, free, plan=c.new_plan(9))
     assert c.seq_lens.tolist() == [3, 2] and plan.positions[:6].tolist() == [0, 1, 2, 0, 1, 0] and int(free.used) == 8
